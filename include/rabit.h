@@ -144,6 +144,97 @@ RABIT_API int rabit_linear_group(const rabit_layer* const* layers, const void* c
                        int n_layers, int batch, void* stream);
 
 /*
+ * Low-rank adapters beside a layer, of many requests at once (no counterpart in the paper, which keeps all of a layer in its
+ * binary paths): every batch row names one adapter of a shared pool, or none, and
+ *
+ *     u[t]    = A[id_t] x[t]                                    rank values per row
+ *     y[t]    = layer(x[t]) + scale[id_t] * B[id_t]^T u[t]      for 0 <= id_t < count; otherwise y[t] = layer(x[t]) and u[t] = 0
+ *
+ * Both factors are stored as `rank` rows along a side of the layer, so that the backward pass, with respect to the input, is
+ * the same operation on the transposed layer (rabit_transpose) with the factors exchanged.
+ */
+typedef struct rabit_adapters {
+    const void* a;         /* DEVICE fp16 [count][rank][n_in]   16-byte aligned: the factors that meet the input */
+    const void* b;         /* DEVICE fp16 [count][rank][n_out]  16-byte aligned: the factors that make the output, transposed */
+    const float* scale;    /* DEVICE fp32 [count] */
+    int count;             /* adapters in the pool, >= 1 */
+    int rank;              /* 1 .. RABIT_MAX_RANK, the same for all; a smaller one is filled up with zero rows */
+    int n_in, n_out;       /* N and M of the layer */
+} rabit_adapters;
+#define RABIT_MAX_RANK 128
+
+/*
+ * rabit_linear with adapters.
+ *   layer, x, y, batch, stream   as rabit_linear
+ *   adapters  HOST   the pool; n_in and n_out must be the layer's N and M
+ *   ids       DEVICE int32 [batch]: the adapter of each row; a value outside 0 .. count-1 means none
+ *   u         DEVICE fp32 [batch][rank], 16-byte aligned: receives the rows' low-rank products (the backward pass needs them; a
+ *             caller that does not gives a scratch buffer).  y and u may not overlap one another nor any input.
+ * Rows may name adapters in any order; rows of one adapter that follow one another (a prompt) share its reads.
+ * The layer's sum is rounded to fp16 in y and the adapter's part, kept in fp32, is added to that and rounded again: an error of at most
+ * half a step of the layer's sum and half a step of y.  An infinite or NaN value in a row of x or in an adapter reaches the
+ * rows that it belongs to and no others.
+ * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.
+ */
+RABIT_API int rabit_linear_adapted(const rabit_layer* layer, const rabit_adapters* adapters, const void* x, const int* ids,
+                         void* y, float* u, int batch, void* stream);
+
+/*
+ * rabit_linear_group with adapters: layer l with the pool adapters[l] (HOST array; an entry may be NULL: that layer has none, and us[l] is not
+ * used), all rows named by the one array ids.  us: HOST array of DEVICE buffers as u above.  Otherwise as rabit_linear_group.
+ */
+RABIT_API int rabit_linear_group_adapted(const rabit_layer* const* layers, const rabit_adapters* const* adapters, const void* const* xs, const int* ids,
+                               void* const* ys, float* const* us, int n_layers, int batch, void* stream);
+
+/*
+ * Gradients of the factors.  With x and u of the forward pass, dy the gradient of y and p = B dy (the u of the backward call on the transposed layer):
+ *     da[i][r][j] = scale[i] * sum over rows t with id_t = i of p[t][r] * x[t][j]
+ *     db[i][r][j] = scale[i] * sum over rows t with id_t = i of u[t][r] * dy[t][j]
+ *   x   DEVICE fp16 [batch][n_in], dy DEVICE fp16 [batch][n_out], 16-byte aligned
+ *   u, p   DEVICE fp32 [batch][rank], 16-byte aligned
+ *   da  DEVICE fp32 [count][rank][n_in], db DEVICE fp32 [count][rank][n_out], 16-byte aligned, not overlapping each other nor any input.
+ *       accumulate = 0: overwritten (zero for an adapter that no row names); otherwise the gradients are added to what is there.
+ * Only the sizes, scale and nothing else of `adapters` is read.  Sums are fp32 in an order that the sizes and ids fix: the same call
+ * gives the same bits.  What a row of another adapter, or of none, holds does not matter, be it infinite or NaN.
+ * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.  The buffers' device must be the current device.
+ */
+RABIT_API int rabit_adapter_gradients(const rabit_adapters* adapters, const void* x, const float* u, const void* dy, const float* p, const int* ids,
+                            float* da, float* db, int batch, int accumulate, void* stream);
+
+/*
+ * The layer of the transposed weight (N x M: planes transposed, g and h exchanged), made on the device from the packed image of `layer`; run on output
+ * gradients it gives input gradients.  For a layer with M a multiple of 32 (M becomes the contraction).
+ *   dev_buf   DEVICE, 256-byte aligned, dev_bytes >= rabit_packed_bytes(K, N, M), on the layer's device; as for rabit_pack
+ * Reads the scales back once (synchronises `stream`; not while it is being captured); the kernels behind that are enqueued on `stream`: the
+ * new layer may be used by later work on it.  The image is byte for byte what rabit_pack makes of the transposed planes.
+ */
+RABIT_API int rabit_transpose(const rabit_layer* layer, void* dev_buf, size_t dev_bytes, void* stream, rabit_layer** out);
+
+/*
+ * Clipping by the global norm over many gradient tensors:
+ *     norm = sqrt(sum of the squares of all elements of all tensors);   every element times min(1, max_norm / (norm + 1e-6))
+ * A rabit_gradients describes the tensors; it refers to their memory, which the caller owns and keeps in place.
+ *   tensors   HOST array of n DEVICE fp32 pointers (4-byte aligned); counts HOST array of their element counts (an empty one may be NULL)
+ *   outs      HOST array of n DEVICE fp32 pointers that receive the clipped values, or NULL to clip in place; an output is its own
+ *             tensor or overlaps none, nor another output
+ *   dev_buf   DEVICE, 256-byte aligned, at least rabit_gradients_bytes(counts, n): table and partial sums, owned by the caller
+ * rabit_gradients_bind copies the table on `stream` and returns when it has been staged.
+ */
+typedef struct rabit_gradients rabit_gradients;
+RABIT_API size_t rabit_gradients_bytes(const size_t* counts, int n);
+RABIT_API int rabit_gradients_bind(const float* const* tensors, float* const* outs, const size_t* counts, int n,
+                         void* dev_buf, size_t dev_bytes, void* stream, rabit_gradients** out);
+/*
+ *   norm_out  DEVICE fp32, receives the norm before clipping (as it is: infinite or NaN where the gradients are)
+ *   max_norm  > 0 and finite
+ * Squares are summed in 64 bits in an order that the sizes fix.  An infinite norm makes the factor 0, a NaN makes it NaN, as the formula says.
+ * Calls on one rabit_gradients must not overlap in time (they share its partial sums).
+ * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.
+ */
+RABIT_API int rabit_clip_gradients(const rabit_gradients* gradients, float max_norm, float* norm_out, void* stream);
+RABIT_API int rabit_gradients_free(rabit_gradients* gradients);
+
+/*
  * Host-buffer form of rabit_linear (same operation, Section 4.1 forward with the Eq. 2 weight)
  * for callers whose activations live in host memory:
  *   x_host  HOST fp16 [batch][N]   (pinned memory makes the copies asynchronous; up to 256 KB a kernel makes them)

@@ -21,6 +21,13 @@ from .binding import (  # noqa: F401
     PreparedGroupHost,
     rabit_linear_host,
     rabit_linear_static_scratch,
+    RabitAdapters,
+    rabit_linear_adapted,
+    rabit_linear_group_adapted,
+    rabit_transpose,
+    rabit_adapter_gradients,
+    RabitGradients,
+    rabit_clip_gradients,
     rabit_free,
     last_error,
 )

@@ -74,6 +74,22 @@ def _load() -> ctypes.CDLL:
     lib.rabit_selftest_stream_read.argtypes = [_c_void_p, _c_size_t, _c_void_p, _c_void_p]
     lib.rabit_unpack.restype = _c_int
     lib.rabit_unpack.argtypes = [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p]
+    lib.rabit_linear_adapted.restype = _c_int
+    lib.rabit_linear_adapted.argtypes = [_c_void_p] * 6 + [_c_int, _c_void_p]
+    lib.rabit_linear_group_adapted.restype = _c_int
+    lib.rabit_linear_group_adapted.argtypes = [_c_void_p] * 6 + [_c_int, _c_int, _c_void_p]
+    lib.rabit_adapter_gradients.restype = _c_int
+    lib.rabit_adapter_gradients.argtypes = [_c_void_p] * 8 + [_c_int, _c_int, _c_void_p]
+    lib.rabit_transpose.restype = _c_int
+    lib.rabit_transpose.argtypes = [_c_void_p, _c_void_p, _c_size_t, _c_void_p, ctypes.POINTER(_c_void_p)]
+    lib.rabit_gradients_bytes.restype = _c_size_t
+    lib.rabit_gradients_bytes.argtypes = [_c_void_p, _c_int]
+    lib.rabit_gradients_bind.restype = _c_int
+    lib.rabit_gradients_bind.argtypes = [_c_void_p, _c_void_p, _c_void_p, _c_int, _c_void_p, _c_size_t, _c_void_p, ctypes.POINTER(_c_void_p)]
+    lib.rabit_clip_gradients.restype = _c_int
+    lib.rabit_clip_gradients.argtypes = [_c_void_p, ctypes.c_float, _c_void_p, _c_void_p]
+    lib.rabit_gradients_free.restype = _c_int
+    lib.rabit_gradients_free.argtypes = [_c_void_p]
     for name in ("rabit_layer_K", "rabit_layer_M", "rabit_layer_N"):
         getattr(lib, name).restype = _c_int
         getattr(lib, name).argtypes = [_c_void_p]
@@ -97,7 +113,8 @@ except ImportError as e:
     raise ImportError(f"the native binding module is missing or does not load ({e}): build it with "
                       "`python paper_2602_05367_b200/build.py`") from e
 _native.init(RabitError, *(ctypes.cast(getattr(_lib, name), _c_void_p).value for name in
-                           ("rabit_linear", "rabit_linear_group", "rabit_linear_group_host", "rabit_layer_M", "rabit_layer_N", "rabit_last_error")))
+                           ("rabit_linear", "rabit_linear_group", "rabit_linear_group_host", "rabit_layer_M", "rabit_layer_N", "rabit_last_error",
+                            "rabit_linear_adapted", "rabit_linear_group_adapted")))
 
 
 def _stream_of(device, stream: Optional[int]) -> int:
@@ -355,6 +372,144 @@ def rabit_linear_static_scratch(layer: RabitLayer, x, y, stream: Optional[int] =
     with torch.cuda.device(x.device):
         _check(_lib.rabit_linear_static_scratch(layer.handle, _c_void_p(x.data_ptr()), _c_void_p(y.data_ptr()), batch, _c_void_p(st)))
     return y
+
+
+class _AdaptersStruct(ctypes.Structure):
+    """rabit_adapters of include/rabit.h"""
+    _fields_ = [("a", _c_void_p), ("b", _c_void_p), ("scale", _c_void_p), ("count", _c_int), ("rank", _c_int), ("n_in", _c_int), ("n_out", _c_int)]
+
+
+class RabitAdapters:
+    """A pool of low-rank adapters beside a layer: a [count][rank][N] and b [count][rank][M] contiguous CUDA float16 (b: the usual second
+    factor [M][rank], transposed), scale [count] CUDA float32.  Holds the tensors; their values may change between calls."""
+
+    def __init__(self, a, b, scale):
+        if a.dtype != torch.float16 or b.dtype != torch.float16 or scale.dtype != torch.float32:
+            raise ValueError("a and b must be float16, scale float32")
+        if a.dim() != 3 or b.dim() != 3 or scale.dim() != 1 or a.shape[:2] != b.shape[:2] or scale.shape[0] != a.shape[0]:
+            raise ValueError("a must be [count][rank][N], b [count][rank][M], scale [count]")
+        for t in (a, b, scale):
+            if not t.is_cuda or not t.is_contiguous() or t.device != a.device:
+                raise ValueError("a, b and scale must be contiguous CUDA tensors on one device")
+        self.a, self.b, self.scale = a, b, scale
+        self.count, self.rank, self.N, self.M = a.shape[0], a.shape[1], a.shape[2], b.shape[2]
+        self._struct = _AdaptersStruct(a.data_ptr(), b.data_ptr(), scale.data_ptr(), self.count, self.rank, self.N, self.M)
+        self._addr = ctypes.addressof(self._struct)
+
+    def transposed(self) -> "RabitAdapters":
+        """The same adapters beside the transposed layer (rabit_transpose): the factors exchanged, no copy."""
+        return RabitAdapters(self.b, self.a, self.scale)
+
+
+def rabit_linear_adapted(layer: RabitLayer, adapters: RabitAdapters, x, ids, y=None, u=None, stream: Optional[int] = None):
+    """y[t] = layer(x[t]) + scale[i] * b[i]^T (a[i] x[t]) with i = ids[t] (CUDA int32 [batch]; outside the pool: no adapter).  u, if given,
+    receives the low-rank products (CUDA float32 [batch][rank]; zero for rows without adapter).  Returns y [batch][M].
+    With rabit_transpose(layer) and adapters.transposed() and the gradient of y as x it gives the gradient of x."""
+    return _native.linear_adapted(layer, adapters, x, ids, y, u, stream)
+
+
+def rabit_linear_group_adapted(layers, adapters, xs, ids, ys, us=None, stream: Optional[int] = None):
+    """rabit_linear_group with adapters: layer l with the pool adapters[l] (None: that layer has none), all rows named by the one tensor
+    ids.  us, if given: per layer None or the tensor that receives its low-rank products."""
+    return _native.linear_group_adapted(layers, adapters, xs, ids, ys, us, stream)
+
+
+def rabit_transpose(layer: RabitLayer, stream: Optional[int] = None) -> RabitLayer:
+    """The layer of the transposed weight, [N][M] (M a multiple of 32): output gradients in, input gradients out.  A load-time step."""
+    K, M, N = layer.K, layer.N, layer.M
+    handle, dev = layer.handle, layer.dev_buf.device
+    nbytes = packed_bytes(K, M, N)
+    if nbytes == 0:
+        raise RabitError(-2, f"rabit_transpose: the layer's M = {N} becomes the contraction and must be a multiple of 32")
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    st = _stream_of(dev, stream)
+    out = _c_void_p()
+    with torch.cuda.device(dev):
+        _check(_lib.rabit_transpose(handle, _c_void_p(buf.data_ptr()), nbytes, _c_void_p(st), ctypes.byref(out)))
+    return RabitLayer(out.value, buf, K, M, N)
+
+
+def _dense(name, t, dtype, shape, device):
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != int(np.prod(shape)) or t.device != device:
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of {'*'.join(map(str, shape))} elements on the adapters' device")
+    return t.data_ptr()
+
+
+def rabit_adapter_gradients(adapters: RabitAdapters, x, u, dy, p, ids, da=None, db=None, accumulate: bool = False, stream: Optional[int] = None):
+    """Gradients of the factors: da[i] = scale[i] * sum of p[t]^T x[t] and db[i] = scale[i] * sum of u[t]^T dy[t] over the rows t with
+    ids[t] = i.  x float16 [batch][N] and u float32 [batch][rank] of the forward call, dy float16 [batch][M] and p float32 [batch][rank]
+    of the backward call on the transposed layer.  da, db: CUDA float32 like a and b, overwritten or, with `accumulate`, added to."""
+    A, dev = adapters, adapters.a.device
+    batch = ids.numel()
+    if accumulate and (da is None or db is None):
+        raise ValueError("accumulate needs da and db")
+    if da is None:
+        da = torch.empty(A.a.shape, dtype=torch.float32, device=dev)
+    if db is None:
+        db = torch.empty(A.b.shape, dtype=torch.float32, device=dev)
+    args = [_dense("x", x, torch.float16, (batch, A.N), dev), _dense("u", u, torch.float32, (batch, A.rank), dev), _dense("dy", dy, torch.float16, (batch, A.M), dev),
+            _dense("p", p, torch.float32, (batch, A.rank), dev), _dense("ids", ids, torch.int32, (batch,), dev), _dense("da", da, torch.float32, A.a.shape, dev),
+            _dense("db", db, torch.float32, A.b.shape, dev)]
+    st = _stream_of(dev, stream)
+    with torch.cuda.device(dev):
+        _check(_lib.rabit_adapter_gradients(_c_void_p(A._addr), *map(_c_void_p, args), batch, 1 if accumulate else 0, _c_void_p(st)))
+    return da, db
+
+
+class RabitGradients:
+    """Gradient tensors (contiguous CUDA float32, any number of them, all on one device) that rabit_clip_gradients treats as one vector; clipped
+    in place, or into `outs`.  Holds the tensors and the buffer with their table and the partial sums."""
+
+    def __init__(self, tensors, outs=None, stream: Optional[int] = None):
+        tensors, outs = list(tensors), None if outs is None else list(outs)
+        n = len(tensors)
+        if n < 1 or (outs is not None and [t.numel() for t in outs] != [t.numel() for t in tensors]):
+            raise ValueError("at least one tensor, and as many outs of the same sizes")
+        dev = tensors[0].device
+        for t in tensors + (outs or []):
+            if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.device != dev:
+                raise ValueError("gradients must be contiguous CUDA float32 tensors on one device")
+        counts = (_c_size_t * n)(*[t.numel() for t in tensors])
+        src = (_c_void_p * n)(*[t.data_ptr() for t in tensors])
+        dst = None if outs is None else (_c_void_p * n)(*[t.data_ptr() for t in outs])
+        self._keep = (tensors, outs)
+        nbytes = int(_lib.rabit_gradients_bytes(counts, n))
+        self._handle = None
+        self.dev_buf = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        out = _c_void_p()
+        with torch.cuda.device(dev):
+            _check(_lib.rabit_gradients_bind(src, dst, counts, n, _c_void_p(self.dev_buf.data_ptr()), nbytes, _c_void_p(_stream_of(dev, stream)), ctypes.byref(out)))
+        self._handle = out
+
+    @property
+    def handle(self) -> ctypes.c_void_p:
+        if self._handle is None:
+            raise RabitError(-1, "gradients already freed")
+        return self._handle
+
+    def free(self) -> None:
+        if self._handle is not None:
+            _lib.rabit_gradients_free(self._handle)
+            self._handle = self._keep = self.dev_buf = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def rabit_clip_gradients(gradients: RabitGradients, max_norm: float, norm=None, stream: Optional[int] = None):
+    """Every gradient times min(1, max_norm / (norm + 1e-6)) with the norm over all of them; returns the norm (CUDA float32 [1])."""
+    handle, dev = gradients.handle, gradients.dev_buf.device
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    else:
+        _dense("norm", norm, torch.float32, (1,), dev)
+    st = _stream_of(dev, stream)
+    with torch.cuda.device(dev):
+        _check(_lib.rabit_clip_gradients(handle, max_norm, _c_void_p(norm.data_ptr()), _c_void_p(st)))
+    return norm
 
 
 def rabit_free(layer: RabitLayer) -> None:

@@ -17,7 +17,8 @@ LIB = os.path.join(HERE, "librabit.so")
 LIB_TRACE = os.path.join(HERE, "librabit_trace.so")          # the same sources with -DRABIT_TRACE (phase stamps)
 LIB_CHECKED = os.path.join(HERE, "librabit_checked.so")      # the same sources with -DRABIT_CHECKED (index checks in the GEMVs and the GEMM)
 SOURCES = ["rabit_api.cu", "rabit_pack.cu", "rabit_gemv_plain.cu", "rabit_gemv_mma.cu", "rabit_gemv_lut.cu", "rabit_gemv_f16.cu", "rabit_gemm_tc.cu",
-           "rabit_noalloc.cu", "rabit_fetch.cu", "rabit_derive.cu", "rabit_selftest.cu"]
+           "rabit_noalloc.cu", "rabit_fetch.cu", "rabit_derive.cu", "rabit_adapters.cu", "rabit_clip.cu", "rabit_selftest.cu"]
+HEADER = os.path.join(HERE, "..", "include", "rabit.h")
 BINDING_SOURCE = os.path.join(CSRC, "rabit_binding.cpp")
 BINDING = os.path.join(HERE, "_rabit_binding" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 NVCC_FLAGS = [
@@ -35,13 +36,13 @@ def needs_build() -> bool:
         return True
     t = os.path.getmtime(LIB)
     deps = _sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    deps.append(os.path.join(HERE, "..", "include", "rabit.h"))
+    deps.append(HEADER)
     return any(os.path.getmtime(d) > t for d in deps)
 
 
 def build_binding(force: bool = False, verbose: bool = False) -> str:
     """The CPython module of the hot calls (csrc/rabit_binding.cpp)."""
-    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= os.path.getmtime(BINDING_SOURCE):
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(BINDING) >= os.path.getmtime(f) for f in (BINDING_SOURCE, HEADER)):
         return BINDING
     import importlib.util
     root = os.path.dirname(importlib.util.find_spec("torch").origin)           # (torch itself need not be imported to build)

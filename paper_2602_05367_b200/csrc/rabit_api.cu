@@ -135,10 +135,60 @@ extern "C" int rabit_derive_pack(const float* W_dev, const uint16_t* g, const ui
     return RABIT_OK;
 }
 
-static bool ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
-    uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-    return a0 < b0 + bn && b0 < a0 + an;
+static int transpose_call(const rabit_layer* layer, void* dev_buf, size_t dev_bytes, void* stream, rabit_layer** out) {
+    rabit_clear_error();
+    if (!out) return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: out is NULL");
+    *out = nullptr;
+    if (!layer || !dev_buf) return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: null layer or dev_buf");
+    if (((uintptr_t)dev_buf & 255u) != 0) return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: dev_buf must be 256-byte aligned");
+    const RabitGeom& F = layer->geom;
+    const int K = F.K, M = F.N, N = F.M;                               // of the new layer
+    RabitGeom G;
+    if (!rabit_make_geom(K, M, N, &G))
+        return rabit_fail(RABIT_UNSUPPORTED_SHAPE, "rabit_transpose: the layer's M = %d becomes the contraction and must be a multiple of 32", N);
+    const size_t need = rabit_packed_bytes(K, M, N);
+    if (dev_bytes < need) return rabit_fail(RABIT_BUFFER_TOO_SMALL, "rabit_transpose: dev_buf holds %zu bytes, layer needs %zu", dev_bytes, need);
+    if (rabit_ranges_overlap(dev_buf, need, layer->dev_base, layer->dev_bytes)) return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: dev_buf overlaps the layer's image");
+    cudaStream_t st = (cudaStream_t)stream;
+    int dev = -1;
+    RABIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != layer->device)
+        return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: the layer lives on device %d but device %d is current", layer->device, dev);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    RABIT_CUDA_TRY(cudaStreamIsCapturing(st, &capturing));
+    if (capturing != cudaStreamCaptureStatusNone) return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: the stream is being captured");
+    cudaPointerAttributes attr;
+    RABIT_CUDA_TRY(cudaPointerGetAttributes(&attr, dev_buf));
+    if ((attr.type != cudaMemoryTypeDevice && attr.type != cudaMemoryTypeManaged) || attr.device != layer->device)
+        return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: dev_buf is not memory of the layer's device");
+
+    // The scales decide the fixed-point grid of the new layer on the host, which does not keep them: they come back (a few KB).
+    std::vector<uint16_t> g((size_t)K * M), h((size_t)K * N), padded((size_t)K * F.Mp);
+    RABIT_CUDA_TRY(cudaMemcpyAsync(padded.data(), layer->d_g, padded.size() * 2, cudaMemcpyDeviceToHost, st));
+    RABIT_CUDA_TRY(cudaMemcpyAsync(g.data(), layer->d_h, g.size() * 2, cudaMemcpyDeviceToHost, st));
+    RABIT_CUDA_TRY(cudaStreamSynchronize(st));
+    for (int k = 0; k < K; ++k) std::memcpy(h.data() + (size_t)k * N, padded.data() + (size_t)k * F.Mp, (size_t)N * 2);
+    RabitHeader hdr;
+    std::vector<uint8_t> tail;
+    if (!rabit_build_meta(g.data(), h.data(), K, M, N, &G, &hdr, &tail)) return rabit_fail(RABIT_UNSUPPORTED_SHAPE, "rabit_transpose: unsupported shape");
+    char* base = (char*)dev_buf;
+    RABIT_CUDA_TRY(cudaMemcpyAsync(base + hdr.off_g, tail.data(), tail.size(), cudaMemcpyHostToDevice, st));
+    cudaError_t e = rabit_launch_transpose(G, hdr, base, F, layer->d_bits, st);
+    if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "rabit_transpose: launch failed: %s", cudaGetErrorString(e));
+    // (a fill behind the kernel that writes the weights: see rabit_derive_pack)
+    RABIT_CUDA_TRY(cudaMemsetAsync(base + hdr.off_acc, 0, (size_t)(hdr.total_bytes - hdr.off_acc), st));
+    rabit_layer* L = new (std::nothrow) rabit_layer;
+    if (!L) return rabit_fail(RABIT_INVALID_ARG, "rabit_transpose: out of host memory");
+    bind_layer(L, G, hdr, dev_buf, layer->device);
+    *out = L;
+    return RABIT_OK;
 }
+
+extern "C" int rabit_transpose(const rabit_layer* layer, void* dev_buf, size_t dev_bytes, void* stream, rabit_layer** out) {
+    return rabit_guarded("rabit_transpose", [&] { return transpose_call(layer, dev_buf, dev_bytes, stream, out); });
+}
+
+static bool ranges_overlap(const void* a, size_t an, const void* b, size_t bn) { return rabit_ranges_overlap(a, an, b, bn); }
 
 // Rows up to which the f16 GEMV is the faster of the two tensor-core kernels: its MMAs carry eight rows, a second set for 9 to
 // 16 makes it slower than the GEMM, which costs the same from 1 to 16 (B200, us at 8 / 9 / 16 rows against the GEMM:

@@ -1,0 +1,170 @@
+// The global norm over many gradient tensors, and clipping by it.
+//
+//   norm = sqrt(sum g^2),   g * min(1, max_norm / (norm + 1e-6))
+//
+// Two kernels: partial sums of squares, one per CTA; then every CTA adds all of them in the same order, which is cheaper than a third
+// launch, and scales its share.  Bound: memory (4 bytes in, 4 out per element; the second reading hits L2 up to its size).
+// Squares are taken and summed in 64 bits: an fp32 gradient of 1e20 has no fp32 square, and the conversion and the double add cost less than the bytes.
+#include <algorithm>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "rabit_internal.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr size_t kChunk = 8192;                       // elements that a CTA takes at a time
+constexpr int kMaxGrid = 1024;
+
+struct Chunk {                                        // a piece of one tensor
+    const float* src;
+    float* dst;
+    unsigned long long n;
+};
+
+__device__ __forceinline__ double block_sum(double v, double* warps) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) s += warps[w];
+    return s;
+}
+
+__global__ void __launch_bounds__(kThreads) squares_kernel(const Chunk* __restrict__ chunks, int n_chunks, double* __restrict__ partial) {
+    __shared__ double warps[kThreads / 32];
+    double sum = 0.0;
+    for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+        const Chunk ch = chunks[c];
+        for (unsigned i = threadIdx.x; i < ch.n; i += kThreads) {
+            const double v = ch.src[i];
+            sum = fma(v, v, sum);
+        }
+    }
+    sum = block_sum(sum, warps);
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+__global__ void __launch_bounds__(kThreads) scale_kernel(const Chunk* __restrict__ chunks, int n_chunks, const double* __restrict__ partial, double max_norm, float* __restrict__ norm_out) {
+    __shared__ double warps[kThreads / 32];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) sum += partial[i];
+    const double norm = sqrt(block_sum(sum, warps));
+    double f = max_norm / (norm + 1e-6);
+    if (f > 1.0) f = 1.0;                             // (a NaN stays)
+    const float factor = (float)f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+        const Chunk ch = chunks[c];
+        if (ch.dst == ch.src && factor == 1.f) continue;
+        for (unsigned i = threadIdx.x; i < ch.n; i += kThreads) ch.dst[i] = ch.src[i] * factor;
+    }
+}
+
+size_t chunks_of(const size_t* counts, int n) {
+    size_t total = 0;
+    for (int i = 0; i < n; ++i) total += (counts[i] + kChunk - 1) / kChunk;
+    return total;
+}
+
+}  // namespace
+
+struct rabit_gradients {
+    int device, n_chunks, grid;
+    const Chunk* chunks;
+    double* partial;
+};
+
+// table of chunks | one partial sum per CTA
+extern "C" size_t rabit_gradients_bytes(const size_t* counts, int n) {
+    if (!counts || n < 1) return 0;
+    return rabit_align256(chunks_of(counts, n) * sizeof(Chunk)) + kMaxGrid * sizeof(double);
+}
+
+static int bind_call(const float* const* tensors, float* const* outs, const size_t* counts, int n, void* dev_buf, size_t dev_bytes, void* stream, rabit_gradients** out) {
+    const char* who = "rabit_gradients_bind";
+    rabit_clear_error();
+    if (!out) return rabit_fail(RABIT_INVALID_ARG, "%s: out is NULL", who);
+    *out = nullptr;
+    if (!tensors || !counts || !dev_buf) return rabit_fail(RABIT_INVALID_ARG, "%s: null pointer", who);
+    if (n < 1) return rabit_fail(RABIT_INVALID_ARG, "%s: n must be >= 1 (got %d)", who, n);
+    if (((uintptr_t)dev_buf & 255u) != 0) return rabit_fail(RABIT_INVALID_ARG, "%s: dev_buf must be 256-byte aligned", who);
+    for (int i = 0; i < n; ++i) {
+        if (counts[i] > ((size_t)1 << 40)) return rabit_fail(RABIT_INVALID_ARG, "%s: tensor %d has %zu elements", who, i, counts[i]);
+        if (counts[i] && (!tensors[i] || (outs && !outs[i]))) return rabit_fail(RABIT_INVALID_ARG, "%s: null tensor %d", who, i);
+        if (counts[i] && ((((uintptr_t)tensors[i]) & 3u) || (outs && (((uintptr_t)outs[i]) & 3u)))) return rabit_fail(RABIT_INVALID_ARG, "%s: tensor %d is misaligned", who, i);
+    }
+    const size_t n_chunks = chunks_of(counts, n);
+    if (n_chunks > 0x7FFFFFFFu) return rabit_fail(RABIT_UNSUPPORTED_SHAPE, "%s: too many elements", who);
+    const size_t need = rabit_gradients_bytes(counts, n), table_bytes = rabit_align256(n_chunks * sizeof(Chunk));
+    if (dev_bytes < need) return rabit_fail(RABIT_BUFFER_TOO_SMALL, "%s: dev_buf holds %zu bytes, need %zu", who, dev_bytes, need);
+    // what is written overlaps nothing else: a sweep over all ranges by their starts
+    struct Span {
+        uintptr_t at, end;
+        bool written;
+    };
+    std::vector<Span> spans;
+    spans.push_back({(uintptr_t)dev_buf, (uintptr_t)dev_buf + need, true});
+    for (int i = 0; i < n; ++i) {
+        if (!counts[i]) continue;
+        const uintptr_t s = (uintptr_t)tensors[i], d = outs ? (uintptr_t)outs[i] : s;
+        if (s != d) spans.push_back({s, s + counts[i] * 4, false});
+        spans.push_back({d, d + counts[i] * 4, true});
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+    uintptr_t end_all = 0, end_written = 0;
+    for (const Span& s : spans) {
+        if ((s.written && end_all > s.at) || end_written > s.at) return rabit_fail(RABIT_INVALID_ARG, "%s: an output overlaps another tensor or dev_buf", who);
+        end_all = std::max(end_all, s.end);
+        if (s.written) end_written = std::max(end_written, s.end);
+    }
+    cudaPointerAttributes attr;
+    RABIT_CUDA_TRY(cudaPointerGetAttributes(&attr, dev_buf));
+    if (attr.type != cudaMemoryTypeDevice && attr.type != cudaMemoryTypeManaged) return rabit_fail(RABIT_INVALID_ARG, "%s: dev_buf is not device memory", who);
+    std::vector<Chunk> table;
+    table.reserve(n_chunks);
+    for (int i = 0; i < n; ++i)
+        for (size_t at = 0; at < counts[i]; at += kChunk)
+            table.push_back(Chunk{tensors[i] + at, outs ? outs[i] + at : const_cast<float*>(tensors[i]) + at, (unsigned long long)std::min(kChunk, counts[i] - at)});
+    if (!table.empty()) RABIT_CUDA_TRY(cudaMemcpyAsync(dev_buf, table.data(), table.size() * sizeof(Chunk), cudaMemcpyHostToDevice, (cudaStream_t)stream));
+    int sms = 0;
+    RABIT_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, attr.device));
+    rabit_gradients* R = new rabit_gradients;
+    R->device = attr.device;
+    R->n_chunks = (int)n_chunks;
+    R->grid = (int)std::max<size_t>(1, std::min<size_t>(n_chunks, std::min(4 * sms, kMaxGrid)));
+    R->chunks = (const Chunk*)dev_buf;
+    R->partial = (double*)((char*)dev_buf + table_bytes);
+    *out = R;
+    return RABIT_OK;
+}
+
+extern "C" int rabit_gradients_bind(const float* const* tensors, float* const* outs, const size_t* counts, int n, void* dev_buf, size_t dev_bytes, void* stream, rabit_gradients** out) {
+    return rabit_guarded("rabit_gradients_bind", [&] { return bind_call(tensors, outs, counts, n, dev_buf, dev_bytes, stream, out); });
+}
+
+extern "C" int rabit_clip_gradients(const rabit_gradients* R, float max_norm, float* norm_out, void* stream) {
+    const char* who = "rabit_clip_gradients";
+    rabit_clear_error();
+    if (!R || !norm_out || (((uintptr_t)norm_out) & 3u)) return rabit_fail(RABIT_INVALID_ARG, "%s: gradients or norm_out is NULL or misaligned", who);
+    if (!(max_norm > 0.f) || !(max_norm <= 3.402823466e38f)) return rabit_fail(RABIT_INVALID_ARG, "%s: max_norm must be positive and finite", who);
+    int dev = -1;
+    RABIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != R->device) return rabit_fail(RABIT_INVALID_ARG, "%s: the gradients live on device %d but device %d is current", who, R->device, dev);
+    cudaStream_t st = (cudaStream_t)stream;
+    squares_kernel<<<R->grid, kThreads, 0, st>>>(R->chunks, R->n_chunks, R->partial);
+    scale_kernel<<<R->grid, kThreads, 0, st>>>(R->chunks, R->n_chunks, R->partial, (double)max_norm, norm_out);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return RABIT_OK;
+}
+
+extern "C" int rabit_gradients_free(rabit_gradients* R) {
+    rabit_clear_error();
+    delete R;
+    return RABIT_OK;
+}

@@ -223,18 +223,11 @@ rabit_planes_to_lut_kernel(RabitGeom G, const uint32_t* __restrict__ planes, uin
     }
 }
 
-// Look-up blocks -> sign tiles: one CTA per (row tile, slice), one warp per column tile.  A tile word is eight rows of four
-// columns: eight nibbles, each spread over the four bytes and shifted to its row block's bit.
-__global__ void __launch_bounds__(kWarps * 32)
-rabit_lut_to_tiles_kernel(RabitGeom G, const uint4* __restrict__ lut, uint4* __restrict__ tiles, const __grid_constant__ Fills F) {
-    __shared__ __align__(16) unsigned char bytes[4 * RABIT_MAX_K * RABIT_LUT_PART_BYTES];
+// The calling warp's sign tile (row tile rt, column tile ct) of every path from the look-up bytes of its row tile and slice in shared memory.  A tile
+// word is eight rows of four columns: eight nibbles, each spread over the four bytes and shifted to its row block's bit.
+__device__ __forceinline__ void tiles_of_bytes(const RabitGeom& G, const unsigned char* bytes, int rt, int ct, uint4* __restrict__ tiles) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int rt = blockIdx.x / G.n_cs, cs = blockIdx.x - rt * G.n_cs, ct = cs * kWarps + warp;
     const int gq = lane >> 2, tq = lane & 3;
-    do_fills(F);
-    const uint4* src = lut + ((size_t)cs * G.n_rb + 4 * rt) * G.K * (RABIT_LUT_PART_BYTES / 16);
-    for (int i = threadIdx.x; i < 4 * G.K * (RABIT_LUT_PART_BYTES / 16); i += kWarps * 32) reinterpret_cast<uint4*>(bytes)[i] = src[i];
-    __syncthreads();
     if (ct >= G.n_ct) return;
     for (int k = 0; k < G.K; ++k) {
         uint32_t o[4];
@@ -249,6 +242,61 @@ rabit_lut_to_tiles_kernel(RabitGeom G, const uint4* __restrict__ lut, uint4* __r
         }
         tiles[rabit_tile_pos(G, rt, k, ct) * 32 + lane] = make_uint4(o[0], o[1], o[2], o[3]);
     }
+}
+
+// Look-up blocks -> sign tiles: one CTA per (row tile, slice), one warp per column tile.
+__global__ void __launch_bounds__(kWarps * 32)
+rabit_lut_to_tiles_kernel(RabitGeom G, const uint4* __restrict__ lut, uint4* __restrict__ tiles, const __grid_constant__ Fills F) {
+    __shared__ __align__(16) unsigned char bytes[4 * RABIT_MAX_K * RABIT_LUT_PART_BYTES];
+    const int rt = blockIdx.x / G.n_cs, cs = blockIdx.x - rt * G.n_cs, ct = cs * kWarps + (threadIdx.x >> 5);
+    do_fills(F);
+    const uint4* src = lut + ((size_t)cs * G.n_rb + 4 * rt) * G.K * (RABIT_LUT_PART_BYTES / 16);
+    for (int i = threadIdx.x; i < 4 * G.K * (RABIT_LUT_PART_BYTES / 16); i += kWarps * 32) reinterpret_cast<uint4*>(bytes)[i] = src[i];
+    __syncthreads();
+    tiles_of_bytes(G, bytes, rt, ct, tiles);
+}
+
+// Sign tiles of a layer -> both arrangements of its transpose: one CTA per (row tile, slice) of the new layer, which are two row tiles x four column
+// tiles of the old one.  The bits of one old column in sixteen old rows 16p + 8 alo + 0..7 sit in eight lanes' bytes, bit p: an 8 x 8 bit
+// matrix, transposed, is the byte groups 2p + alo of a new row.  A load-time step, bound by the launch and its memory round trips.
+__device__ __forceinline__ uint64_t transpose_8x8(uint64_t v) {                 // bit c of byte r -> bit r of byte c
+    uint64_t t = (v ^ (v >> 7)) & 0x00AA00AA00AA00AAULL;
+    v ^= t ^ (t << 7);
+    t = (v ^ (v >> 14)) & 0x0000CCCC0000CCCCULL;
+    v ^= t ^ (t << 14);
+    t = (v ^ (v >> 28)) & 0x00000000F0F0F0F0ULL;
+    return v ^ t ^ (t << 28);
+}
+__global__ void __launch_bounds__(kWarps * 32)
+rabit_transpose_kernel(RabitGeom G, RabitGeom from, const uint4* __restrict__ src, uint4* __restrict__ lut, uint4* __restrict__ tiles, const __grid_constant__ Fills F) {
+    constexpr int kTiles = 4;                                                   // old column tiles of a new row tile
+    static_assert(kTiles * RABIT_TILE_COLS == RABIT_TILE_ROWS && 2 * RABIT_TILE_ROWS == RABIT_LUT_COLS, "a new (row tile, slice) is 2 x 4 old tiles");
+    __shared__ __align__(16) unsigned char bytes[4 * RABIT_MAX_K * RABIT_LUT_PART_BYTES];
+    __shared__ __align__(16) unsigned char old[2 * RABIT_MAX_K * kTiles * RABIT_TILE_BYTES];
+    const int rt = blockIdx.x / G.n_cs, cs = blockIdx.x - rt * G.n_cs, K = G.K;
+    do_fills(F);
+    for (int i = threadIdx.x; i < 2 * K * kTiles * (RABIT_TILE_BYTES / 16); i += kWarps * 32) {
+        const int lane = i & 31, t = (i >> 5) % kTiles, k = (i >> 5) / kTiles % K, half = (i >> 5) / (kTiles * K);
+        const int ort = 2 * cs + half, oct = kTiles * rt + t;
+        const bool inside = ort < from.n_rt && oct < from.n_ct;
+        reinterpret_cast<uint4*>(old)[i] = inside ? src[rabit_tile_pos(from, ort, k, oct) * 32 + lane] : make_uint4(0u, 0u, 0u, 0u);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * K * RABIT_TILE_ROWS * 2; i += kWarps * 32) {
+        const int rl = i & (RABIT_TILE_ROWS - 1), alo = (i / RABIT_TILE_ROWS) & 1, k = i / (2 * RABIT_TILE_ROWS) % K, half = i / (2 * RABIT_TILE_ROWS * K);
+        const int jj = rl & 31;                                                 // old column inside its tile
+        const unsigned char* p = old + (((half * K + k) * kTiles) + (rl >> 5)) * RABIT_TILE_BYTES + ((jj >> 2) & 3) * 16 + (alo | ((jj >> 4) << 1)) * 4 + (jj & 3);
+        uint64_t v = 0;
+#pragma unroll
+        for (int gq = 0; gq < 8; ++gq) v |= (uint64_t)p[gq * 64] << (8 * gq);
+        v = transpose_8x8(v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) bytes[slice_byte(K, k, rl, 16 * half + 2 * q + alo)] = (unsigned char)(v >> (8 * q));
+    }
+    __syncthreads();
+    uint4* dst = lut + ((size_t)cs * G.n_rb + 4 * rt) * K * (RABIT_LUT_PART_BYTES / 16);
+    for (int i = threadIdx.x; i < 4 * K * (RABIT_LUT_PART_BYTES / 16); i += kWarps * 32) dst[i] = reinterpret_cast<const uint4*>(bytes)[i];
+    tiles_of_bytes(G, bytes, rt, cs * kWarps + (threadIdx.x >> 5), tiles);
 }
 
 void make_fills(const RabitHeader& hdr, char* base, Fills* F) {
@@ -304,5 +352,14 @@ cudaError_t rabit_launch_pack_planes(const RabitGeom& G, const RabitHeader& hdr,
     uint4 *tiles = reinterpret_cast<uint4*>(base + hdr.off_bits), *lut = reinterpret_cast<uint4*>(base + hdr.off_lut);
     rabit_planes_to_lut_kernel<<<(unsigned int)((blocks * 4 + kWarps - 1) / kWarps), kWarps * 32, 0, stream>>>(G, planes, lut);
     rabit_lut_to_tiles_kernel<<<(unsigned int)blocks, kWarps * 32, 0, stream>>>(G, lut, tiles, F);
+    return cudaGetLastError();
+}
+
+cudaError_t rabit_launch_transpose(const RabitGeom& G, const RabitHeader& hdr, char* base, const RabitGeom& from, const uint4* from_tiles, cudaStream_t stream) {
+    const long long blocks = (long long)G.n_rt * G.n_cs;
+    if (blocks > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+    Fills F;
+    make_fills(hdr, base, &F);
+    rabit_transpose_kernel<<<(unsigned int)blocks, kWarps * 32, 0, stream>>>(G, from, from_tiles, reinterpret_cast<uint4*>(base + hdr.off_lut), reinterpret_cast<uint4*>(base + hdr.off_bits), F);
     return cudaGetLastError();
 }

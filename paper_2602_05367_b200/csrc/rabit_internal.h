@@ -68,8 +68,16 @@ bool rabit_build_meta(const uint16_t* g, const uint16_t* h, int K, int M, int N,
 cudaError_t rabit_launch_derive(const RabitGeom& G, const RabitHeader& hdr, char* base, const float* W, cudaStream_t stream);
 cudaError_t rabit_launch_pack_planes(const RabitGeom& G, const RabitHeader& hdr, char* base, const uint32_t* planes, cudaStream_t stream);
 
+// The same from the sign tiles of another layer, of which the new one (geometry G) is the transpose.
+cudaError_t rabit_launch_transpose(const RabitGeom& G, const RabitHeader& hdr, char* base, const RabitGeom& from, const uint4* from_tiles, cudaStream_t stream);
+
 // up to 8 copies from device-visible host memory to the device by a kernel (rabit_fetch.cu); sizes are multiples of 16 bytes
 cudaError_t rabit_launch_fetch(const void* const* src, void* const* dst, const size_t* bytes, int n, cudaStream_t stream);
+
+inline bool rabit_ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+    return a0 < b0 + bn && b0 < a0 + an;
+}
 
 // kernel launchers; each enqueues on `stream` and returns a cudaError_t from the launch
 cudaError_t rabit_launch_plain(const rabit_layer& L, const void* x, void* y, int batch, cudaStream_t stream);
