@@ -4,6 +4,7 @@
 //   da[i] = scale[i] * sum_{t: id_t = i} p[t] x[t]^T,   db[i] = scale[i] * sum_{t: id_t = i} u[t] dy[t]^T
 //
 // Every factor is `rank` rows along a side of the layer, so both products of the forward pass and of the input gradient are the same two kernels.
+#include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -13,57 +14,487 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+namespace cg = cooperative_groups;
 
-// u[t][j] = sum_n A[id][j][n] x[t][n]: one CTA per row, a warp per rank row.
-__global__ void __launch_bounds__(kThreads) narrow_kernel(const __half* __restrict__ x, const int* __restrict__ ids, const __half* __restrict__ a, float* __restrict__ u, int count, int rank, int n) {
-    const int t = blockIdx.x, id = ids[t], lane = threadIdx.x & 31;
-    const bool some = id >= 0 && id < count;
-    const uint4* xr = reinterpret_cast<const uint4*>(x + (size_t)t * n);
-    for (int j = threadIdx.x >> 5; j < rank; j += kThreads / 32) {
-        float sum = 0.f;
-        if (some) {
-            const uint4* ar = reinterpret_cast<const uint4*>(a + ((size_t)id * rank + j) * n);
-            for (int i = lane; i < n / 8; i += 32) {
-                const uint4 av = ar[i], xv = xr[i];
-                const __half2 *ah = reinterpret_cast<const __half2*>(&av), *xh = reinterpret_cast<const __half2*>(&xv);
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxGroup = 8;                           // layers in one launch
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], float b0, float b1) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(__float_as_uint(b0)), "r"(__float_as_uint(b1)));
+}
+// An fp32 value as the sum of two tf32 values: its top 11 bits, and the top 11 bits of the rest (off by less than 2^-21 of it).  What is exact in
+// the first part has no second one, infinities among it.
+__device__ __forceinline__ void split_tf32(float v, uint32_t& hi, uint32_t& lo) {
+    hi = __float_as_uint(v) & 0xFFFFE000u;
+    const float top = __uint_as_float(hi);
+    lo = top == v ? 0u : __float_as_uint(v - top) & 0xFFFFE000u;
+}
+__device__ __forceinline__ float half_of(uint32_t pair, int upper) {
+    return __half2float(__ushort_as_half((unsigned short)(upper ? pair >> 16 : pair)));
+}
+
+// ---- u[t] = A[id_t] x[t] -----------------------------------------------------------------------------------
+
+struct NarrowLayer {
+    const __half *x, *a;
+    float* u;
+    int n, rank, count;
+};
+struct NarrowParams {
+    NarrowLayer layer[kMaxGroup];
+    const int* ids;
+    int batch;
+};
+
+// A cluster takes a tile of 16 * MT rows and cuts the contraction into one part per warp of its CTAs; parts meet in shared memory, then over the cluster,
+// in a fixed order.  Products are m16n8k16 MMAs of fp16 operands, rows by ranks.  The order of a contraction is free, so a lane takes 8 consecutive columns of
+// each of its rows (one 16-byte load, no detour through shared memory) as the four operand words of two MMAs.
+// Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own.  gridDim.y clusters share
+// the adapters of a tile, so that a batch of single tokens with an adapter each does not read them one after the other.
+// The tensor core truncates when it accumulates: sums of 128 columns are added up in fp32 registers.
+// Bound: x from memory once, the factors from L2 once per tile.
+template <int MT, int NR>
+__global__ void __launch_bounds__(kThreads) narrow_kernel(const __grid_constant__ NarrowParams P) {
+    constexpr int kRows = 16 * MT, kRanks = 8 * NR;
+    constexpr int kStep = 2 * MT + NR <= 4 ? 4 : 2 * MT + NR <= 8 ? 2 : 1;      // units of 32 columns whose loads are in flight together
+    extern __shared__ __align__(16) float red[];                                // [kWarps][kRows][kRanks]
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
+    const NarrowLayer& L = P.layer[blockIdx.z];
+    const int row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, rank = L.rank;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    int id = lane < kRows && row0 + lane < P.batch ? P.ids[row0 + lane] : -1;
+    if (id >= L.count) id = -1;
+    const uint32_t named = __ballot_sync(0xFFFFFFFFu, id >= 0);
+    const int units = n / 32, worker = part * kWarps + warp, workers = parts * kWarps;
+    const int u0 = (int)((long long)units * worker / workers), u1 = (int)((long long)units * (worker + 1) / workers);
+    float sum[MT][NR][4] = {};
+    uint32_t mine = 0u;                                                         // rows whose adapter this cluster has taken
+    int turn = 0;
+    for (uint32_t left = named; left != 0u; ++turn) {
+        const int cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
+        const uint32_t match = __ballot_sync(0xFFFFFFFFu, id == cur);
+        left &= ~match;
+        if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
+        mine |= match;
+        const __half* a = L.a + (size_t)cur * rank * n + 8 * tq;
+        const __half* x = L.x + (size_t)row0 * n + 8 * tq;
+        for (int ub = u0; ub < u1; ub += 4) {
+            float acc[MT][NR][4] = {};
+#pragma unroll 1
+            for (int s0 = 0; s0 < 4; s0 += kStep) {
+                uint4 xv[kStep][2 * MT], av[kStep][NR];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float2 af = __half22float2(ah[q]), xf = __half22float2(xh[q]);
-                    sum = fmaf(af.x, xf.x, sum);
-                    sum = fmaf(af.y, xf.y, sum);
+                for (int s = 0; s < kStep; ++s) {
+                    const bool in = ub + s0 + s < u1;
+                    const size_t col = (size_t)(ub + s0 + s) * 32;
+#pragma unroll
+                    for (int m = 0; m < 2 * MT; ++m) xv[s][m] = in && row0 + 8 * m + gq < P.batch ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m + gq) * n + col) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int j = 0; j < NR; ++j) av[s][j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j + gq) * n + col) : make_uint4(0u, 0u, 0u, 0u);
+                }
+#pragma unroll
+                for (int s = 0; s < kStep; ++s)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int j = 0; j < NR; ++j) {
+                            const uint4 &lo = xv[s][2 * m], &hi = xv[s][2 * m + 1], &w = av[s][j];
+                            mma_f16(acc[m][j], lo.x, hi.x, lo.y, hi.y, w.x, w.y);
+                            mma_f16(acc[m][j], lo.z, hi.z, lo.w, hi.w, w.z, w.w);
+                        }
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const bool first = (match >> (16 * m + gq)) & 1u, second = (match >> (16 * m + 8 + gq)) & 1u;
+#pragma unroll
+                for (int j = 0; j < NR; ++j) {
+                    if (first) { sum[m][j][0] += acc[m][j][0]; sum[m][j][1] += acc[m][j][1]; }
+                    if (second) { sum[m][j][2] += acc[m][j][2]; sum[m][j][3] += acc[m][j][3]; }
                 }
             }
         }
+    }
+    const uint32_t bare = blockIdx.y == 0 ? ~named : 0u;                        // their u is zero: the first cluster's
+    if (mine == 0u && bare == 0u) return;                                       // (the whole cluster agrees)
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        if (lane == 0) u[(size_t)t * rank + j] = sum;
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            float* at = red + ((size_t)warp * kRows + 16 * m + gq) * kRanks + 8 * j + 2 * tq;
+            *reinterpret_cast<float2*>(at) = make_float2(sum[m][j][0], sum[m][j][1]);
+            *reinterpret_cast<float2*>(at + 8 * kRanks) = make_float2(sum[m][j][2], sum[m][j][3]);
+        }
+    __syncthreads();
+    for (int e = threadIdx.x; e < kRows * kRanks; e += kThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) s += red[w * kRows * kRanks + e];
+        red[e] = s;                                                             // (nobody else touches element e of any warp's part)
+    }
+    cluster.sync();
+    for (int e = part * kThreads + threadIdx.x; e < kRows * kRanks; e += parts * kThreads) {
+        const int row = e / kRanks, j = e % kRanks;
+        if (j >= rank || row0 + row >= P.batch || !(((mine | bare) >> row) & 1u)) continue;
+        float s = 0.f;
+        for (int q = 0; q < parts; ++q) s += cluster.map_shared_rank(red, q)[e];
+        L.u[(size_t)(row0 + row) * rank + j] = s;
+    }
+    cluster.sync();                                                             // (shared memory stays until all have read it)
+}
+
+// ---- y[t] += scale[id_t] * B[id_t]^T u[t] --------------------------------------------------------------------
+
+struct WidenLayer {
+    const __half* b;
+    const float *u, *scale;
+    __half* y;
+    int m, rank, count;
+};
+struct WidenParams {
+    WidenLayer layer[kMaxGroup];
+    const int* ids;
+    int batch, rows;                                                            // rows of a CTA at a time: 16, 32, 48 or 64
+};
+constexpr int kWidenRows = 64, kWidenCols = 32 * kWarps;
+
+// A CTA takes up to 64 rows and 256 columns, a warp 32 of them: rows by columns as m16n8k8 MMAs over the rank, the factor's fragments in registers for all
+// rows, u split into two tf32 parts (fp16 parts would need a common exponent per row, which a large entry beside small ones spoils).  The order of columns in
+// MMA tiles and of ranks is free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor entries come from
+// 16-byte loads, its u entries are four consecutive ones.  A row belongs to one adapter, so y is read and written once.
+// Bound: y, in and out.
+template <int R16, bool VEC>
+__global__ void __launch_bounds__(kThreads) widen_kernel(const __grid_constant__ WidenParams P) {
+    constexpr int kRanks = 16 * R16, kStride = kRanks + 4, kHeld = R16 <= 4 ? R16 : 4;   // 16-rank steps whose fragments are held
+    __shared__ __align__(16) float us[kWidenRows * kStride];
+    __shared__ int ids[kWidenRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
+    const WidenLayer& L = P.layer[blockIdx.z];
+    const int col0 = blockIdx.x * kWidenCols + warp * 32, m_all = L.m, rank = L.rank;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if ((int)blockIdx.x * kWidenCols >= m_all) return;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int row0 = blockIdx.y * P.rows; row0 < P.batch; row0 += gridDim.y * P.rows) {
+        __syncthreads();
+        if (threadIdx.x < kWidenRows) {
+            const int id = (int)threadIdx.x < P.rows && row0 + (int)threadIdx.x < P.batch ? P.ids[row0 + threadIdx.x] : -1;
+            ids[threadIdx.x] = id < L.count ? id : -1;
+        }
+        for (int i = threadIdx.x; i < P.rows * kRanks; i += kThreads) {
+            const int r = i / kRanks, j = i % kRanks;
+            us[r * kStride + j] = row0 + r < P.batch && j < rank ? L.u[(size_t)(row0 + r) * rank + j] : 0.f;
+        }
+        __syncthreads();
+        if (col0 >= m_all) continue;
+        const int id0 = ids[lane], id1 = ids[lane + 32];
+        unsigned long long left = __ballot_sync(0xFFFFFFFFu, id0 >= 0) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 >= 0) << 32);
+        while (left != 0ULL) {
+            const int cur = ids[__ffsll(left) - 1];
+            const unsigned long long match = __ballot_sync(0xFFFFFFFFu, id0 == cur) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 == cur) << 32);
+            left &= ~match;
+            const float scale = L.scale[cur];
+            const __half* b = L.b + (size_t)cur * rank * m_all;
+            float f[kHeld][4][4];                                               // [16 ranks][column tile][rank 4 tq + i]
+            auto load_factor = [&](int k0) {
+                const int c = col0 + 8 * (gq >> 1);
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = 16 * (k0 + k) + 4 * tq + i;
+                        const __half* src = b + (size_t)j * m_all + c;
+                        if (VEC) {
+                            const uint4 v = j < rank && c < m_all ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+                            f[k][0][i] = half_of(v.x, gq & 1); f[k][1][i] = half_of(v.y, gq & 1); f[k][2][i] = half_of(v.z, gq & 1); f[k][3][i] = half_of(v.w, gq & 1);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) f[k][q][i] = j < rank && c + 2 * q + (gq & 1) < m_all ? __half2float(src[2 * q + (gq & 1)]) : 0.f;
+                        }
+                    }
+            };
+            load_factor(0);
+            for (int mt = 0; mt < P.rows / 16; ++mt) {
+                if (((match >> (16 * mt)) & 0xFFFFULL) == 0ULL) continue;
+                const bool hit[2] = {((match >> (16 * mt + gq)) & 1ULL) != 0ULL, ((match >> (16 * mt + 8 + gq)) & 1ULL) != 0ULL};
+                const int c = col0 + 8 * tq;
+                __half* yr[2] = {L.y + (size_t)(row0 + 16 * mt + gq) * m_all + c, L.y + (size_t)(row0 + 16 * mt + 8 + gq) * m_all + c};
+                uint4 old[2];
+                if (VEC) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) old[h] = hit[h] && c < m_all ? *reinterpret_cast<const uint4*>(yr[h]) : make_uint4(0u, 0u, 0u, 0u);
+                }
+                float acc[4][4] = {};
+#pragma unroll
+                for (int k0 = 0; k0 < R16; k0 += kHeld) {
+                    if (R16 > kHeld) load_factor(k0);
+#pragma unroll
+                    for (int k = 0; k < kHeld; ++k) {
+                        const float4 ua = *reinterpret_cast<const float4*>(us + (16 * mt + gq) * kStride + 16 * (k0 + k) + 4 * tq);
+                        const float4 ub = *reinterpret_cast<const float4*>(us + (16 * mt + 8 + gq) * kStride + 16 * (k0 + k) + 4 * tq);
+                        uint32_t hi[2][4], lo[2][4];
+                        split_tf32(ua.x, hi[0][0], lo[0][0]); split_tf32(ub.x, hi[0][1], lo[0][1]); split_tf32(ua.y, hi[0][2], lo[0][2]); split_tf32(ub.y, hi[0][3], lo[0][3]);
+                        split_tf32(ua.z, hi[1][0], lo[1][0]); split_tf32(ub.z, hi[1][1], lo[1][1]); split_tf32(ua.w, hi[1][2], lo[1][2]); split_tf32(ub.w, hi[1][3], lo[1][3]);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            mma_tf32(acc[q], hi[0], f[k][q][0], f[k][q][1]);
+                            mma_tf32(acc[q], lo[0], f[k][q][0], f[k][q][1]);
+                            mma_tf32(acc[q], hi[1], f[k][q][2], f[k][q][3]);
+                            mma_tf32(acc[q], lo[1], f[k][q][2], f[k][q][3]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (!hit[h]) continue;
+                    if (VEC) {
+                        if (c >= m_all) continue;
+                        uint32_t v[4] = {old[h].x, old[h].y, old[h].z, old[h].w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], half_of(v[q], 0)), fmaf(scale, acc[q][2 * h + 1], half_of(v[q], 1)));
+                            v[q] = *reinterpret_cast<const uint32_t*>(&r);
+                        }
+                        *reinterpret_cast<uint4*>(yr[h]) = make_uint4(v[0], v[1], v[2], v[3]);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (c + 2 * q + e < m_all) yr[h][2 * q + e] = __float2half_rn(fmaf(scale, acc[q][2 * h + e], __half2float(yr[h][2 * q + e])));
+                    }
+                }
+            }
+        }
     }
 }
 
-// y[t][m] += scale[id] * sum_j B[id][j][m] u[t][j]: a thread per output.
-__global__ void __launch_bounds__(kThreads) widen_kernel(const float* __restrict__ u, const int* __restrict__ ids, const __half* __restrict__ b, const float* __restrict__ scale, __half* __restrict__ y, int count, int rank, int m_all) {
-    const int t = blockIdx.y, id = ids[t], m = blockIdx.x * kThreads + threadIdx.x;
-    if (id < 0 || id >= count || m >= m_all) return;
-    float sum = 0.f;
-    for (int j = 0; j < rank; ++j) sum = fmaf(__half2float(b[((size_t)id * rank + j) * m_all + m]), u[(size_t)t * rank + j], sum);
-    __half* at = y + (size_t)t * m_all + m;
-    *at = __float2half_rn(fmaf(scale[id], sum, __half2float(*at)));
+// ---- out[i][j][d] (+)= scale[i] * sum over the adapter's rows of low[t][j] v[t][d] -----------------------------
+
+struct FactorSide {
+    const __half* v;
+    const float* low;
+    float* out;
+    int side, blocks;                                                           // column blocks of this side
+};
+struct FactorParams {
+    FactorSide s[2];
+    const int* ids;
+    const float* scale;
+    int batch, rank, rank_groups, accumulate;
+};
+constexpr int kFactorRows = 64, kFactorList = 4096, kFactorChunk = 64;
+
+template <int RW>
+struct FactorSmem {                                                             // list of rows | low tile; the partial sums lie over both at the end
+    static constexpr int kStride(int ranks) { return ranks + 8; }               // (banks: 4 rows x 8 ranks of a fragment are 32 different ones)
+    static int bytes(int groups) {
+        const int ranks = 16 * RW * groups, work = kFactorList * 4 + kFactorRows * kStride(ranks) * 4, sums = ranks * 64 * (kWarps / groups) * 4;
+        return std::max(work, sums);
+    }
+};
+
+// Ranks by columns as m16n8k8 MMAs over the rows, low split into two tf32 parts (as in widen_kernel), v exact.  A warp takes 16 * RW ranks and 64 columns: a lane loads 8
+// consecutive columns of a row, one for each of 8 MMA tiles, straight to registers.  The rows of a cluster's adapter are dealt out to its CTAs in
+// chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor multiplied by zero (0 * NaN).
+// Sums of 64 rows are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
+// Bound: v from memory, tf32 MMAs from rank 32 on.
+template <int RW, bool VEC>
+__global__ void __launch_bounds__(kThreads) factor_kernel(const __grid_constant__ FactorParams P) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int counts[kWarps];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
+    const int groups = P.rank_groups, group = warp % groups, wc = warp / groups, ranks = 16 * RW * groups, stride = ranks + 8, block_cols = 64 * (kWarps / groups);
+    int block = (int)blockIdx.x / parts;
+    const FactorSide& S = P.s[block < P.s[0].blocks ? 0 : 1];
+    if (block >= P.s[0].blocks) block -= P.s[0].blocks;
+    const int adapter = blockIdx.y, side = S.side, col = block * block_cols + wc * 64 + 8 * gq, rank = P.rank;
+    int* list = reinterpret_cast<int*>(smem);
+    float* low = reinterpret_cast<float*>(smem) + kFactorList;
+    float sum[RW][8][4] = {};
+    for (long long base = 0; base < P.batch; base += (long long)kFactorList * parts) {
+        // the rows of this round that are the adapter's, in order
+        int n_list = 0;
+        for (int at = 0; at < kFactorList; at += kThreads) {
+            const int pos = at + (int)threadIdx.x;
+            const long long t = base + ((long long)(pos / kFactorChunk) * parts + part) * kFactorChunk + pos % kFactorChunk;
+            if (base + (long long)(at / kFactorChunk) * parts * kFactorChunk >= P.batch) break;
+            const bool hit = t < P.batch && P.ids[t] == adapter;
+            const uint32_t hits = __ballot_sync(0xFFFFFFFFu, hit);
+            if (lane == 0) counts[warp] = __popc(hits);
+            __syncthreads();
+            int before = n_list;
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) before += counts[w];
+                n_list += counts[w];
+            }
+            if (hit) list[before + __popc(hits & ((1u << lane) - 1u))] = (int)t;
+            __syncthreads();
+        }
+        for (int r0 = 0; r0 < n_list; r0 += kFactorRows) {
+            const int here = min(kFactorRows, n_list - r0);
+            for (int i = threadIdx.x; i < kFactorRows * ranks; i += kThreads) {
+                const int r = i / ranks, j = i % ranks;
+                low[r * stride + j] = r < here && j < rank ? S.low[(size_t)list[r0 + r] * rank + j] : 0.f;
+            }
+            __syncthreads();
+            float acc[RW][8][4] = {};
+#pragma unroll
+            for (int s0 = 0; s0 < kFactorRows / 8; s0 += 4) {
+                if (8 * s0 >= here) break;
+                uint4 v[4][2];
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int r = 8 * (s0 + s) + 4 * h + tq;
+                        v[s][h] = make_uint4(0u, 0u, 0u, 0u);
+                        if (r < here && col < side) {
+                            const __half* src = S.v + (size_t)list[r0 + r] * side + col;
+                            if (VEC) {
+                                v[s][h] = *reinterpret_cast<const uint4*>(src);
+                            } else {
+                                uint32_t w[4] = {};
+#pragma unroll
+                                for (int q = 0; q < 8; ++q)
+                                    if (col + q < side) w[q >> 1] |= (uint32_t)__half_as_ushort(src[q]) << (16 * (q & 1));
+                                v[s][h] = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                        }
+                    }
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    uint32_t hi[RW][4], lo[RW][4];
+#pragma unroll
+                    for (int m = 0; m < RW; ++m) {
+                        const float* at = low + (8 * (s0 + s) + tq) * stride + (group * RW + m) * 16 + gq;
+                        split_tf32(at[0], hi[m][0], lo[m][0]);
+                        split_tf32(at[8], hi[m][1], lo[m][1]);
+                        split_tf32(at[4 * stride], hi[m][2], lo[m][2]);
+                        split_tf32(at[4 * stride + 8], hi[m][3], lo[m][3]);
+                    }
+                    const uint32_t w[2][4] = {{v[s][0].x, v[s][0].y, v[s][0].z, v[s][0].w}, {v[s][1].x, v[s][1].y, v[s][1].z, v[s][1].w}};
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float b0 = half_of(w[0][q >> 1], q & 1), b1 = half_of(w[1][q >> 1], q & 1);
+#pragma unroll
+                        for (int m = 0; m < RW; ++m) {
+                            mma_tf32(acc[m][q], hi[m], b0, b1);
+                            mma_tf32(acc[m][q], lo[m], b0, b1);
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < RW; ++m)
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[m][q][e] += acc[m][q][e];
+            __syncthreads();
+        }
+    }
+    // the CTA's sums [rank][column of the block], then over the cluster.  Column of MMA column n of tile q: 8 n + q.
+    float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int m = 0; m < RW; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float* at = sums + ((group * RW + m) * 16 + gq + 8 * (e >> 1)) * block_cols + wc * 64 + 8 * (2 * tq + (e & 1));
+#pragma unroll
+            for (int q = 0; q < 8; q += 4) *reinterpret_cast<float4*>(at + q) = make_float4(sum[m][q][e], sum[m][q + 1][e], sum[m][q + 2][e], sum[m][q + 3][e]);
+        }
+    cluster.sync();
+    const float scale = P.scale[adapter];
+    const int first = block * block_cols, cols = min(block_cols, side - first);
+    for (int e = part * kThreads + threadIdx.x; e < rank * block_cols; e += parts * kThreads) {
+        const int j = e / block_cols, c = e % block_cols;
+        if (c >= cols) continue;
+        float total = 0.f;
+        for (int q = 0; q < parts; ++q) total += cluster.map_shared_rank(sums, q)[j * block_cols + c];
+        float* at = S.out + ((size_t)adapter * rank + j) * side + first + c;
+        *at = (P.accumulate ? *at : 0.f) + scale * total;
+    }
+    cluster.sync();
 }
 
-// out[i][j][d] (+)= scale[i] * sum over the adapter's rows of low[t][j] v[t][d]: a thread per element.
-__global__ void __launch_bounds__(kThreads) factor_kernel(const __half* __restrict__ v, const float* __restrict__ low, const int* __restrict__ ids, const float* __restrict__ scale, float* __restrict__ out, int batch, int rank, int side, int accumulate) {
-    const int d = blockIdx.x * kThreads + threadIdx.x, j = blockIdx.y, i = blockIdx.z;
-    if (d >= side) return;
-    float total = 0.f;
-    for (int t0 = 0; t0 < batch; t0 += 64) {                     // (partial sums of 64 rows: the rounding error of a long sum stays small)
-        float sum = 0.f;
-        for (int t = t0; t < min(batch, t0 + 64); ++t)
-            if (ids[t] == i) sum = fmaf(low[(size_t)t * rank + j], __half2float(v[(size_t)t * side + d]), sum);
-        total += sum;
+// ---- launches ----------------------------------------------------------------------------------------------
+
+template <typename Params>
+cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, bool dependent, const Params& P, cudaStream_t stream) {
+    if (smem > 48 * 1024) {                                                     // (an attribute of the function on the current device; setting it again is cheap)
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
     }
-    float* at = out + ((size_t)i * rank + j) * side + d;
-    *at = (accumulate ? *at : 0.f) + scale[i] * total;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    cfg.attrs = attr;
+    if (cluster > 0) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim = {(unsigned)cluster, 1, 1};
+        ++cfg.numAttrs;
+    }
+    if (dependent) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++cfg.numAttrs;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, P);
+}
+
+// Clusters of 8, 4, 2 or 1 CTAs for `tiles` clusters: as many CTAs as keep the SMs busy once.
+int cluster_for(long long tiles) {
+    int c = 8;
+    while (c > 1 && tiles * c > 400) c /= 2;
+    return c;
+}
+
+cudaError_t launch_narrow(const NarrowParams& P, int n_layers, int max_rank, cudaStream_t stream) {
+    const int mt = P.batch > 256 && max_rank <= 64 ? 2 : 1;
+    const long long tiles = (P.batch + 16 * mt - 1) / (16 * mt);
+    const int shares = P.batch <= 64 ? std::min(P.batch, 16) : P.batch <= 256 ? 4 : 2, c = cluster_for(tiles * n_layers);
+    const dim3 grid((unsigned)(tiles * c), (unsigned)shares, (unsigned)n_layers);
+    auto go = [&](auto kernel, int nr) { return launch(kernel, grid, c, kWarps * 16 * mt * 8 * nr * 4, true, P, stream); };
+    if (mt == 1) return max_rank <= 16 ? go(narrow_kernel<1, 2>, 2) : max_rank <= 32 ? go(narrow_kernel<1, 4>, 4) : max_rank <= 64 ? go(narrow_kernel<1, 8>, 8) : go(narrow_kernel<1, 16>, 16);
+    return max_rank <= 16 ? go(narrow_kernel<2, 2>, 2) : max_rank <= 32 ? go(narrow_kernel<2, 4>, 4) : go(narrow_kernel<2, 8>, 8);
+}
+
+cudaError_t launch_widen(WidenParams& P, int n_layers, int max_rank, int max_m, bool vec, cudaStream_t stream) {
+    const int cols = (max_m + kWidenCols - 1) / kWidenCols;
+    P.rows = kWidenRows;                                                        // fewer rows at a time while the CTAs do not fill the SMs
+    while (P.rows > 16 && (long long)cols * n_layers * ((P.batch + P.rows - 1) / P.rows) < 296) P.rows /= 2;
+    const dim3 grid((unsigned)cols, (unsigned)std::min((P.batch + P.rows - 1) / P.rows, 65535), (unsigned)n_layers);
+    auto go = [&](auto kernel) { return launch(kernel, grid, 0, 0, true, P, stream); };
+    if (vec) return max_rank <= 16 ? go(widen_kernel<1, true>) : max_rank <= 32 ? go(widen_kernel<2, true>) : max_rank <= 64 ? go(widen_kernel<4, true>) : go(widen_kernel<8, true>);
+    return max_rank <= 16 ? go(widen_kernel<1, false>) : max_rank <= 32 ? go(widen_kernel<2, false>) : max_rank <= 64 ? go(widen_kernel<4, false>) : go(widen_kernel<8, false>);
+}
+
+cudaError_t launch_factor(FactorParams& P, int count, cudaStream_t stream) {
+    const int rw = P.rank <= 16 ? 1 : 2;
+    P.rank_groups = P.rank <= 32 ? 1 : P.rank <= 64 ? 2 : 4;
+    const int block_cols = 64 * (kWarps / P.rank_groups);
+    for (FactorSide& s : P.s) s.blocks = (s.side + block_cols - 1) / block_cols;
+    const bool vec = P.s[0].side % 8 == 0 && P.s[1].side % 8 == 0;
+    const long long blocks = (long long)P.s[0].blocks + P.s[1].blocks;
+    int c = cluster_for(blocks * count);
+    while (c > 1 && (P.batch + kFactorChunk - 1) / kFactorChunk < c) c /= 2;    // (a CTA without rows would only take part in the sum)
+    const dim3 grid((unsigned)(blocks * c), (unsigned)count);
+    auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, c, bytes, false, P, stream); };
+    if (rw == 1) return vec ? go(factor_kernel<1, true>, FactorSmem<1>::bytes(P.rank_groups)) : go(factor_kernel<1, false>, FactorSmem<1>::bytes(P.rank_groups));
+    return vec ? go(factor_kernel<2, true>, FactorSmem<2>::bytes(P.rank_groups)) : go(factor_kernel<2, false>, FactorSmem<2>::bytes(P.rank_groups));
 }
 
 int check_pool(const char* who, const rabit_adapters* A) {
@@ -81,6 +512,20 @@ struct Range {
     size_t bytes;
     bool meets(const Range& o) const { return p && o.p && rabit_ranges_overlap(p, bytes, o.p, o.bytes); }
 };
+
+// What rabit_linear and rabit_linear_group check of these arguments, before the first kernel of an adapted call is enqueued.
+int check_layers(const char* who, const rabit_layer* const* layers, const void* const* xs, void* const* ys, int n_layers, int batch) {
+    for (int l = 0; l < n_layers; ++l) {
+        if ((((uintptr_t)xs[l]) & 15u) || (((uintptr_t)ys[l]) & 15u)) return rabit_fail(RABIT_INVALID_ARG, "%s: x and y must be 16-byte aligned (entry %d)", who, l);
+        if (layers[l]->device != layers[0]->device) return rabit_fail(RABIT_INVALID_ARG, "%s: entry %d lives on another device", who, l);
+        const Range r_y{ys[l], (size_t)batch * layers[l]->geom.M * 2};
+        for (int m = 0; m < n_layers; ++m) {
+            if (r_y.meets(Range{xs[m], (size_t)batch * layers[m]->geom.N * 2})) return rabit_fail(RABIT_INVALID_ARG, "%s: output %d overlaps input %d", who, l, m);
+            if (m > l && r_y.meets(Range{ys[m], (size_t)batch * layers[m]->geom.M * 2})) return rabit_fail(RABIT_INVALID_ARG, "%s: outputs %d and %d overlap", who, l, m);
+        }
+    }
+    return RABIT_OK;
+}
 
 int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_adapters* const* adapters, const void* const* xs, const int* ids,
                  void* const* ys, float* const* us, int n_layers, int batch, void* stream) {
@@ -117,19 +562,58 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
                 if (layers[m] && ((ys[m] && f.meets(Range{ys[m], (size_t)batch * layers[m]->geom.M * 2})) || (adapters[m] && us[m] && f.meets(Range{us[m], (size_t)batch * adapters[m]->rank * 4}))))
                     return rabit_fail(RABIT_INVALID_ARG, "%s: y or u of entry %d overlaps the adapters of entry %d", who, m, l);
     }
+    cudaStream_t st = (cudaStream_t)stream;
+    int dev = -1;
+    RABIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != layers[0]->device) return rabit_fail(RABIT_INVALID_ARG, "%s: the layers live on device %d but device %d is current", who, layers[0]->device, dev);
+
+    // u of all adapted layers, the layers themselves, then the adapters' part on top of their outputs: the kernels of the first step run while those of
+    // the second fetch their weights.  What the layers' calls refuse, they refuse before anything of this call has run.
+    int at[kMaxGroup], n = 0;
+    auto each_group = [&](auto&& body) {
+        cudaError_t e = cudaSuccess;
+        n = 0;
+        for (int l = 0; l < n_layers && e == cudaSuccess; ++l) {
+            if (adapters[l]) at[n++] = l;
+            if (n == kMaxGroup || (l == n_layers - 1 && n > 0)) {
+                e = body();
+                n = 0;
+            }
+        }
+        return e;
+    };
+    if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
+    cudaError_t e = each_group([&] {
+        NarrowParams P{};
+        P.ids = ids;
+        P.batch = batch;
+        int max_rank = 0;
+        for (int i = 0; i < n; ++i) {
+            const rabit_adapters* A = adapters[at[i]];
+            P.layer[i] = NarrowLayer{(const __half*)xs[at[i]], (const __half*)A->a, us[at[i]], A->n_in, A->rank, A->count};
+            max_rank = std::max(max_rank, A->rank);
+        }
+        return launch_narrow(P, n, max_rank, st);
+    });
+    if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     int rc = n_layers == 1 ? rabit_linear(layers[0], xs[0], ys[0], batch, stream) : rabit_linear_group(layers, xs, ys, n_layers, batch, stream);
     if (rc != RABIT_OK) return rc;
-    cudaStream_t st = (cudaStream_t)stream;
-    for (int l = 0; l < n_layers; ++l) {
-        const rabit_adapters* A = adapters[l];
-        if (!A) continue;
-        narrow_kernel<<<batch, kThreads, 0, st>>>((const __half*)xs[l], ids, (const __half*)A->a, us[l], A->count, A->rank, A->n_in);
-        for (int t0 = 0; t0 < batch; t0 += 32768)
-            widen_kernel<<<dim3((A->n_out + kThreads - 1) / kThreads, std::min(batch - t0, 32768)), kThreads, 0, st>>>(us[l] + (size_t)t0 * A->rank, ids + t0, (const __half*)A->b, A->scale,
-                                                                                                            (__half*)ys[l] + (size_t)t0 * A->n_out, A->count, A->rank, A->n_out);
-        cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
-    }
+    e = each_group([&] {
+        WidenParams P{};
+        P.ids = ids;
+        P.batch = batch;
+        int max_rank = 0, max_m = 0;
+        bool vec = true;
+        for (int i = 0; i < n; ++i) {
+            const rabit_adapters* A = adapters[at[i]];
+            P.layer[i] = WidenLayer{(const __half*)A->b, us[at[i]], A->scale, (__half*)ys[at[i]], A->n_out, A->rank, A->count};
+            max_rank = std::max(max_rank, A->rank);
+            max_m = std::max(max_m, A->n_out);
+            vec = vec && A->n_out % 8 == 0;
+        }
+        return launch_widen(P, n, max_rank, max_m, vec, st);
+    });
+    if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return RABIT_OK;
 }
 
@@ -152,9 +636,15 @@ int gradients_call(const rabit_adapters* A, const void* x, const float* u, const
             if (o.meets(i)) return rabit_fail(RABIT_INVALID_ARG, "%s: a gradient overlaps an input", who);
     if (A->count > 65535) return rabit_fail(RABIT_UNSUPPORTED_SHAPE, "%s: at most 65535 adapters (got %d)", who, A->count);
     cudaStream_t st = (cudaStream_t)stream;
-    factor_kernel<<<dim3((A->n_in + kThreads - 1) / kThreads, A->rank, A->count), kThreads, 0, st>>>((const __half*)x, p, ids, A->scale, da, batch, A->rank, A->n_in, accumulate);
-    factor_kernel<<<dim3((A->n_out + kThreads - 1) / kThreads, A->rank, A->count), kThreads, 0, st>>>((const __half*)dy, u, ids, A->scale, db, batch, A->rank, A->n_out, accumulate);
-    cudaError_t e = cudaGetLastError();
+    FactorParams P{};
+    P.s[0] = FactorSide{(const __half*)x, p, da, A->n_in, 0};
+    P.s[1] = FactorSide{(const __half*)dy, u, db, A->n_out, 0};
+    P.ids = ids;
+    P.scale = A->scale;
+    P.batch = batch;
+    P.rank = A->rank;
+    P.accumulate = accumulate;
+    cudaError_t e = launch_factor(P, A->count, st);
     if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return RABIT_OK;
 }
