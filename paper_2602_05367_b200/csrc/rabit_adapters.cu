@@ -53,15 +53,22 @@ struct NarrowParams {
 
 // A cluster takes a tile of 16 * MT rows and cuts the contraction into one part per warp of its CTAs; parts meet in shared memory, then over the cluster,
 // in a fixed order.  Products are m16n8k16 MMAs of fp16 operands, rows by ranks.  The order of a contraction is free, so a lane takes 8 consecutive columns of
-// each of its rows (one 16-byte load, no detour through shared memory) as the four operand words of two MMAs.
+// each of its rows (one 16-byte load, no detour through shared memory) as the four operand words of two MMAs; the loads of the next columns are in
+// flight beside the MMAs.
 // Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own.  gridDim.y clusters share
 // the adapters of a tile, so that a batch of single tokens with an adapter each does not read them one after the other.
-// The tensor core truncates when it accumulates: sums of 128 columns are added up in fp32 registers.
+// The tensor core truncates when it accumulates: after at most 16 MMAs the sums go to fp32 words in shared memory.
 // Bound: x from memory once, the factors from L2 once per tile.
 template <int MT, int NR>
-__global__ void __launch_bounds__(kThreads) narrow_kernel(const __grid_constant__ NarrowParams P) {
-    constexpr int kRows = 16 * MT, kRanks = 8 * NR;
-    constexpr int kStep = 2 * MT + NR <= 4 ? 4 : 2 * MT + NR <= 8 ? 2 : 1;      // units of 32 columns whose loads are in flight together
+struct Narrow {
+    static constexpr int kRows = 16 * MT, kRanks = 8 * NR, kLoads = 2 * MT + NR;
+    static constexpr int kStep = kLoads <= 4 ? 2 : 1;                           // units of 32 columns per set of loads; two sets
+    static constexpr int kChain = 4 / kStep;                                    // pairs of sets between two flushes: 16 MMAs
+};
+template <int MT, int NR>
+__global__ void __launch_bounds__(kThreads, (Narrow<MT, NR>::kLoads <= 8 ? 2 : 1)) narrow_kernel(const __grid_constant__ NarrowParams P) {
+    using C = Narrow<MT, NR>;
+    constexpr int kRows = C::kRows, kRanks = C::kRanks, kStep = C::kStep;
     extern __shared__ __align__(16) float red[];                                // [kWarps][kRows][kRanks]
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -69,6 +76,11 @@ __global__ void __launch_bounds__(kThreads) narrow_kernel(const __grid_constant_
     const NarrowLayer& L = P.layer[blockIdx.z];
     const int row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, rank = L.rank;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;           // the lane's sums: rows 8 m + gq, ranks 8 j + 2 tq and the next
+#pragma unroll
+    for (int m = 0; m < 2 * MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NR; ++j) *reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j) = make_float2(0.f, 0.f);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     int id = lane < kRows && row0 + lane < P.batch ? P.ids[row0 + lane] : -1;
@@ -76,7 +88,6 @@ __global__ void __launch_bounds__(kThreads) narrow_kernel(const __grid_constant_
     const uint32_t named = __ballot_sync(0xFFFFFFFFu, id >= 0);
     const int units = n / 32, worker = part * kWarps + warp, workers = parts * kWarps;
     const int u0 = (int)((long long)units * worker / workers), u1 = (int)((long long)units * (worker + 1) / workers);
-    float sum[MT][NR][4] = {};
     uint32_t mine = 0u;                                                         // rows whose adapter this cluster has taken
     int turn = 0;
     for (uint32_t left = named; left != 0u; ++turn) {
@@ -85,54 +96,66 @@ __global__ void __launch_bounds__(kThreads) narrow_kernel(const __grid_constant_
         left &= ~match;
         if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
         mine |= match;
-        const __half* a = L.a + (size_t)cur * rank * n + 8 * tq;
-        const __half* x = L.x + (size_t)row0 * n + 8 * tq;
-        for (int ub = u0; ub < u1; ub += 4) {
-            float acc[MT][NR][4] = {};
-#pragma unroll 1
-            for (int s0 = 0; s0 < 4; s0 += kStep) {
-                uint4 xv[kStep][2 * MT], av[kStep][NR];
+        const __half* a = L.a + ((size_t)cur * rank + gq) * n + 8 * tq;
+        const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
+        float acc[MT][NR][4] = {};
+        struct Loads {
+            uint4 x[kStep][2 * MT], a[kStep][NR];
+        };
+        auto load = [&](Loads& l, int u) {
 #pragma unroll
-                for (int s = 0; s < kStep; ++s) {
-                    const bool in = ub + s0 + s < u1;
-                    const size_t col = (size_t)(ub + s0 + s) * 32;
+            for (int s = 0; s < kStep; ++s) {
+                const bool in = u + s < u1;
+                const size_t col = (size_t)(u + s) * 32;
 #pragma unroll
-                    for (int m = 0; m < 2 * MT; ++m) xv[s][m] = in && row0 + 8 * m + gq < P.batch ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m + gq) * n + col) : make_uint4(0u, 0u, 0u, 0u);
+                for (int m = 0; m < 2 * MT; ++m) l.x[s][m] = in && row0 + 8 * m + gq < P.batch ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m) * n + col) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                    for (int j = 0; j < NR; ++j) av[s][j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j + gq) * n + col) : make_uint4(0u, 0u, 0u, 0u);
-                }
-#pragma unroll
-                for (int s = 0; s < kStep; ++s)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-#pragma unroll
-                        for (int j = 0; j < NR; ++j) {
-                            const uint4 &lo = xv[s][2 * m], &hi = xv[s][2 * m + 1], &w = av[s][j];
-                            mma_f16(acc[m][j], lo.x, hi.x, lo.y, hi.y, w.x, w.y);
-                            mma_f16(acc[m][j], lo.z, hi.z, lo.w, hi.w, w.z, w.w);
-                        }
+                for (int j = 0; j < NR; ++j) l.a[s][j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
             }
+        };
+        auto multiply = [&](const Loads& l) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const bool first = (match >> (16 * m + gq)) & 1u, second = (match >> (16 * m + 8 + gq)) & 1u;
+            for (int s = 0; s < kStep; ++s)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int j = 0; j < NR; ++j) {
+                        const uint4 &lo = l.x[s][2 * m], &hi = l.x[s][2 * m + 1], &w = l.a[s][j];
+                        mma_f16(acc[m][j], lo.x, hi.x, lo.y, hi.y, w.x, w.y);
+                        mma_f16(acc[m][j], lo.z, hi.z, lo.w, hi.w, w.z, w.w);
+                    }
+        };
+        auto flush = [&]() {
+#pragma unroll
+            for (int m = 0; m < 2 * MT; ++m) {
+                const bool keep = (match >> (8 * m + gq)) & 1u;
 #pragma unroll
                 for (int j = 0; j < NR; ++j) {
-                    if (first) { sum[m][j][0] += acc[m][j][0]; sum[m][j][1] += acc[m][j][1]; }
-                    if (second) { sum[m][j][2] += acc[m][j][2]; sum[m][j][3] += acc[m][j][3]; }
+                    float2* at = reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j);
+                    float* v = acc[m >> 1][j] + 2 * (m & 1);
+                    if (keep) {
+                        const float2 old = *at;
+                        *at = make_float2(old.x + v[0], old.y + v[1]);
+                    }
+                    v[0] = v[1] = 0.f;
                 }
             }
+        };
+        Loads even, odd;
+        load(even, u0);
+        int pairs = 0;
+#pragma unroll 1
+        for (int u = u0; u < u1; u += 2 * kStep) {
+            load(odd, u + kStep);
+            multiply(even);
+            load(even, u + 2 * kStep);
+            multiply(odd);
+            if (++pairs % C::kChain == 0) flush();
         }
+        if (pairs % C::kChain != 0) flush();
     }
     const uint32_t bare = blockIdx.y == 0 ? ~named : 0u;                        // their u is zero: the first cluster's
     if (mine == 0u && bare == 0u) return;                                       // (the whole cluster agrees)
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int j = 0; j < NR; ++j) {
-            float* at = red + ((size_t)warp * kRows + 16 * m + gq) * kRanks + 8 * j + 2 * tq;
-            *reinterpret_cast<float2*>(at) = make_float2(sum[m][j][0], sum[m][j][1]);
-            *reinterpret_cast<float2*>(at + 8 * kRanks) = make_float2(sum[m][j][2], sum[m][j][3]);
-        }
     __syncthreads();
     for (int e = threadIdx.x; e < kRows * kRanks; e += kThreads) {
         float s = 0.f;
@@ -151,6 +174,35 @@ __global__ void __launch_bounds__(kThreads) narrow_kernel(const __grid_constant_
     cluster.sync();                                                             // (shared memory stays until all have read it)
 }
 
+// ---- asynchronous copies to shared memory --------------------------------------------------------------------
+
+__device__ __forceinline__ void copy_async_16(void* dst, const void* src, bool valid) {   // (not valid: zeros)
+    const uint32_t size = valid ? 16u : 0u;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(size) : "memory");
+}
+__device__ __forceinline__ void copy_async_4(void* dst, const void* src, bool valid) {
+    const uint32_t size = valid ? 4u : 0u;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(size) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// 8 halves at src, of which those before `n` are inside; VEC: src is 16-byte aligned and all or none are
+template <bool VEC>
+__device__ __forceinline__ uint4 load_8(const __half* src, int n) {
+    if constexpr (VEC) {
+        return n > 0 ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+    } else {
+        uint32_t w[4] = {};
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < n) w[q >> 1] |= (uint32_t)__half_as_ushort(src[q]) << (16 * (q & 1));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
 // ---- y[t] += scale[id_t] * B[id_t]^T u[t] --------------------------------------------------------------------
 
 struct WidenLayer {
@@ -162,117 +214,159 @@ struct WidenLayer {
 struct WidenParams {
     WidenLayer layer[kMaxGroup];
     const int* ids;
-    int batch, rows;                                                            // rows of a CTA at a time: 16, 32, 48 or 64
+    int batch, rows, shares;                                                    // rows of a CTA: 16, 32 or 64; CTAs that share the adapters of the rows
 };
 constexpr int kWidenRows = 64, kWidenCols = 32 * kWarps;
 
 // A CTA takes up to 64 rows and 256 columns, a warp 32 of them: rows by columns as m16n8k8 MMAs over the rank, the factor's fragments in registers for all
 // rows, u split into two tf32 parts (fp16 parts would need a common exponent per row, which a large entry beside small ones spoils).  The order of columns in
 // MMA tiles and of ranks is free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor entries come from
-// 16-byte loads, its u entries are four consecutive ones.  A row belongs to one adapter, so y is read and written once.
+// 16-byte loads, its u entries are four consecutive ones.  A row belongs to one adapter, so y is read and written once; it is read ahead of the MMAs.
 // Bound: y, in and out.
 template <int R16, bool VEC>
-__global__ void __launch_bounds__(kThreads) widen_kernel(const __grid_constant__ WidenParams P) {
-    constexpr int kRanks = 16 * R16, kStride = kRanks + 4, kHeld = R16 <= 4 ? R16 : 4;   // 16-rank steps whose fragments are held
+__global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const __grid_constant__ WidenParams P) {
+    constexpr int kRanks = 16 * R16, kStride = kRanks + 4, kTiles = kWidenRows / 16;
     __shared__ __align__(16) float us[kWidenRows * kStride];
-    __shared__ int ids[kWidenRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
     const WidenLayer& L = P.layer[blockIdx.z];
     const int col0 = blockIdx.x * kWidenCols + warp * 32, m_all = L.m, rank = L.rank;
+    const int share = (int)blockIdx.y % P.shares, row0 = (int)blockIdx.y / P.shares * P.rows;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if ((int)blockIdx.x * kWidenCols >= m_all) return;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int row0 = blockIdx.y * P.rows; row0 < P.batch; row0 += gridDim.y * P.rows) {
-        __syncthreads();
-        if (threadIdx.x < kWidenRows) {
-            const int id = (int)threadIdx.x < P.rows && row0 + (int)threadIdx.x < P.batch ? P.ids[row0 + threadIdx.x] : -1;
-            ids[threadIdx.x] = id < L.count ? id : -1;
-        }
-        for (int i = threadIdx.x; i < P.rows * kRanks; i += kThreads) {
-            const int r = i / kRanks, j = i % kRanks;
-            us[r * kStride + j] = row0 + r < P.batch && j < rank ? L.u[(size_t)(row0 + r) * rank + j] : 0.f;
-        }
-        __syncthreads();
-        if (col0 >= m_all) continue;
-        const int id0 = ids[lane], id1 = ids[lane + 32];
-        unsigned long long left = __ballot_sync(0xFFFFFFFFu, id0 >= 0) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 >= 0) << 32);
-        while (left != 0ULL) {
-            const int cur = ids[__ffsll(left) - 1];
-            const unsigned long long match = __ballot_sync(0xFFFFFFFFu, id0 == cur) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 == cur) << 32);
+
+    int id0 = lane < P.rows && row0 + lane < P.batch ? P.ids[row0 + lane] : -1, id1 = lane + 32 < P.rows && row0 + lane + 32 < P.batch ? P.ids[row0 + lane + 32] : -1;
+    if (id0 >= L.count) id0 = -1;
+    if (id1 >= L.count) id1 = -1;
+    auto rows_of = [&](int cur) { return __ballot_sync(0xFFFFFFFFu, id0 == cur) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 == cur) << 32); };
+    auto first_of = [&](unsigned long long left) {
+        const int at = __ffsll(left) - 1;
+        return at < 32 ? __shfl_sync(0xFFFFFFFFu, id0, at) : __shfl_sync(0xFFFFFFFFu, id1, at - 32);
+    };
+    const unsigned long long named = __ballot_sync(0xFFFFFFFFu, id0 >= 0) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 >= 0) << 32);
+    unsigned long long mine = named;                                            // rows whose adapters are this CTA's
+    if (P.shares > 1) {
+        mine = 0ULL;
+        int turn = 0;
+        for (unsigned long long left = named; left != 0ULL; ++turn) {
+            const unsigned long long match = rows_of(first_of(left));
             left &= ~match;
-            const float scale = L.scale[cur];
-            const __half* b = L.b + (size_t)cur * rank * m_all;
-            float f[kHeld][4][4];                                               // [16 ranks][column tile][rank 4 tq + i]
-            auto load_factor = [&](int k0) {
-                const int c = col0 + 8 * (gq >> 1);
+            if (turn % P.shares == share) mine |= match;
+        }
+    }
+    if (mine == 0ULL) return;                                                   // (every warp sees the same)
+    const bool fours = rank % 4 == 0;
+    for (int i = threadIdx.x; i < P.rows * (kRanks / 4); i += kThreads) {
+        const int r = i / (kRanks / 4), j = i % (kRanks / 4) * 4;
+        const float* src = L.u + (size_t)(row0 + r) * rank + j;
+        const bool in = (mine >> r) & 1ULL;
+        float* dst = us + r * kStride + j;
+        if (fours) {
+            copy_async_16(dst, in && j < rank ? src : L.u, in && j < rank);
+        } else {
 #pragma unroll
-                for (int k = 0; k < kHeld; ++k)
+            for (int q = 0; q < 4; ++q) copy_async_4(dst + q, in && j + q < rank ? src + q : L.u, in && j + q < rank);
+        }
+    }
+    copy_async_commit();
+
+    const int c = col0 + 8 * tq;                                                // the lane's columns in y
+    uint4 old[kTiles][2];
+    auto load_y = [&](int mt) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = 16 * (k0 + k) + 4 * tq + i;
-                        const __half* src = b + (size_t)j * m_all + c;
-                        if (VEC) {
-                            const uint4 v = j < rank && c < m_all ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
-                            f[k][0][i] = half_of(v.x, gq & 1); f[k][1][i] = half_of(v.y, gq & 1); f[k][2][i] = half_of(v.z, gq & 1); f[k][3][i] = half_of(v.w, gq & 1);
-                        } else {
+        for (int h = 0; h < 2; ++h) {
+            const int r = 16 * mt + 8 * h + gq;
+            old[R16 <= 2 ? mt : 0][h] = load_8<VEC>(L.y + (size_t)(row0 + r) * m_all + c, (mine >> r) & 1ULL ? m_all - c : 0);
+        }
+    };
+    if (R16 <= 2) {
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) f[k][q][i] = j < rank && c + 2 * q + (gq & 1) < m_all ? __half2float(src[2 * q + (gq & 1)]) : 0.f;
-                        }
-                    }
-            };
-            load_factor(0);
-            for (int mt = 0; mt < P.rows / 16; ++mt) {
-                if (((match >> (16 * mt)) & 0xFFFFULL) == 0ULL) continue;
-                const bool hit[2] = {((match >> (16 * mt + gq)) & 1ULL) != 0ULL, ((match >> (16 * mt + 8 + gq)) & 1ULL) != 0ULL};
-                const int c = col0 + 8 * tq;
-                __half* yr[2] = {L.y + (size_t)(row0 + 16 * mt + gq) * m_all + c, L.y + (size_t)(row0 + 16 * mt + 8 + gq) * m_all + c};
-                uint4 old[2];
-                if (VEC) {
+        for (int mt = 0; mt < kTiles; ++mt) load_y(mt);
+    }
+    uint32_t f[R16][4][2];                                                      // [16 ranks][column tile]: ranks 4 tq and 4 tq + 1, the two behind them
+    auto load_factor = [&](int cur) {
+        const int cf = col0 + 8 * (gq >> 1);
+        const uint32_t pick = gq & 1 ? 0x7632u : 0x5410u;
+        const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + cf;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) old[h] = hit[h] && c < m_all ? *reinterpret_cast<const uint4*>(yr[h]) : make_uint4(0u, 0u, 0u, 0u);
-                }
-                float acc[4][4] = {};
+        for (int k = 0; k < R16; ++k) {
+            uint4 v[4];
 #pragma unroll
-                for (int k0 = 0; k0 < R16; k0 += kHeld) {
-                    if (R16 > kHeld) load_factor(k0);
+            for (int i = 0; i < 4; ++i) v[i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all, 16 * k + 4 * tq + i < rank ? m_all - cf : 0);
 #pragma unroll
-                    for (int k = 0; k < kHeld; ++k) {
-                        const float4 ua = *reinterpret_cast<const float4*>(us + (16 * mt + gq) * kStride + 16 * (k0 + k) + 4 * tq);
-                        const float4 ub = *reinterpret_cast<const float4*>(us + (16 * mt + 8 + gq) * kStride + 16 * (k0 + k) + 4 * tq);
-                        uint32_t hi[2][4], lo[2][4];
-                        split_tf32(ua.x, hi[0][0], lo[0][0]); split_tf32(ub.x, hi[0][1], lo[0][1]); split_tf32(ua.y, hi[0][2], lo[0][2]); split_tf32(ub.y, hi[0][3], lo[0][3]);
-                        split_tf32(ua.z, hi[1][0], lo[1][0]); split_tf32(ub.z, hi[1][1], lo[1][1]); split_tf32(ua.w, hi[1][2], lo[1][2]); split_tf32(ub.w, hi[1][3], lo[1][3]);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            mma_tf32(acc[q], hi[0], f[k][q][0], f[k][q][1]);
-                            mma_tf32(acc[q], lo[0], f[k][q][0], f[k][q][1]);
-                            mma_tf32(acc[q], hi[1], f[k][q][2], f[k][q][3]);
-                            mma_tf32(acc[q], lo[1], f[k][q][2], f[k][q][3]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (!hit[h]) continue;
-                    if (VEC) {
-                        if (c >= m_all) continue;
-                        uint32_t v[4] = {old[h].x, old[h].y, old[h].z, old[h].w};
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], half_of(v[q], 0)), fmaf(scale, acc[q][2 * h + 1], half_of(v[q], 1)));
-                            v[q] = *reinterpret_cast<const uint32_t*>(&r);
-                        }
-                        *reinterpret_cast<uint4*>(yr[h]) = make_uint4(v[0], v[1], v[2], v[3]);
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                if (c + 2 * q + e < m_all) yr[h][2 * q + e] = __float2half_rn(fmaf(scale, acc[q][2 * h + e], __half2float(yr[h][2 * q + e])));
-                    }
-                }
+            for (int p = 0; p < 2; ++p) {
+                f[k][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
+                f[k][1][p] = __byte_perm(v[2 * p].y, v[2 * p + 1].y, pick);
+                f[k][2][p] = __byte_perm(v[2 * p].z, v[2 * p + 1].z, pick);
+                f[k][3][p] = __byte_perm(v[2 * p].w, v[2 * p + 1].w, pick);
             }
         }
+    };
+    int cur = first_of(mine);
+    load_factor(cur);
+    copy_async_wait<0>();
+    __syncthreads();
+    for (unsigned long long left = mine;;) {
+        const unsigned long long match = rows_of(cur);
+        left &= ~match;
+        const float scale = L.scale[cur];
+        auto tile = [&](int mt) {
+            const uint32_t hits = (uint32_t)(match >> (16 * mt)) & 0xFFFFu;
+            if (hits == 0u) return;
+            if (R16 > 2) load_y(mt);
+            float acc[4][4] = {};
+#pragma unroll
+            for (int k = 0; k < R16; ++k) {
+                const float4 ua = *reinterpret_cast<const float4*>(us + (16 * mt + gq) * kStride + 16 * k + 4 * tq);
+                const float4 ub = *reinterpret_cast<const float4*>(us + (16 * mt + 8 + gq) * kStride + 16 * k + 4 * tq);
+                uint32_t hi[2][4], lo[2][4];
+                split_tf32(ua.x, hi[0][0], lo[0][0]); split_tf32(ub.x, hi[0][1], lo[0][1]); split_tf32(ua.y, hi[0][2], lo[0][2]); split_tf32(ub.y, hi[0][3], lo[0][3]);
+                split_tf32(ua.z, hi[1][0], lo[1][0]); split_tf32(ub.z, hi[1][1], lo[1][1]); split_tf32(ua.w, hi[1][2], lo[1][2]); split_tf32(ub.w, hi[1][3], lo[1][3]);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    float w[4][2];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        w[q][0] = half_of(f[k][q][p], 0);
+                        w[q][1] = half_of(f[k][q][p], 1);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q], hi[p], w[q][0], w[q][1]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q], lo[p], w[q][0], w[q][1]);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!((hits >> (8 * h + gq)) & 1u) || c >= m_all) continue;
+                const uint4 was = old[R16 <= 2 ? mt : 0][h];
+                uint32_t v[4] = {was.x, was.y, was.z, was.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], half_of(v[q], 0)), fmaf(scale, acc[q][2 * h + 1], half_of(v[q], 1)));
+                    v[q] = *reinterpret_cast<const uint32_t*>(&r);
+                }
+                __half* yr = L.y + (size_t)(row0 + 16 * mt + 8 * h + gq) * m_all + c;
+                if (VEC) {
+                    *reinterpret_cast<uint4*>(yr) = make_uint4(v[0], v[1], v[2], v[3]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (c + q < m_all) yr[q] = __ushort_as_half((unsigned short)(v[q >> 1] >> (16 * (q & 1))));
+                }
+            }
+        };
+        if (R16 <= 2) {
+#pragma unroll
+            for (int mt = 0; mt < kTiles; ++mt) tile(mt);
+        } else {
+#pragma unroll 1
+            for (int mt = 0; mt < kTiles; ++mt) tile(mt);
+        }
+        // (the rows left to this CTA, taken adapter by adapter)
+        if (left == 0ULL) break;
+        cur = first_of(left);
+        load_factor(cur);
     }
 }
 
@@ -288,39 +382,41 @@ struct FactorParams {
     FactorSide s[2];
     const int* ids;
     const float* scale;
-    int batch, rank, rank_groups, accumulate;
+    int batch, rank, accumulate;
 };
-constexpr int kFactorRows = 64, kFactorList = 4096, kFactorChunk = 64;
+constexpr int kFactorRows = 32, kFactorStages = 3, kFactorList = 1024, kFactorChunk = 64;
 
-template <int RW>
-struct FactorSmem {                                                             // list of rows | low tile; the partial sums lie over both at the end
-    static constexpr int kStride(int ranks) { return ranks + 8; }               // (banks: 4 rows x 8 ranks of a fragment are 32 different ones)
-    static int bytes(int groups) {
-        const int ranks = 16 * RW * groups, work = kFactorList * 4 + kFactorRows * kStride(ranks) * 4, sums = ranks * 64 * (kWarps / groups) * 4;
-        return std::max(work, sums);
-    }
+template <int GROUPS>
+struct Factor {                                                                 // a stage: rows of v, rows of low; behind the stages the list of rows; sums over all of it at the end
+    static constexpr int kRanks = 16 * GROUPS, kCols = 64 * (kWarps / GROUPS);
+    static constexpr int kVStride = kCols * 2 + 32, kLowStride = kRanks + 8;    // bytes, words: no two of the rows that a fragment load touches meet in a bank
+    static constexpr int kVBytes = kFactorRows * kVStride, kStageBytes = kVBytes + kFactorRows * kLowStride * 4;
+    static constexpr int kBytes = kFactorStages * kStageBytes + kFactorList * 4;
+    static_assert(kRanks * kCols * 4 <= kBytes && 2 * (kBytes + 1024 + 128) <= 228 * 1024, "the sums fit, two CTAs per SM");
 };
 
-// Ranks by columns as m16n8k8 MMAs over the rows, low split into two tf32 parts (as in widen_kernel), v exact.  A warp takes 16 * RW ranks and 64 columns: a lane loads 8
-// consecutive columns of a row, one for each of 8 MMA tiles, straight to registers.  The rows of a cluster's adapter are dealt out to its CTAs in
-// chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor multiplied by zero (0 * NaN).
-// Sums of 64 rows are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
+// Ranks by columns as m16n8k8 MMAs over the rows, low split into two tf32 parts (as in widen_kernel), v exact.  A warp takes 16 ranks and 64 columns, GROUPS warps
+// the same columns: of a row a lane reads 8 consecutive columns, one for each of 8 MMA tiles.  The rows of a cluster's adapter are dealt out to its CTAs in
+// chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor multiplied by zero (0 * NaN), then streams
+// them through a ring of three stages of 32 rows.
+// Sums of 32 rows are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
 // Bound: v from memory, tf32 MMAs from rank 32 on.
-template <int RW, bool VEC>
-__global__ void __launch_bounds__(kThreads) factor_kernel(const __grid_constant__ FactorParams P) {
+template <int GROUPS, bool VEC>
+__global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_constant__ FactorParams P) {
+    using F = Factor<GROUPS>;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int counts[kWarps];
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
-    const int groups = P.rank_groups, group = warp % groups, wc = warp / groups, ranks = 16 * RW * groups, stride = ranks + 8, block_cols = 64 * (kWarps / groups);
+    const int group = warp % GROUPS, wc = warp / GROUPS;
     int block = (int)blockIdx.x / parts;
     const FactorSide& S = P.s[block < P.s[0].blocks ? 0 : 1];
     if (block >= P.s[0].blocks) block -= P.s[0].blocks;
-    const int adapter = blockIdx.y, side = S.side, col = block * block_cols + wc * 64 + 8 * gq, rank = P.rank;
-    int* list = reinterpret_cast<int*>(smem);
-    float* low = reinterpret_cast<float*>(smem) + kFactorList;
-    float sum[RW][8][4] = {};
+    const int adapter = blockIdx.y, side = S.side, first = block * F::kCols, rank = P.rank;
+    const bool fours = rank % 4 == 0;
+    int* list = reinterpret_cast<int*>(smem + kFactorStages * F::kStageBytes);
+    float sum[8][4] = {};
     for (long long base = 0; base < P.batch; base += (long long)kFactorList * parts) {
         // the rows of this round that are the adapter's, in order
         int n_list = 0;
@@ -340,87 +436,95 @@ __global__ void __launch_bounds__(kThreads) factor_kernel(const __grid_constant_
             if (hit) list[before + __popc(hits & ((1u << lane) - 1u))] = (int)t;
             __syncthreads();
         }
-        for (int r0 = 0; r0 < n_list; r0 += kFactorRows) {
-            const int here = min(kFactorRows, n_list - r0);
-            for (int i = threadIdx.x; i < kFactorRows * ranks; i += kThreads) {
-                const int r = i / ranks, j = i % ranks;
-                low[r * stride + j] = r < here && j < rank ? S.low[(size_t)list[r0 + r] * rank + j] : 0.f;
-            }
-            __syncthreads();
-            float acc[RW][8][4] = {};
+        const int n_tiles = (n_list + kFactorRows - 1) / kFactorRows;
+        auto fetch = [&](int tile) {
+            unsigned char* stage = smem + tile % kFactorStages * F::kStageBytes;
+            if (tile < n_tiles) {
+                constexpr int kPieces = F::kCols / 8;                           // 16 bytes of a row each
 #pragma unroll
-            for (int s0 = 0; s0 < kFactorRows / 8; s0 += 4) {
-                if (8 * s0 >= here) break;
-                uint4 v[4][2];
+                for (int i0 = 0; i0 < kFactorRows * kPieces; i0 += kThreads) {
+                    const int i = i0 + (int)threadIdx.x, r = i / kPieces, col = first + i % kPieces * 8, at = tile * kFactorRows + r;
+                    const bool in = at < n_list && col < side;
+                    const __half* src = in ? S.v + (size_t)list[at] * side + col : S.v;
+                    unsigned char* dst = stage + r * F::kVStride + i % kPieces * 16;
+                    if (VEC) copy_async_16(dst, src, in);
+                    else *reinterpret_cast<uint4*>(dst) = load_8<false>(src, in ? side - col : 0);
+                }
+                float* low = reinterpret_cast<float*>(stage + F::kVBytes);
+                constexpr int kFours = F::kRanks / 4;
+                for (int i = threadIdx.x; i < kFactorRows * kFours; i += kThreads) {
+                    const int r = i / kFours, j = i % kFours * 4, at = tile * kFactorRows + r;
+                    const bool in = at < n_list;
+                    const float* src = in ? S.low + (size_t)list[at] * rank + j : S.low;
+                    float* dst = low + r * F::kLowStride + j;
+                    if (fours) {
+                        copy_async_16(dst, in && j < rank ? src : S.low, in && j < rank);
+                    } else {
 #pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int r = 8 * (s0 + s) + 4 * h + tq;
-                        v[s][h] = make_uint4(0u, 0u, 0u, 0u);
-                        if (r < here && col < side) {
-                            const __half* src = S.v + (size_t)list[r0 + r] * side + col;
-                            if (VEC) {
-                                v[s][h] = *reinterpret_cast<const uint4*>(src);
-                            } else {
-                                uint32_t w[4] = {};
-#pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    if (col + q < side) w[q >> 1] |= (uint32_t)__half_as_ushort(src[q]) << (16 * (q & 1));
-                                v[s][h] = make_uint4(w[0], w[1], w[2], w[3]);
-                            }
-                        }
-                    }
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    uint32_t hi[RW][4], lo[RW][4];
-#pragma unroll
-                    for (int m = 0; m < RW; ++m) {
-                        const float* at = low + (8 * (s0 + s) + tq) * stride + (group * RW + m) * 16 + gq;
-                        split_tf32(at[0], hi[m][0], lo[m][0]);
-                        split_tf32(at[8], hi[m][1], lo[m][1]);
-                        split_tf32(at[4 * stride], hi[m][2], lo[m][2]);
-                        split_tf32(at[4 * stride + 8], hi[m][3], lo[m][3]);
-                    }
-                    const uint32_t w[2][4] = {{v[s][0].x, v[s][0].y, v[s][0].z, v[s][0].w}, {v[s][1].x, v[s][1].y, v[s][1].z, v[s][1].w}};
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const float b0 = half_of(w[0][q >> 1], q & 1), b1 = half_of(w[1][q >> 1], q & 1);
-#pragma unroll
-                        for (int m = 0; m < RW; ++m) {
-                            mma_tf32(acc[m][q], hi[m], b0, b1);
-                            mma_tf32(acc[m][q], lo[m], b0, b1);
-                        }
+                        for (int q = 0; q < 4; ++q) copy_async_4(dst + q, in && j + q < rank ? src + q : S.low, in && j + q < rank);
                     }
                 }
             }
+            copy_async_commit();
+        };
+        fetch(0);
+        fetch(1);
+        for (int tile = 0; tile < n_tiles; ++tile) {
+            copy_async_wait<1>();
+            __syncthreads();                                                    // everybody's copies of this tile are there, and the slot of the one before is free
+            fetch(tile + 2);
+            const unsigned char* stage = smem + tile % kFactorStages * F::kStageBytes;
+            const float* low = reinterpret_cast<const float*>(stage + F::kVBytes) + tq * F::kLowStride + group * 16 + gq;
+            const unsigned char* v = stage + tq * F::kVStride + (wc * 64 + 8 * gq) * 2;
+            float acc[8][4] = {};
 #pragma unroll
-            for (int m = 0; m < RW; ++m)
+            for (int s = 0; s < kFactorRows / 8; ++s) {
+                uint32_t hi[4], lo[4];
+                const float* at = low + 8 * s * F::kLowStride;
+                split_tf32(at[0], hi[0], lo[0]);
+                split_tf32(at[8], hi[1], lo[1]);
+                split_tf32(at[4 * F::kLowStride], hi[2], lo[2]);
+                split_tf32(at[4 * F::kLowStride + 8], hi[3], lo[3]);
+                const uint4 v0 = *reinterpret_cast<const uint4*>(v + 8 * s * F::kVStride), v1 = *reinterpret_cast<const uint4*>(v + (8 * s + 4) * F::kVStride);
+                const uint32_t w[2][4] = {{v0.x, v0.y, v0.z, v0.w}, {v1.x, v1.y, v1.z, v1.w}};
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
+                for (int q0 = 0; q0 < 8; q0 += 4) {
+                    float b[4][2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[m][q][e] += acc[m][q][e];
-            __syncthreads();
+                    for (int q = 0; q < 4; ++q) {
+                        b[q][0] = half_of(w[0][(q0 + q) >> 1], q & 1);
+                        b[q][1] = half_of(w[1][(q0 + q) >> 1], q & 1);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q0 + q], hi, b[q][0], b[q][1]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q0 + q], lo, b[q][0], b[q][1]);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[q][e] += acc[q][e];
         }
+        copy_async_wait<0>();
+        __syncthreads();                                                        // (the list is written again)
     }
     // the CTA's sums [rank][column of the block], then over the cluster.  Column of MMA column n of tile q: 8 n + q.
     float* sums = reinterpret_cast<float*>(smem);
 #pragma unroll
-    for (int m = 0; m < RW; ++m)
+    for (int e = 0; e < 4; ++e) {
+        float* at = sums + (group * 16 + gq + 8 * (e >> 1)) * F::kCols + wc * 64 + 8 * (2 * tq + (e & 1));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float* at = sums + ((group * RW + m) * 16 + gq + 8 * (e >> 1)) * block_cols + wc * 64 + 8 * (2 * tq + (e & 1));
-#pragma unroll
-            for (int q = 0; q < 8; q += 4) *reinterpret_cast<float4*>(at + q) = make_float4(sum[m][q][e], sum[m][q + 1][e], sum[m][q + 2][e], sum[m][q + 3][e]);
-        }
+        for (int q = 0; q < 8; q += 4) *reinterpret_cast<float4*>(at + q) = make_float4(sum[q][e], sum[q + 1][e], sum[q + 2][e], sum[q + 3][e]);
+    }
     cluster.sync();
     const float scale = P.scale[adapter];
-    const int first = block * block_cols, cols = min(block_cols, side - first);
-    for (int e = part * kThreads + threadIdx.x; e < rank * block_cols; e += parts * kThreads) {
-        const int j = e / block_cols, c = e % block_cols;
+    const int cols = min(F::kCols, side - first);
+    for (int e = part * kThreads + threadIdx.x; e < rank * F::kCols; e += parts * kThreads) {
+        const int j = e / F::kCols, c = e % F::kCols;
         if (c >= cols) continue;
         float total = 0.f;
-        for (int q = 0; q < parts; ++q) total += cluster.map_shared_rank(sums, q)[j * block_cols + c];
+        for (int q = 0; q < parts; ++q) total += cluster.map_shared_rank(sums, q)[e];
         float* at = S.out + ((size_t)adapter * rank + j) * side + first + c;
         *at = (P.accumulate ? *at : 0.f) + scale * total;
     }
@@ -462,39 +566,52 @@ int cluster_for(long long tiles) {
     return c;
 }
 
+// CTAs or clusters that share the adapters of a tile of rows: all that can differ while the batch is small, few for prompts.
+int shares_for(int batch) { return batch <= 64 ? std::min(batch, 16) : batch <= 256 ? 4 : 2; }
+
 cudaError_t launch_narrow(const NarrowParams& P, int n_layers, int max_rank, cudaStream_t stream) {
     const int mt = P.batch > 256 && max_rank <= 64 ? 2 : 1;
     const long long tiles = (P.batch + 16 * mt - 1) / (16 * mt);
-    const int shares = P.batch <= 64 ? std::min(P.batch, 16) : P.batch <= 256 ? 4 : 2, c = cluster_for(tiles * n_layers);
-    const dim3 grid((unsigned)(tiles * c), (unsigned)shares, (unsigned)n_layers);
+    const int c = cluster_for(tiles * n_layers);
+    const dim3 grid((unsigned)(tiles * c), (unsigned)shares_for(P.batch), (unsigned)n_layers);
     auto go = [&](auto kernel, int nr) { return launch(kernel, grid, c, kWarps * 16 * mt * 8 * nr * 4, true, P, stream); };
     if (mt == 1) return max_rank <= 16 ? go(narrow_kernel<1, 2>, 2) : max_rank <= 32 ? go(narrow_kernel<1, 4>, 4) : max_rank <= 64 ? go(narrow_kernel<1, 8>, 8) : go(narrow_kernel<1, 16>, 16);
     return max_rank <= 16 ? go(narrow_kernel<2, 2>, 2) : max_rank <= 32 ? go(narrow_kernel<2, 4>, 4) : go(narrow_kernel<2, 8>, 8);
 }
 
-cudaError_t launch_widen(WidenParams& P, int n_layers, int max_rank, int max_m, bool vec, cudaStream_t stream) {
-    const int cols = (max_m + kWidenCols - 1) / kWidenCols;
-    P.rows = kWidenRows;                                                        // fewer rows at a time while the CTAs do not fill the SMs
-    while (P.rows > 16 && (long long)cols * n_layers * ((P.batch + P.rows - 1) / P.rows) < 296) P.rows /= 2;
-    const dim3 grid((unsigned)cols, (unsigned)std::min((P.batch + P.rows - 1) / P.rows, 65535), (unsigned)n_layers);
-    auto go = [&](auto kernel) { return launch(kernel, grid, 0, 0, true, P, stream); };
-    if (vec) return max_rank <= 16 ? go(widen_kernel<1, true>) : max_rank <= 32 ? go(widen_kernel<2, true>) : max_rank <= 64 ? go(widen_kernel<4, true>) : go(widen_kernel<8, true>);
-    return max_rank <= 16 ? go(widen_kernel<1, false>) : max_rank <= 32 ? go(widen_kernel<2, false>) : max_rank <= 64 ? go(widen_kernel<4, false>) : go(widen_kernel<8, false>);
+// At most 65535 blocks along y: 32768 rows at a time.
+constexpr int kWidenBatch = 32768;
+cudaError_t launch_widen(WidenParams P, int n_layers, int max_rank, int max_m, bool vec, cudaStream_t stream) {
+    const int cols = (max_m + kWidenCols - 1) / kWidenCols, batch = P.batch;
+    cudaError_t e = cudaSuccess;
+    for (int t0 = 0; t0 < batch && e == cudaSuccess; t0 += kWidenBatch) {
+        P.batch = std::min(batch - t0, kWidenBatch);
+        P.rows = kWidenRows;                                                    // fewer rows at a time while the CTAs do not fill the SMs
+        while (P.rows > 16 && (long long)cols * n_layers * ((P.batch + P.rows - 1) / P.rows) < 296) P.rows /= 2;
+        P.shares = batch <= 64 ? shares_for(batch) : 1;
+        const dim3 grid((unsigned)cols, (unsigned)((P.batch + P.rows - 1) / P.rows * P.shares), (unsigned)n_layers);
+        auto go = [&](auto kernel) { return launch(kernel, grid, 0, 0, true, P, stream); };
+        if (vec) e = max_rank <= 16 ? go(widen_kernel<1, true>) : max_rank <= 32 ? go(widen_kernel<2, true>) : max_rank <= 64 ? go(widen_kernel<4, true>) : go(widen_kernel<8, true>);
+        else e = max_rank <= 16 ? go(widen_kernel<1, false>) : max_rank <= 32 ? go(widen_kernel<2, false>) : max_rank <= 64 ? go(widen_kernel<4, false>) : go(widen_kernel<8, false>);
+        P.ids += P.batch;
+        for (int l = 0; l < n_layers; ++l) {
+            P.layer[l].u += (size_t)P.batch * P.layer[l].rank;
+            P.layer[l].y += (size_t)P.batch * P.layer[l].m;
+        }
+    }
+    return e;
 }
 
+template <int GROUPS>
 cudaError_t launch_factor(FactorParams& P, int count, cudaStream_t stream) {
-    const int rw = P.rank <= 16 ? 1 : 2;
-    P.rank_groups = P.rank <= 32 ? 1 : P.rank <= 64 ? 2 : 4;
-    const int block_cols = 64 * (kWarps / P.rank_groups);
-    for (FactorSide& s : P.s) s.blocks = (s.side + block_cols - 1) / block_cols;
+    using F = Factor<GROUPS>;
+    for (FactorSide& s : P.s) s.blocks = (s.side + F::kCols - 1) / F::kCols;
     const bool vec = P.s[0].side % 8 == 0 && P.s[1].side % 8 == 0;
     const long long blocks = (long long)P.s[0].blocks + P.s[1].blocks;
     int c = cluster_for(blocks * count);
     while (c > 1 && (P.batch + kFactorChunk - 1) / kFactorChunk < c) c /= 2;    // (a CTA without rows would only take part in the sum)
     const dim3 grid((unsigned)(blocks * c), (unsigned)count);
-    auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, c, bytes, false, P, stream); };
-    if (rw == 1) return vec ? go(factor_kernel<1, true>, FactorSmem<1>::bytes(P.rank_groups)) : go(factor_kernel<1, false>, FactorSmem<1>::bytes(P.rank_groups));
-    return vec ? go(factor_kernel<2, true>, FactorSmem<2>::bytes(P.rank_groups)) : go(factor_kernel<2, false>, FactorSmem<2>::bytes(P.rank_groups));
+    return vec ? launch(factor_kernel<GROUPS, true>, grid, c, F::kBytes, false, P, stream) : launch(factor_kernel<GROUPS, false>, grid, c, F::kBytes, false, P, stream);
 }
 
 int check_pool(const char* who, const rabit_adapters* A) {
@@ -644,7 +761,8 @@ int gradients_call(const rabit_adapters* A, const void* x, const float* u, const
     P.batch = batch;
     P.rank = A->rank;
     P.accumulate = accumulate;
-    cudaError_t e = launch_factor(P, A->count, st);
+    cudaError_t e = A->rank <= 16 ? launch_factor<1>(P, A->count, st) : A->rank <= 32 ? launch_factor<2>(P, A->count, st)
+                  : A->rank <= 64 ? launch_factor<4>(P, A->count, st) : launch_factor<8>(P, A->count, st);
     if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return RABIT_OK;
 }

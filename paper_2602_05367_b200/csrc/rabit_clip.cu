@@ -15,14 +15,44 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr size_t kChunk = 8192;                       // elements that a CTA takes at a time
-constexpr int kMaxGrid = 1024;
+constexpr size_t kChunk = 4096;                       // elements that a CTA takes at a time
+constexpr int kMaxGrid = 2048;
 
 struct Chunk {                                        // a piece of one tensor
     const float* src;
     float* dst;
-    unsigned long long n;
+    uint32_t n, aligned;                              // aligned: both pointers on 16 bytes
 };
+constexpr int kFours = (int)(kChunk / 4 / kThreads);  // 16-byte accesses of a thread to a chunk
+static_assert((size_t)kFours * 4 * kThreads == kChunk, "a chunk is whole accesses of all threads");
+
+// a thread's share of a chunk, 4 * kFours elements, zero behind its end; `store` puts them back
+__device__ __forceinline__ void load_chunk(const Chunk& c, float (&v)[4 * kFours]) {
+#pragma unroll
+    for (int i = 0; i < kFours; ++i) {
+        const uint32_t at = 4u * (i * kThreads + threadIdx.x);
+        if (c.aligned && at + 4 <= c.n) {
+            const float4 w = *reinterpret_cast<const float4*>(c.src + at);
+            v[4 * i] = w.x; v[4 * i + 1] = w.y; v[4 * i + 2] = w.z; v[4 * i + 3] = w.w;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[4 * i + q] = at + q < c.n ? c.src[at + q] : 0.f;
+        }
+    }
+}
+__device__ __forceinline__ void store_chunk(const Chunk& c, const float (&v)[4 * kFours]) {
+#pragma unroll
+    for (int i = 0; i < kFours; ++i) {
+        const uint32_t at = 4u * (i * kThreads + threadIdx.x);
+        if (c.aligned && at + 4 <= c.n) {
+            *reinterpret_cast<float4*>(c.dst + at) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (at + q < c.n) c.dst[at + q] = v[4 * i + q];
+        }
+    }
+}
 
 __device__ __forceinline__ double block_sum(double v, double* warps) {
 #pragma unroll
@@ -38,12 +68,15 @@ __device__ __forceinline__ double block_sum(double v, double* warps) {
 __global__ void __launch_bounds__(kThreads) squares_kernel(const Chunk* __restrict__ chunks, int n_chunks, double* __restrict__ partial) {
     __shared__ double warps[kThreads / 32];
     double sum = 0.0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    Chunk next = (int)blockIdx.x < n_chunks ? chunks[blockIdx.x] : Chunk{};
     for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-        const Chunk ch = chunks[c];
-        for (unsigned i = threadIdx.x; i < ch.n; i += kThreads) {
-            const double v = ch.src[i];
-            sum = fma(v, v, sum);
-        }
+        const Chunk ch = next;
+        if (c + (int)gridDim.x < n_chunks) next = chunks[c + gridDim.x];
+        float v[4 * kFours];
+        load_chunk(ch, v);
+#pragma unroll
+        for (int i = 0; i < 4 * kFours; ++i) sum = fma((double)v[i], (double)v[i], sum);
     }
     sum = block_sum(sum, warps);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
@@ -51,6 +84,7 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Chunk* __restri
 
 __global__ void __launch_bounds__(kThreads) scale_kernel(const Chunk* __restrict__ chunks, int n_chunks, const double* __restrict__ partial, double max_norm, float* __restrict__ norm_out) {
     __shared__ double warps[kThreads / 32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     double sum = 0.0;
     for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) sum += partial[i];
     const double norm = sqrt(block_sum(sum, warps));
@@ -58,10 +92,17 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Chunk* __restrict
     if (f > 1.0) f = 1.0;                             // (a NaN stays)
     const float factor = (float)f;
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    // from the last chunk to the first: what was read last is still in L2
+    Chunk next = (int)blockIdx.x < n_chunks ? chunks[n_chunks - 1 - blockIdx.x] : Chunk{};
     for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-        const Chunk ch = chunks[c];
+        const Chunk ch = next;
+        if (c + (int)gridDim.x < n_chunks) next = chunks[n_chunks - 1 - c - gridDim.x];
         if (ch.dst == ch.src && factor == 1.f) continue;
-        for (unsigned i = threadIdx.x; i < ch.n; i += kThreads) ch.dst[i] = ch.src[i] * factor;
+        float v[4 * kFours];
+        load_chunk(ch, v);
+#pragma unroll
+        for (int i = 0; i < 4 * kFours; ++i) v[i] *= factor;
+        store_chunk(ch, v);
     }
 }
 
@@ -128,15 +169,18 @@ static int bind_call(const float* const* tensors, float* const* outs, const size
     std::vector<Chunk> table;
     table.reserve(n_chunks);
     for (int i = 0; i < n; ++i)
-        for (size_t at = 0; at < counts[i]; at += kChunk)
-            table.push_back(Chunk{tensors[i] + at, outs ? outs[i] + at : const_cast<float*>(tensors[i]) + at, (unsigned long long)std::min(kChunk, counts[i] - at)});
+        for (size_t at = 0; at < counts[i]; at += kChunk) {
+            const float* src = tensors[i] + at;
+            float* dst = outs ? outs[i] + at : const_cast<float*>(src);
+            table.push_back(Chunk{src, dst, (uint32_t)std::min(kChunk, counts[i] - at), (uint32_t)(((uintptr_t)src | (uintptr_t)dst) % 16 == 0)});
+        }
     if (!table.empty()) RABIT_CUDA_TRY(cudaMemcpyAsync(dev_buf, table.data(), table.size() * sizeof(Chunk), cudaMemcpyHostToDevice, (cudaStream_t)stream));
     int sms = 0;
     RABIT_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, attr.device));
     rabit_gradients* R = new rabit_gradients;
     R->device = attr.device;
     R->n_chunks = (int)n_chunks;
-    R->grid = (int)std::max<size_t>(1, std::min<size_t>(n_chunks, std::min(4 * sms, kMaxGrid)));
+    R->grid = (int)std::max<size_t>(1, std::min<size_t>(n_chunks, std::min(8 * sms, kMaxGrid)));
     R->chunks = (const Chunk*)dev_buf;
     R->partial = (double*)((char*)dev_buf + table_bytes);
     *out = R;
@@ -157,8 +201,17 @@ extern "C" int rabit_clip_gradients(const rabit_gradients* R, float max_norm, fl
     if (dev != R->device) return rabit_fail(RABIT_INVALID_ARG, "%s: the gradients live on device %d but device %d is current", who, R->device, dev);
     cudaStream_t st = (cudaStream_t)stream;
     squares_kernel<<<R->grid, kThreads, 0, st>>>(R->chunks, R->n_chunks, R->partial);
-    scale_kernel<<<R->grid, kThreads, 0, st>>>(R->chunks, R->n_chunks, R->partial, (double)max_norm, norm_out);
     cudaError_t e = cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)R->grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, scale_kernel, R->chunks, R->n_chunks, (const double*)R->partial, (double)max_norm, norm_out);
     if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return RABIT_OK;
 }
