@@ -38,6 +38,32 @@ __device__ __forceinline__ float half_of(uint32_t pair, int upper) {
     return __half2float(__ushort_as_half((unsigned short)(upper ? pair >> 16 : pair)));
 }
 
+constexpr int kMaxCluster = 8;
+// Elements 4 e .. 4 e + 3 of `values` (the same place in every CTA of the cluster), added up in the order of the CTAs.  The loads go out together: one after
+// the other they were most of the time of the kernels below.
+__device__ __forceinline__ float4 cluster_sum(const cg::cluster_group& cluster, float* values, int parts, int e) {
+    float4 v[kMaxCluster];
+#pragma unroll
+    for (int q = 0; q < kMaxCluster; ++q) v[q] = q < parts ? reinterpret_cast<const float4*>(cluster.map_shared_rank(values, q))[e] : make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 s = v[0];
+#pragma unroll
+    for (int q = 1; q < kMaxCluster; ++q) {
+        s.x += v[q].x; s.y += v[q].y; s.z += v[q].z; s.w += v[q].w;
+    }
+    return s;
+}
+// Four neighbours of a row of u (or of a gradient) to memory, of which those before `n` exist
+__device__ __forceinline__ void store_4(float* at, const float4& v, int n, bool fours) {
+    if (fours) {
+        *reinterpret_cast<float4*>(at) = v;
+    } else {
+        if (n > 0) at[0] = v.x;
+        if (n > 1) at[1] = v.y;
+        if (n > 2) at[2] = v.z;
+        if (n > 3) at[3] = v.w;
+    }
+}
+
 // ---- u[t] = A[id_t] x[t] -----------------------------------------------------------------------------------
 
 struct NarrowLayer {
@@ -51,24 +77,18 @@ struct NarrowParams {
     int batch;
 };
 
-// A cluster takes a tile of 16 * MT rows and cuts the contraction into one part per warp of its CTAs; parts meet in shared memory, then over the cluster,
-// in a fixed order.  Products are m16n8k16 MMAs of fp16 operands, rows by ranks.  The order of a contraction is free, so a lane takes 8 consecutive columns of
-// each of its rows (one 16-byte load, no detour through shared memory) as the four operand words of two MMAs; the loads of the next columns are in
-// flight beside the MMAs.
+// Up to 256 rows.  A cluster takes a tile of 16 rows and cuts the contraction into one part per warp of its CTAs; parts meet in shared memory, then over the
+// cluster, in a fixed order.  Products are m16n8k16 MMAs of fp16 operands, rows by ranks.  The order of a contraction is free, so a lane takes 8 consecutive
+// columns of each of its rows (one 16-byte load, no detour through shared memory) as the four operand words of two MMAs; the loads of the next columns
+// are in flight beside the MMAs.
 // Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own.  gridDim.y clusters share
 // the adapters of a tile, so that a batch of single tokens with an adapter each does not read them one after the other.
 // The tensor core truncates when it accumulates: after at most 16 MMAs the sums go to fp32 words in shared memory.
-// Bound: x from memory once, the factors from L2 once per tile.
-template <int MT, int NR>
-struct Narrow {
-    static constexpr int kRows = 16 * MT, kRanks = 8 * NR, kLoads = 2 * MT + NR;
-    static constexpr int kStep = kLoads <= 4 ? 2 : 1;                           // units of 32 columns per set of loads; two sets
-    static constexpr int kChain = 4 / kStep;                                    // pairs of sets between two flushes: 16 MMAs
-};
-template <int MT, int NR>
-__global__ void __launch_bounds__(kThreads, (Narrow<MT, NR>::kLoads <= 8 ? 2 : 1)) narrow_kernel(const __grid_constant__ NarrowParams P) {
-    using C = Narrow<MT, NR>;
-    constexpr int kRows = C::kRows, kRanks = C::kRanks, kStep = C::kStep;
+// Bound: latencies (launch, ids, x and factor, the sum over the cluster).
+constexpr int kNarrowRows = 16;
+template <int NR>
+__global__ void __launch_bounds__(kThreads, NR <= 2 ? 3 : NR <= 4 ? 2 : 1) narrow_kernel(const __grid_constant__ NarrowParams P) {
+    constexpr int kRows = kNarrowRows, kRanks = 8 * NR;
     extern __shared__ __align__(16) float red[];                                // [kWarps][kRows][kRanks]
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -76,9 +96,9 @@ __global__ void __launch_bounds__(kThreads, (Narrow<MT, NR>::kLoads <= 8 ? 2 : 1
     const NarrowLayer& L = P.layer[blockIdx.z];
     const int row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, rank = L.rank;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;           // the lane's sums: rows 8 m + gq, ranks 8 j + 2 tq and the next
+    float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;           // the lane's sums: rows gq and gq + 8, ranks 8 j + 2 tq and the next
 #pragma unroll
-    for (int m = 0; m < 2 * MT; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int j = 0; j < NR; ++j) *reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j) = make_float2(0.f, 0.f);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -98,61 +118,51 @@ __global__ void __launch_bounds__(kThreads, (Narrow<MT, NR>::kLoads <= 8 ? 2 : 1
         mine |= match;
         const __half* a = L.a + ((size_t)cur * rank + gq) * n + 8 * tq;
         const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
-        float acc[MT][NR][4] = {};
+        const bool has[2] = {(match >> gq & 1u) != 0u, (match >> (8 + gq) & 1u) != 0u};   // (other rows' x is not needed)
+        float acc[NR][4] = {};
         struct Loads {
-            uint4 x[kStep][2 * MT], a[kStep][NR];
+            uint4 x[2], a[NR];
         };
         auto load = [&](Loads& l, int u) {
+            const bool in = u < u1;
+            const size_t col = (size_t)u * 32;
 #pragma unroll
-            for (int s = 0; s < kStep; ++s) {
-                const bool in = u + s < u1;
-                const size_t col = (size_t)(u + s) * 32;
+            for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m) * n + col) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                for (int m = 0; m < 2 * MT; ++m) l.x[s][m] = in && row0 + 8 * m + gq < P.batch ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m) * n + col) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-                for (int j = 0; j < NR; ++j) l.a[s][j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
-            }
+            for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
         };
         auto multiply = [&](const Loads& l) {
 #pragma unroll
-            for (int s = 0; s < kStep; ++s)
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int j = 0; j < NR; ++j) {
-                        const uint4 &lo = l.x[s][2 * m], &hi = l.x[s][2 * m + 1], &w = l.a[s][j];
-                        mma_f16(acc[m][j], lo.x, hi.x, lo.y, hi.y, w.x, w.y);
-                        mma_f16(acc[m][j], lo.z, hi.z, lo.w, hi.w, w.z, w.w);
-                    }
+            for (int j = 0; j < NR; ++j) {
+                mma_f16(acc[j], l.x[0].x, l.x[1].x, l.x[0].y, l.x[1].y, l.a[j].x, l.a[j].y);
+                mma_f16(acc[j], l.x[0].z, l.x[1].z, l.x[0].w, l.x[1].w, l.a[j].z, l.a[j].w);
+            }
         };
         auto flush = [&]() {
 #pragma unroll
-            for (int m = 0; m < 2 * MT; ++m) {
-                const bool keep = (match >> (8 * m + gq)) & 1u;
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int j = 0; j < NR; ++j) {
                     float2* at = reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j);
-                    float* v = acc[m >> 1][j] + 2 * (m & 1);
-                    if (keep) {
+                    if (has[m]) {
                         const float2 old = *at;
-                        *at = make_float2(old.x + v[0], old.y + v[1]);
+                        *at = make_float2(old.x + acc[j][2 * m], old.y + acc[j][2 * m + 1]);
                     }
-                    v[0] = v[1] = 0.f;
+                    acc[j][2 * m] = acc[j][2 * m + 1] = 0.f;
                 }
-            }
         };
         Loads even, odd;
         load(even, u0);
         int pairs = 0;
 #pragma unroll 1
-        for (int u = u0; u < u1; u += 2 * kStep) {
-            load(odd, u + kStep);
+        for (int u = u0; u < u1; u += 2) {
+            load(odd, u + 1);
             multiply(even);
-            load(even, u + 2 * kStep);
+            load(even, u + 2);
             multiply(odd);
-            if (++pairs % C::kChain == 0) flush();
+            if (++pairs % 4 == 0) flush();
         }
-        if (pairs % C::kChain != 0) flush();
+        if (pairs % 4 != 0) flush();
     }
     const uint32_t bare = blockIdx.y == 0 ? ~named : 0u;                        // their u is zero: the first cluster's
     if (mine == 0u && bare == 0u) return;                                       // (the whole cluster agrees)
@@ -164,12 +174,10 @@ __global__ void __launch_bounds__(kThreads, (Narrow<MT, NR>::kLoads <= 8 ? 2 : 1
         red[e] = s;                                                             // (nobody else touches element e of any warp's part)
     }
     cluster.sync();
-    for (int e = part * kThreads + threadIdx.x; e < kRows * kRanks; e += parts * kThreads) {
-        const int row = e / kRanks, j = e % kRanks;
+    for (int e = part * kThreads + threadIdx.x; e < kRows * kRanks / 4; e += parts * kThreads) {
+        const int row = e / (kRanks / 4), j = e % (kRanks / 4) * 4;
         if (j >= rank || row0 + row >= P.batch || !(((mine | bare) >> row) & 1u)) continue;
-        float s = 0.f;
-        for (int q = 0; q < parts; ++q) s += cluster.map_shared_rank(red, q)[e];
-        L.u[(size_t)(row0 + row) * rank + j] = s;
+        store_4(L.u + (size_t)(row0 + row) * rank + j, cluster_sum(cluster, red, parts, e), rank - j, rank % 4 == 0);
     }
     cluster.sync();                                                             // (shared memory stays until all have read it)
 }
@@ -203,6 +211,164 @@ __device__ __forceinline__ uint4 load_8(const __half* src, int n) {
     }
 }
 
+// ---- u[t] = A[id_t] x[t], more rows ----------------------------------------------------------------------------
+
+// The same for more rows: a CTA takes 16 * WM of them, WM warps side by side, so that the factor's columns in shared memory serve all; 8 / WM such groups of warps
+// and the CTAs of a cluster cut the contraction.  x and the factor come through a ring of asynchronous copies, 64 columns per group of warps and
+// stage: a lane reads back the x that it copied itself.
+// Bound: x from memory; from rank 64 on the reads of the factor from shared memory as well.
+template <int NR, int WM>
+struct Tile {
+    static constexpr int kRows = 16 * WM, kRanks = 8 * NR, WK = kWarps / WM;
+    static constexpr int kABytes = WK * kRanks * 128, kStageBytes = kABytes + kWarps * 4 * 32 * 16;
+    static constexpr int kPerSm = NR <= 8 ? 2 : 1, kStages = kPerSm == 1 || kStageBytes <= 27 * 1024 ? 4 : 3;
+    static constexpr int kBytes = kStages * kStageBytes;
+    static_assert(WK * kRows * kRanks * 4 <= kBytes && kPerSm * (kBytes + 1024) <= 228 * 1024 && kBytes <= 227 * 1024, "the sums fit, and so many CTAs per SM");
+};
+template <int NR, int WM>
+__global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_kernel(const __grid_constant__ NarrowParams P) {
+    using T = Tile<NR, WM>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3, wm = warp % WM, wk = warp / WM;
+    const NarrowLayer& L = P.layer[blockIdx.z];
+    const int tile0 = (int)(blockIdx.x / parts) * T::kRows, n = L.n, rank = L.rank, row0 = tile0 + 16 * wm;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    // rows of the tile lane by lane, 32 to a word
+    constexpr int kWords = (T::kRows + 31) / 32;
+    int id[kWords];
+    uint32_t left[kWords], mine[kWords], named[kWords];
+    bool any = false;
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        const int r = 32 * w + lane;
+        id[w] = r < T::kRows && tile0 + r < P.batch ? P.ids[tile0 + r] : -1;
+        if (id[w] >= L.count) id[w] = -1;
+        named[w] = left[w] = __ballot_sync(0xFFFFFFFFu, id[w] >= 0);
+        mine[w] = 0u;
+        any = any || left[w] != 0u;
+    }
+    const int chunks = (n + 63) / 64;
+    const int c0 = (int)((long long)chunks * part / parts), c1 = (int)((long long)chunks * (part + 1) / parts), iters = (c1 - c0 + T::WK - 1) / T::WK;
+    float sum[NR][4] = {};
+    int turn = 0;
+    for (; any; ++turn) {
+        int cur = -1;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+            const int v = __shfl_sync(0xFFFFFFFFu, id[w], left[w] ? __ffs(left[w]) - 1 : 0);
+            if (cur < 0 && left[w]) cur = v;
+        }
+        uint32_t own = 0u;                                                      // of this warp's 16 rows
+        any = false;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+            const uint32_t match = __ballot_sync(0xFFFFFFFFu, id[w] == cur);
+            left[w] &= ~match;
+            any = any || left[w] != 0u;
+            if (turn % (int)gridDim.y == (int)blockIdx.y) {
+                mine[w] |= match;
+                if (w == wm / 2) own = (match >> (16 * (wm & 1))) & 0xFFFFu;
+            }
+        }
+        if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
+        const bool has[2] = {(own >> gq & 1u) != 0u, (own >> (8 + gq) & 1u) != 0u};
+        const __half* a = L.a + (size_t)cur * rank * n;
+        const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
+        auto fetch = [&](int it) {
+            unsigned char* stage = smem + it % T::kStages * T::kStageBytes;
+            if (it < iters) {
+#pragma unroll
+                for (int i0 = 0; i0 < T::WK * T::kRanks * 8; i0 += kThreads) {  // 8 pieces of 16 bytes per row; odd rows have their two halves exchanged (banks)
+                    const int i = i0 + (int)threadIdx.x, piece = i & 7, j = (i >> 3) % T::kRanks, k = (i >> 3) / T::kRanks, chunk = c0 + it * T::WK + k, col = chunk * 64 + piece * 8;
+                    if (T::WK * T::kRanks * 8 % kThreads != 0 && i >= T::WK * T::kRanks * 8) break;
+                    const bool in = chunk < c1 && col < n && j < rank;
+                    copy_async_16(stage + (k * T::kRanks + j) * 128 + ((piece ^ ((j & 1) << 2)) << 4), in ? a + (size_t)j * n + col : L.a, in);
+                }
+                if (own != 0u) {
+                    const int chunk = c0 + it * T::WK + wk;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const bool in = chunk < c1 && chunk * 64 + s * 32 < n && has[m];
+                            copy_async_16(stage + T::kABytes + ((warp * 4 + 2 * s + m) * 32 + lane) * 16, in ? x + (size_t)(8 * m) * n + chunk * 64 + s * 32 : L.x, in);
+                        }
+                }
+            }
+            copy_async_commit();
+        };
+#pragma unroll
+        for (int it = 0; it < T::kStages - 1; ++it) fetch(it);
+        float acc[NR][4] = {};
+        auto flush = [&]() {
+#pragma unroll
+            for (int j = 0; j < NR; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (has[e >> 1]) sum[j][e] += acc[j][e];
+                    acc[j][e] = 0.f;
+                }
+        };
+        for (int it = 0; it < iters; ++it) {
+            copy_async_wait<T::kStages - 2>();
+            __syncthreads();                                                    // everybody's copies of this stage are there, and the slot of the one before is free
+            fetch(it + T::kStages - 1);
+            if (own == 0u) continue;
+            const unsigned char* stage = smem + it % T::kStages * T::kStageBytes;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint4 x0 = *reinterpret_cast<const uint4*>(stage + T::kABytes + ((warp * 4 + 2 * s) * 32 + lane) * 16), x1 = *reinterpret_cast<const uint4*>(stage + T::kABytes + ((warp * 4 + 2 * s + 1) * 32 + lane) * 16);
+                const unsigned char* at = stage + (wk * T::kRanks + gq) * 128 + ((s ^ (gq & 1)) << 6) + tq * 16;
+#pragma unroll
+                for (int j = 0; j < NR; ++j) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(at + j * 8 * 128);
+                    mma_f16(acc[j], x0.x, x1.x, x0.y, x1.y, w.x, w.y);
+                    mma_f16(acc[j], x0.z, x1.z, x0.w, x1.w, w.z, w.w);
+                }
+            }
+            if (it % 4 == 3) flush();
+        }
+        flush();
+        copy_async_wait<0>();
+        __syncthreads();                                                        // (the next adapter fills the same stages)
+    }
+    bool taken = blockIdx.y == 0;                                               // rows without adapter: u is zero, the first cluster's
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) taken = taken || mine[w] != 0u;
+    if (!taken) return;                                                         // (the whole cluster agrees)
+    float* red = reinterpret_cast<float*>(smem);                                // [WK][kRows][kRanks]
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+        float* at = red + ((size_t)wk * T::kRows + 16 * wm + gq) * T::kRanks + 8 * j + 2 * tq;
+        *reinterpret_cast<float2*>(at) = make_float2(sum[j][0], sum[j][1]);
+        *reinterpret_cast<float2*>(at + 8 * T::kRanks) = make_float2(sum[j][2], sum[j][3]);
+    }
+    if (T::WK > 1) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < T::kRows * T::kRanks; e += kThreads) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < T::WK; ++w) s += red[w * T::kRows * T::kRanks + e];
+            red[e] = s;
+        }
+    }
+    cluster.sync();
+    for (int e = part * kThreads + threadIdx.x; e < T::kRows * T::kRanks / 4; e += parts * kThreads) {
+        const int row = e / (T::kRanks / 4), j = e % (T::kRanks / 4) * 4;
+        uint32_t word = 0u;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+            if (row / 32 == w) word = mine[w] | (blockIdx.y == 0 ? ~named[w] : 0u);
+        if (j >= rank || tile0 + row >= P.batch || !((word >> (row & 31)) & 1u)) continue;
+        store_4(L.u + (size_t)(tile0 + row) * rank + j, cluster_sum(cluster, red, parts, e), rank - j, rank % 4 == 0);
+    }
+    cluster.sync();
+}
+
 // ---- y[t] += scale[id_t] * B[id_t]^T u[t] --------------------------------------------------------------------
 
 struct WidenLayer {
@@ -214,75 +380,129 @@ struct WidenLayer {
 struct WidenParams {
     WidenLayer layer[kMaxGroup];
     const int* ids;
-    int batch, rows, shares;                                                    // rows of a CTA: 16, 32 or 64; CTAs that share the adapters of the rows
+    int batch, blocks;                                                          // row blocks of a CTA, one after the other
 };
 constexpr int kWidenRows = 64, kWidenCols = 32 * kWarps;
+template <int R16>
+struct Widen {
+    static constexpr int kRanks = 16 * R16, kStride = kRanks + 4, kBytes = 2 * kWidenRows * kStride * 4;
+};
 
-// A CTA takes up to 64 rows and 256 columns, a warp 32 of them: rows by columns as m16n8k8 MMAs over the rank, the factor's fragments in registers for all
-// rows, u split into two tf32 parts (fp16 parts would need a common exponent per row, which a large entry beside small ones spoils).  The order of columns in
-// MMA tiles and of ranks is free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor entries come from
-// 16-byte loads, its u entries are four consecutive ones.  A row belongs to one adapter, so y is read and written once; it is read ahead of the MMAs.
-// Bound: y, in and out.
+// 16 rows by 32 columns by 16 ranks: `u` the lane's four ranks of row gq, `u8` words further those of row gq + 8; f the factor's fragments of four column tiles.
+__device__ __forceinline__ void widen_step(float (&acc)[4][4], const float* u, int u8, const uint32_t (&f)[4][2]) {
+    const float4 ua = *reinterpret_cast<const float4*>(u), ub = *reinterpret_cast<const float4*>(u + u8);
+    uint32_t hi[2][4], lo[2][4];
+    split_tf32(ua.x, hi[0][0], lo[0][0]); split_tf32(ub.x, hi[0][1], lo[0][1]); split_tf32(ua.y, hi[0][2], lo[0][2]); split_tf32(ub.y, hi[0][3], lo[0][3]);
+    split_tf32(ua.z, hi[1][0], lo[1][0]); split_tf32(ub.z, hi[1][1], lo[1][1]); split_tf32(ua.w, hi[1][2], lo[1][2]); split_tf32(ub.w, hi[1][3], lo[1][3]);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        float w[4][2];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            w[q][0] = half_of(f[q][p], 0);
+            w[q][1] = half_of(f[q][p], 1);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mma_tf32(acc[q], hi[p], w[q][0], w[q][1]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mma_tf32(acc[q], lo[p], w[q][0], w[q][1]);
+    }
+}
+// Row gq (h = 0) or gq + 8 (h = 1) of those products on top of the 8 columns of y that were read as `old`
+template <bool VEC>
+__device__ __forceinline__ void widen_store(__half* y, int n, const uint4& old, const float (&acc)[4][4], int h, float scale) {
+    uint32_t v[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], half_of(v[q], 0)), fmaf(scale, acc[q][2 * h + 1], half_of(v[q], 1)));
+        v[q] = *reinterpret_cast<const uint32_t*>(&r);
+    }
+    if (VEC) {
+        *reinterpret_cast<uint4*>(y) = make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < n) y[q] = __ushort_as_half((unsigned short)(v[q >> 1] >> (16 * (q & 1))));
+    }
+}
+
+struct DecodeLayer {
+    const __half *x, *a, *b;
+    const float* scale;
+    float* u;
+    __half* y;
+    int n, m, rank, count;
+};
+struct DecodeParams {
+    DecodeLayer layer[kMaxGroup];
+    const int* ids;
+    int batch;
+};
+constexpr int kDecodeRows = 64;                                                 // most rows of a batch
+
+// A CTA takes 256 columns, a warp 32 of them, and blocks of 64 rows one after the other: rows by columns as m16n8k8 MMAs over the rank, the factor's fragments in
+// registers for all rows, u split into two tf32 parts (fp16 parts would need a common exponent per row, which a large entry beside small ones spoils).
+// The order of columns in MMA tiles and of ranks is free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor
+// entries come from 16-byte loads, its u entries are four consecutive ones.  A row belongs to one adapter, so y is read and written once; y, u
+// and ids of the next block are on their way while this one is multiplied.
+// Bound: y, in and out; from rank 64 on the MMAs.
 template <int R16, bool VEC>
 __global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const __grid_constant__ WidenParams P) {
-    constexpr int kRanks = 16 * R16, kStride = kRanks + 4, kTiles = kWidenRows / 16;
-    __shared__ __align__(16) float us[kWidenRows * kStride];
+    using W = Widen<R16>;
+    constexpr int kRanks = W::kRanks, kStride = W::kStride, kTiles = kWidenRows / 16;
+    extern __shared__ __align__(16) float us_all[];                             // two blocks of u
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
     const WidenLayer& L = P.layer[blockIdx.z];
     const int col0 = blockIdx.x * kWidenCols + warp * 32, m_all = L.m, rank = L.rank;
-    const int share = (int)blockIdx.y % P.shares, row0 = (int)blockIdx.y / P.shares * P.rows;
+    const int first_row = (int)blockIdx.y * P.blocks * kWidenRows;
+    const int blocks = min(P.blocks, (P.batch - first_row + kWidenRows - 1) / kWidenRows);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if ((int)blockIdx.x * kWidenCols >= m_all) return;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int id0 = lane < P.rows && row0 + lane < P.batch ? P.ids[row0 + lane] : -1, id1 = lane + 32 < P.rows && row0 + lane + 32 < P.batch ? P.ids[row0 + lane + 32] : -1;
-    if (id0 >= L.count) id0 = -1;
-    if (id1 >= L.count) id1 = -1;
-    auto rows_of = [&](int cur) { return __ballot_sync(0xFFFFFFFFu, id0 == cur) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 == cur) << 32); };
-    auto first_of = [&](unsigned long long left) {
-        const int at = __ffsll(left) - 1;
-        return at < 32 ? __shfl_sync(0xFFFFFFFFu, id0, at) : __shfl_sync(0xFFFFFFFFu, id1, at - 32);
-    };
-    const unsigned long long named = __ballot_sync(0xFFFFFFFFu, id0 >= 0) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id1 >= 0) << 32);
-    unsigned long long mine = named;                                            // rows whose adapters are this CTA's
-    if (P.shares > 1) {
-        mine = 0ULL;
-        int turn = 0;
-        for (unsigned long long left = named; left != 0ULL; ++turn) {
-            const unsigned long long match = rows_of(first_of(left));
-            left &= ~match;
-            if (turn % P.shares == share) mine |= match;
-        }
-    }
-    if (mine == 0ULL) return;                                                   // (every warp sees the same)
     const bool fours = rank % 4 == 0;
-    for (int i = threadIdx.x; i < P.rows * (kRanks / 4); i += kThreads) {
-        const int r = i / (kRanks / 4), j = i % (kRanks / 4) * 4;
-        const float* src = L.u + (size_t)(row0 + r) * rank + j;
-        const bool in = (mine >> r) & 1ULL;
-        float* dst = us + r * kStride + j;
-        if (fours) {
-            copy_async_16(dst, in && j < rank ? src : L.u, in && j < rank);
-        } else {
+    auto stage_u = [&](int blk) {
+        const int row0 = first_row + blk * kWidenRows;
+        float* us = us_all + (blk & 1) * (kWidenRows * kStride);
+        if (blk < blocks) {
+            for (int i = threadIdx.x; i < kWidenRows * (kRanks / 4); i += kThreads) {
+                const int r = i / (kRanks / 4), j = i % (kRanks / 4) * 4;
+                const float* src = L.u + (size_t)(row0 + r) * rank + j;
+                const bool in = row0 + r < P.batch;
+                float* dst = us + r * kStride + j;
+                if (fours) {
+                    copy_async_16(dst, in && j < rank ? src : L.u, in && j < rank);
+                } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) copy_async_4(dst + q, in && j + q < rank ? src + q : L.u, in && j + q < rank);
+                    for (int q = 0; q < 4; ++q) copy_async_4(dst + q, in && j + q < rank ? src + q : L.u, in && j + q < rank);
+                }
+            }
         }
-    }
-    copy_async_commit();
-
-    const int c = col0 + 8 * tq;                                                // the lane's columns in y
-    uint4 old[kTiles][2];
-    auto load_y = [&](int mt) {
+        copy_async_commit();
+    };
+    int id[2] = {-1, -1}, next_id[2];
+    auto load_ids = [&](int (&to)[2], int blk) {
+        const int row0 = first_row + blk * kWidenRows;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int r = 16 * mt + 8 * h + gq;
-            old[R16 <= 2 ? mt : 0][h] = load_8<VEC>(L.y + (size_t)(row0 + r) * m_all + c, (mine >> r) & 1ULL ? m_all - c : 0);
+            const int v = blk < blocks && row0 + 32 * h + lane < P.batch ? P.ids[row0 + 32 * h + lane] : -1;
+            to[h] = v < L.count ? v : -1;
         }
     };
-    if (R16 <= 2) {
+    auto rows_of = [&](int cur) { return __ballot_sync(0xFFFFFFFFu, id[0] == cur) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id[1] == cur) << 32); };
+    auto first_of = [&](unsigned long long left) {
+        const int at = __ffsll(left) - 1;
+        return at < 32 ? __shfl_sync(0xFFFFFFFFu, id[0], at) : __shfl_sync(0xFFFFFFFFu, id[1], at - 32);
+    };
+    const int c = col0 + 8 * tq;                                                // the lane's columns in y
+    uint4 old[kTiles][2];
+    auto load_y = [&](int mt, int blk) {
 #pragma unroll
-        for (int mt = 0; mt < kTiles; ++mt) load_y(mt);
-    }
+        for (int h = 0; h < 2; ++h) {
+            const int r = first_row + blk * kWidenRows + 16 * mt + 8 * h + gq;
+            old[mt][h] = load_8<VEC>(L.y + (size_t)r * m_all + c, blk < blocks && r < P.batch ? m_all - c : 0);
+        }
+    };
     uint32_t f[R16][4][2];                                                      // [16 ranks][column tile]: ranks 4 tq and 4 tq + 1, the two behind them
     auto load_factor = [&](int cur) {
         const int cf = col0 + 8 * (gq >> 1);
@@ -302,71 +522,210 @@ __global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const
             }
         }
     };
-    int cur = first_of(mine);
-    load_factor(cur);
-    copy_async_wait<0>();
-    __syncthreads();
-    for (unsigned long long left = mine;;) {
-        const unsigned long long match = rows_of(cur);
-        left &= ~match;
-        const float scale = L.scale[cur];
-        auto tile = [&](int mt) {
-            const uint32_t hits = (uint32_t)(match >> (16 * mt)) & 0xFFFFu;
-            if (hits == 0u) return;
-            if (R16 > 2) load_y(mt);
-            float acc[4][4] = {};
+
+    load_ids(next_id, 0);
+    stage_u(0);
 #pragma unroll
-            for (int k = 0; k < R16; ++k) {
-                const float4 ua = *reinterpret_cast<const float4*>(us + (16 * mt + gq) * kStride + 16 * k + 4 * tq);
-                const float4 ub = *reinterpret_cast<const float4*>(us + (16 * mt + 8 + gq) * kStride + 16 * k + 4 * tq);
-                uint32_t hi[2][4], lo[2][4];
-                split_tf32(ua.x, hi[0][0], lo[0][0]); split_tf32(ub.x, hi[0][1], lo[0][1]); split_tf32(ua.y, hi[0][2], lo[0][2]); split_tf32(ub.y, hi[0][3], lo[0][3]);
-                split_tf32(ua.z, hi[1][0], lo[1][0]); split_tf32(ub.z, hi[1][1], lo[1][1]); split_tf32(ua.w, hi[1][2], lo[1][2]); split_tf32(ub.w, hi[1][3], lo[1][3]);
+    for (int mt = 0; mt < kTiles; ++mt) load_y(mt, 0);
+    int held = -1;                                                              // the adapter whose factor the registers hold
+    for (int blk = 0; blk < blocks; ++blk) {
+        const int row0 = first_row + blk * kWidenRows;
+        id[0] = next_id[0];
+        id[1] = next_id[1];
+        const unsigned long long named = __ballot_sync(0xFFFFFFFFu, id[0] >= 0) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id[1] >= 0) << 32);
+        int cur = named ? first_of(named) : held;
+        if (cur != held) load_factor(held = cur);
+        load_ids(next_id, blk + 1);
+        copy_async_wait<0>();
+        __syncthreads();                                                        // u of this block is there, and nobody reads the one before any more
+        stage_u(blk + 1);
+        const float* us = us_all + (blk & 1) * (kWidenRows * kStride);
+        for (unsigned long long left = named;;) {
+            const unsigned long long match = left ? rows_of(cur) : 0ULL;
+            left &= ~match;
+            const float scale = match ? L.scale[cur] : 0.f;
+            const bool last = left == 0ULL;
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    float w[4][2];
+            for (int mt = 0; mt < kTiles; ++mt) {
+                const uint32_t hits = (uint32_t)(match >> (16 * mt)) & 0xFFFFu;
+                if (hits != 0u) {
+                    float acc[4][4] = {};
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        w[q][0] = half_of(f[k][q][p], 0);
-                        w[q][1] = half_of(f[k][q][p], 1);
-                    }
+                    for (int k = 0; k < R16; ++k) widen_step(acc, us + (16 * mt + gq) * kStride + 16 * k + 4 * tq, 8 * kStride, f[k]);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q], hi[p], w[q][0], w[q][1]);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q], lo[p], w[q][0], w[q][1]);
+                    for (int h = 0; h < 2; ++h)
+                        if (((hits >> (8 * h + gq)) & 1u) && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 16 * mt + 8 * h + gq) * m_all + c, m_all - c, old[mt][h], acc, h, scale);
                 }
+                if (last) load_y(mt, blk + 1);
             }
+            if (last) break;
+            cur = first_of(left);
+            load_factor(held = cur);
+        }
+    }
+    copy_async_wait<0>();
+}
+
+// ---- both steps in one launch, up to 64 rows -------------------------------------------------------------------
+
+// Single tokens of many requests: behind the layer, one cluster of CTAs per tile of 16 rows and adapter that occurs in it (the blockIdx.y-th; a tile has no more
+// than gridDim.y), which makes u as narrow_kernel does and adds its part to y as widen_kernel does, the CTAs taking columns in turn.  The CTAs
+// send their sums of u to one another, so one cluster barrier lies between the two; the first factor entries of the second are
+// fetched before it.  One launch instead of two around the layer saves a launch's latency and the way of u through memory.
+// Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y).
+template <int R16, bool VEC>
+__global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(const __grid_constant__ DecodeParams P) {
+    constexpr int kRows = kNarrowRows, kRanks = 16 * R16, NR = 2 * R16, kStride = kRanks + 4;
+    extern __shared__ __align__(16) float decode_smem[];
+    float* red = decode_smem;                                                   // [kWarps][kRows][kRanks]: the warps' sums
+    float* inbox = red + kWarps * kRows * kRanks;                               // [kMaxCluster][kRows][kRanks]: the CTAs' sums
+    float* us = inbox + kMaxCluster * kRows * kRanks;                           // [kRows][kStride]: u
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
+    const DecodeLayer& L = P.layer[blockIdx.z];
+    const int row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, m_all = L.m, rank = L.rank;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    int id = lane < kRows && row0 + lane < P.batch ? P.ids[row0 + lane] : -1;
+    if (id >= L.count) id = -1;
+    uint32_t left = __ballot_sync(0xFFFFFFFFu, id >= 0);
+    if (blockIdx.y == 0 && part == 0) {                                         // rows without adapter: u is zero
+        const uint32_t bare = ~left;
+        for (int e = threadIdx.x; e < kRows * rank; e += kThreads)
+            if (row0 + e / rank < P.batch && ((bare >> (e / rank)) & 1u)) L.u[(size_t)row0 * rank + e] = 0.f;
+    }
+    uint32_t match = 0u;
+    int cur = -1;
+    for (int turn = 0; left != 0u && turn <= (int)blockIdx.y; ++turn) {
+        cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
+        match = __ballot_sync(0xFFFFFFFFu, id == cur);
+        left &= ~match;
+        if (turn < (int)blockIdx.y) match = 0u;
+    }
+    if (match == 0u) return;                                                    // fewer adapters than clusters (the whole cluster agrees)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // (all CTAs of the cluster run before any writes to another's memory)
+    const float scale = L.scale[cur];
+    const bool has[2] = {(match >> gq & 1u) != 0u, (match >> (8 + gq) & 1u) != 0u};
+
+    float acc[NR][4] = {};
+    {
+        const int units = n / 32, worker = part * kWarps + warp, workers = parts * kWarps;
+        const int u0 = (int)((long long)units * worker / workers), u1 = (int)((long long)units * (worker + 1) / workers);
+        const __half* a = L.a + ((size_t)cur * rank + gq) * n + 8 * tq;
+        const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
+        struct Loads {
+            uint4 x[2], a[NR];
+        };
+        auto load = [&](Loads& l, int u) {
+            const bool in = u < u1;
+            const size_t col = (size_t)u * 32;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (!((hits >> (8 * h + gq)) & 1u) || c >= m_all) continue;
-                const uint4 was = old[R16 <= 2 ? mt : 0][h];
-                uint32_t v[4] = {was.x, was.y, was.z, was.w};
+            for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m) * n + col) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], half_of(v[q], 0)), fmaf(scale, acc[q][2 * h + 1], half_of(v[q], 1)));
-                    v[q] = *reinterpret_cast<const uint32_t*>(&r);
-                }
-                __half* yr = L.y + (size_t)(row0 + 16 * mt + 8 * h + gq) * m_all + c;
-                if (VEC) {
-                    *reinterpret_cast<uint4*>(yr) = make_uint4(v[0], v[1], v[2], v[3]);
-                } else {
+            for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
+        };
+        auto multiply = [&](const Loads& l) {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (c + q < m_all) yr[q] = __ushort_as_half((unsigned short)(v[q >> 1] >> (16 * (q & 1))));
-                }
+            for (int j = 0; j < NR; ++j) {
+                mma_f16(acc[j], l.x[0].x, l.x[1].x, l.x[0].y, l.x[1].y, l.a[j].x, l.a[j].y);
+                mma_f16(acc[j], l.x[0].z, l.x[1].z, l.x[0].w, l.x[1].w, l.a[j].z, l.a[j].w);
             }
         };
-        if (R16 <= 2) {
+        float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;       // the lane's sums: rows gq and gq + 8, ranks 8 j + 2 tq and the next
+        auto flush = [&](bool first) {                                          // (the tensor core truncates: chains of at most 16 MMAs)
 #pragma unroll
-            for (int mt = 0; mt < kTiles; ++mt) tile(mt);
-        } else {
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < NR; ++j) {
+                    float2* at = reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j);
+                    float2 v = make_float2(acc[j][2 * m], acc[j][2 * m + 1]);
+                    if (!first) {
+                        const float2 old = *at;
+                        v.x += old.x;
+                        v.y += old.y;
+                    }
+                    *at = v;
+                    acc[j][2 * m] = acc[j][2 * m + 1] = 0.f;
+                }
+        };
+        Loads even, odd;
+        load(even, u0);
+        int pairs = 0;
 #pragma unroll 1
-            for (int mt = 0; mt < kTiles; ++mt) tile(mt);
+        for (int u = u0; u < u1; u += 2) {
+            load(odd, u + 1);
+            multiply(even);
+            load(even, u + 2);
+            multiply(odd);
+            if (++pairs % 4 == 0) flush(pairs == 4);
         }
-        // (the rows left to this CTA, taken adapter by adapter)
-        if (left == 0ULL) break;
-        cur = first_of(left);
-        load_factor(cur);
+        if (pairs % 4 != 0 || pairs == 0) flush(pairs < 4);
+    }
+
+    // the second factor's entries of the warp's first 32 columns are on their way while u is put together
+    const int groups = (m_all + 31) / 32, step = parts * kWarps;
+    int g = warp * parts + part;                                                // neighbouring columns to different SMs
+    const uint32_t pick = gq & 1 ? 0x7632u : 0x5410u;
+    const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + 8 * (gq >> 1);
+    uint4 raw[R16][4];
+    auto load_factor = [&](int g) {
+        const int cf = 32 * g + 8 * (gq >> 1);
+#pragma unroll
+        for (int k = 0; k < R16; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[k][i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all + 32 * g, g < groups && 16 * k + 4 * tq + i < rank ? m_all - cf : 0);
+    };
+    load_factor(g);
+    __syncthreads();
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
+        float4 s = reinterpret_cast<const float4*>(red)[e];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            const float4 v = reinterpret_cast<const float4*>(red)[w * (kRows * kRanks / 4) + e];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q)
+            if (q < parts) reinterpret_cast<float4*>(cluster.map_shared_rank(inbox, q))[part * (kRows * kRanks / 4) + e] = s;
+    }
+    cluster.sync();                                                             // (nobody writes to another's memory behind it)
+    for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
+        float4 s = reinterpret_cast<const float4*>(inbox)[e];
+        for (int q = 1; q < parts; ++q) {
+            const float4 v = reinterpret_cast<const float4*>(inbox)[q * (kRows * kRanks / 4) + e];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const int row = e / (kRanks / 4), j = e % (kRanks / 4) * 4;
+        *reinterpret_cast<float4*>(us + row * kStride + j) = s;
+        if (part == 0 && j < rank && ((match >> row) & 1u)) store_4(L.u + (size_t)(row0 + row) * rank + j, s, rank - j, rank % 4 == 0);
+    }
+    __syncthreads();
+
+    uint32_t f[R16][4][2];
+    uint4 old[2];
+    for (; g < groups; g += step) {
+        const int c = 32 * g + 8 * tq;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) old[h] = load_8<VEC>(L.y + (size_t)(row0 + 8 * h + gq) * m_all + c, has[h] ? m_all - c : 0);
+#pragma unroll
+        for (int k = 0; k < R16; ++k)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                f[k][0][p] = __byte_perm(raw[k][2 * p].x, raw[k][2 * p + 1].x, pick);
+                f[k][1][p] = __byte_perm(raw[k][2 * p].y, raw[k][2 * p + 1].y, pick);
+                f[k][2][p] = __byte_perm(raw[k][2 * p].z, raw[k][2 * p + 1].z, pick);
+                f[k][3][p] = __byte_perm(raw[k][2 * p].w, raw[k][2 * p + 1].w, pick);
+            }
+        load_factor(g + step);
+        float sum[4][4] = {};
+#pragma unroll
+        for (int k = 0; k < R16; ++k) widen_step(sum, us + gq * kStride + 16 * k + 4 * tq, 8 * kStride, f[k]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (has[h] && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 8 * h + gq) * m_all + c, m_all - c, old[h], sum, h, scale);
     }
 }
 
@@ -520,13 +879,25 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
     cluster.sync();
     const float scale = P.scale[adapter];
     const int cols = min(F::kCols, side - first);
-    for (int e = part * kThreads + threadIdx.x; e < rank * F::kCols; e += parts * kThreads) {
-        const int j = e / F::kCols, c = e % F::kCols;
+    const bool side_fours = side % 4 == 0;
+    for (int e = part * kThreads + threadIdx.x; e < rank * F::kCols / 4; e += parts * kThreads) {
+        const int j = e / (F::kCols / 4), c = e % (F::kCols / 4) * 4;
         if (c >= cols) continue;
-        float total = 0.f;
-        for (int q = 0; q < parts; ++q) total += cluster.map_shared_rank(sums, q)[e];
+        float4 total = cluster_sum(cluster, sums, parts, e);
+        total.x *= scale; total.y *= scale; total.z *= scale; total.w *= scale;
         float* at = S.out + ((size_t)adapter * rank + j) * side + first + c;
-        *at = (P.accumulate ? *at : 0.f) + scale * total;
+        if (P.accumulate) {
+            if (side_fours) {
+                const float4 old = *reinterpret_cast<const float4*>(at);
+                total.x += old.x; total.y += old.y; total.z += old.z; total.w += old.w;
+            } else {
+                total.x += at[0];
+                if (c + 1 < cols) total.y += at[1];
+                if (c + 2 < cols) total.z += at[2];
+                if (c + 3 < cols) total.w += at[3];
+            }
+        }
+        store_4(at, total, cols - c, side_fours);
     }
     cluster.sync();
 }
@@ -566,40 +937,43 @@ int cluster_for(long long tiles) {
     return c;
 }
 
-// CTAs or clusters that share the adapters of a tile of rows: all that can differ while the batch is small, few for prompts.
-int shares_for(int batch) { return batch <= 64 ? std::min(batch, 16) : batch <= 256 ? 4 : 2; }
+// Clusters that share the adapters of a tile of rows: more while there are few tiles.
+int shares_for(int batch) { return batch < 2048 ? 4 : 2; }
 
 cudaError_t launch_narrow(const NarrowParams& P, int n_layers, int max_rank, cudaStream_t stream) {
-    const int mt = P.batch > 256 && max_rank <= 64 ? 2 : 1;
-    const long long tiles = (P.batch + 16 * mt - 1) / (16 * mt);
+    const int wm = P.batch <= 256 ? 1 : P.batch < 2048 ? 4 : 8;                 // 16, 64 or 128 rows to a tile
+    const long long tiles = (P.batch + 16 * wm - 1) / (16 * wm);
     const int c = cluster_for(tiles * n_layers);
     const dim3 grid((unsigned)(tiles * c), (unsigned)shares_for(P.batch), (unsigned)n_layers);
-    auto go = [&](auto kernel, int nr) { return launch(kernel, grid, c, kWarps * 16 * mt * 8 * nr * 4, true, P, stream); };
-    if (mt == 1) return max_rank <= 16 ? go(narrow_kernel<1, 2>, 2) : max_rank <= 32 ? go(narrow_kernel<1, 4>, 4) : max_rank <= 64 ? go(narrow_kernel<1, 8>, 8) : go(narrow_kernel<1, 16>, 16);
-    return max_rank <= 16 ? go(narrow_kernel<2, 2>, 2) : max_rank <= 32 ? go(narrow_kernel<2, 4>, 4) : go(narrow_kernel<2, 8>, 8);
+    auto small = [&](auto kernel, int nr) { return launch(kernel, grid, c, kWarps * kNarrowRows * 8 * nr * 4, true, P, stream); };
+    if (wm == 1) return max_rank <= 16 ? small(narrow_kernel<2>, 2) : max_rank <= 32 ? small(narrow_kernel<4>, 4) : max_rank <= 64 ? small(narrow_kernel<8>, 8) : small(narrow_kernel<16>, 16);
+    auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, c, bytes, true, P, stream); };
+    if (wm == 4)
+        return max_rank <= 16 ? go(narrow_tile_kernel<2, 4>, Tile<2, 4>::kBytes) : max_rank <= 32 ? go(narrow_tile_kernel<4, 4>, Tile<4, 4>::kBytes)
+             : max_rank <= 64 ? go(narrow_tile_kernel<8, 4>, Tile<8, 4>::kBytes) : go(narrow_tile_kernel<16, 4>, Tile<16, 4>::kBytes);
+    return max_rank <= 16 ? go(narrow_tile_kernel<2, 8>, Tile<2, 8>::kBytes) : max_rank <= 32 ? go(narrow_tile_kernel<4, 8>, Tile<4, 8>::kBytes)
+         : max_rank <= 64 ? go(narrow_tile_kernel<8, 8>, Tile<8, 8>::kBytes) : go(narrow_tile_kernel<16, 8>, Tile<16, 8>::kBytes);
 }
 
-// At most 65535 blocks along y: 32768 rows at a time.
-constexpr int kWidenBatch = 32768;
 cudaError_t launch_widen(WidenParams P, int n_layers, int max_rank, int max_m, bool vec, cudaStream_t stream) {
-    const int cols = (max_m + kWidenCols - 1) / kWidenCols, batch = P.batch;
-    cudaError_t e = cudaSuccess;
-    for (int t0 = 0; t0 < batch && e == cudaSuccess; t0 += kWidenBatch) {
-        P.batch = std::min(batch - t0, kWidenBatch);
-        P.rows = kWidenRows;                                                    // fewer rows at a time while the CTAs do not fill the SMs
-        while (P.rows > 16 && (long long)cols * n_layers * ((P.batch + P.rows - 1) / P.rows) < 296) P.rows /= 2;
-        P.shares = batch <= 64 ? shares_for(batch) : 1;
-        const dim3 grid((unsigned)cols, (unsigned)((P.batch + P.rows - 1) / P.rows * P.shares), (unsigned)n_layers);
-        auto go = [&](auto kernel) { return launch(kernel, grid, 0, 0, true, P, stream); };
-        if (vec) e = max_rank <= 16 ? go(widen_kernel<1, true>) : max_rank <= 32 ? go(widen_kernel<2, true>) : max_rank <= 64 ? go(widen_kernel<4, true>) : go(widen_kernel<8, true>);
-        else e = max_rank <= 16 ? go(widen_kernel<1, false>) : max_rank <= 32 ? go(widen_kernel<2, false>) : max_rank <= 64 ? go(widen_kernel<4, false>) : go(widen_kernel<8, false>);
-        P.ids += P.batch;
-        for (int l = 0; l < n_layers; ++l) {
-            P.layer[l].u += (size_t)P.batch * P.layer[l].rank;
-            P.layer[l].y += (size_t)P.batch * P.layer[l].m;
-        }
-    }
-    return e;
+    // as many row blocks to a CTA as leave two CTAs for every SM (296; one more would be a second wave)
+    const long long cols = (max_m + kWidenCols - 1) / kWidenCols, row_blocks = (P.batch + kWidenRows - 1) / kWidenRows;
+    const long long along = std::min(std::max(296 / (cols * n_layers), 1LL), 65535LL);
+    P.blocks = (int)((row_blocks + along - 1) / along);
+    const dim3 grid((unsigned)cols, (unsigned)((row_blocks + P.blocks - 1) / P.blocks), (unsigned)n_layers);
+    auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, 0, bytes, true, P, stream); };
+    if (vec) return max_rank <= 16 ? go(widen_kernel<1, true>, Widen<1>::kBytes) : max_rank <= 32 ? go(widen_kernel<2, true>, Widen<2>::kBytes)
+                  : max_rank <= 64 ? go(widen_kernel<4, true>, Widen<4>::kBytes) : go(widen_kernel<8, true>, Widen<8>::kBytes);
+    return max_rank <= 16 ? go(widen_kernel<1, false>, Widen<1>::kBytes) : max_rank <= 32 ? go(widen_kernel<2, false>, Widen<2>::kBytes)
+         : max_rank <= 64 ? go(widen_kernel<4, false>, Widen<4>::kBytes) : go(widen_kernel<8, false>, Widen<8>::kBytes);
+}
+
+cudaError_t launch_decode(const DecodeParams& P, int n_layers, int max_rank, bool vec, cudaStream_t stream) {
+    const int tiles = (P.batch + kNarrowRows - 1) / kNarrowRows, shares = std::min(P.batch, kNarrowRows);
+    const dim3 grid((unsigned)(tiles * kMaxCluster), (unsigned)shares, (unsigned)n_layers);
+    auto go = [&](auto kernel, int r16) { return launch(kernel, grid, kMaxCluster, ((kWarps + kMaxCluster) * 16 * r16 + 16 * r16 + 4) * kNarrowRows * 4, true, P, stream); };
+    if (vec) return max_rank <= 16 ? go(decode_kernel<1, true>, 1) : max_rank <= 32 ? go(decode_kernel<2, true>, 2) : max_rank <= 64 ? go(decode_kernel<4, true>, 4) : go(decode_kernel<8, true>, 8);
+    return max_rank <= 16 ? go(decode_kernel<1, false>, 1) : max_rank <= 32 ? go(decode_kernel<2, false>, 2) : max_rank <= 64 ? go(decode_kernel<4, false>, 4) : go(decode_kernel<8, false>, 8);
 }
 
 template <int GROUPS>
@@ -700,35 +1074,40 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         return e;
     };
     if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
-    cudaError_t e = each_group([&] {
-        NarrowParams P{};
-        P.ids = ids;
-        P.batch = batch;
-        int max_rank = 0;
-        for (int i = 0; i < n; ++i) {
-            const rabit_adapters* A = adapters[at[i]];
-            P.layer[i] = NarrowLayer{(const __half*)xs[at[i]], (const __half*)A->a, us[at[i]], A->n_in, A->rank, A->count};
-            max_rank = std::max(max_rank, A->rank);
-        }
-        return launch_narrow(P, n, max_rank, st);
-    });
-    if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    cudaError_t e = cudaSuccess;
+    if (batch > kDecodeRows) {
+        e = each_group([&] {
+            NarrowParams P{};
+            P.ids = ids;
+            P.batch = batch;
+            int max_rank = 0;
+            for (int i = 0; i < n; ++i) {
+                const rabit_adapters* A = adapters[at[i]];
+                P.layer[i] = NarrowLayer{(const __half*)xs[at[i]], (const __half*)A->a, us[at[i]], A->n_in, A->rank, A->count};
+                max_rank = std::max(max_rank, A->rank);
+            }
+            return launch_narrow(P, n, max_rank, st);
+        });
+        if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    }
     int rc = n_layers == 1 ? rabit_linear(layers[0], xs[0], ys[0], batch, stream) : rabit_linear_group(layers, xs, ys, n_layers, batch, stream);
     if (rc != RABIT_OK) return rc;
     e = each_group([&] {
+        DecodeParams D{};
         WidenParams P{};
-        P.ids = ids;
-        P.batch = batch;
+        P.ids = D.ids = ids;
+        P.batch = D.batch = batch;
         int max_rank = 0, max_m = 0;
         bool vec = true;
         for (int i = 0; i < n; ++i) {
             const rabit_adapters* A = adapters[at[i]];
             P.layer[i] = WidenLayer{(const __half*)A->b, us[at[i]], A->scale, (__half*)ys[at[i]], A->n_out, A->rank, A->count};
+            D.layer[i] = DecodeLayer{(const __half*)xs[at[i]], (const __half*)A->a, (const __half*)A->b, A->scale, us[at[i]], (__half*)ys[at[i]], A->n_in, A->n_out, A->rank, A->count};
             max_rank = std::max(max_rank, A->rank);
             max_m = std::max(max_m, A->n_out);
             vec = vec && A->n_out % 8 == 0;
         }
-        return launch_widen(P, n, max_rank, max_m, vec, st);
+        return batch > kDecodeRows ? launch_widen(P, n, max_rank, max_m, vec, st) : launch_decode(D, n, max_rank, vec, st);
     });
     if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return RABIT_OK;
