@@ -36,8 +36,10 @@ def adapted(planes, g, h, a, b, scale, x, ids):
         u[t] = a[i] @ x[t]
         err_u[t] = _sum_steps(N) * STEP32 * (np.abs(a[i]) @ np.abs(x[t])) + 1e-37
         y[t] += scale[i] * (u[t] @ b[i])
-        # u enters with 22 bits, the sum over the rank and the scaling are fp32
-        err[t] += abs(scale[i]) * ((err_u[t] + np.abs(u[t]) * (2.0 ** -21 + (r + 4) * STEP32)) @ np.abs(b[i]))
+        # u enters as two fp16 parts of a power of two of its row: with 22 bits, or to 2^-40 of its largest finite entry (the parts' smallest step is
+        # 2^-24 where the largest entry is at least 2^14: rounding is off by half of it, 2^-39 of that entry at most); the sum over the rank and the scaling are fp32
+        size = np.abs(u[t][np.isfinite(u[t])]).max(initial=0.0)
+        err[t] += abs(scale[i]) * ((err_u[t] + 2.0 ** -39 * size + np.abs(u[t]) * (2.0 ** -21 + (2 * r + 4) * STEP32)) @ np.abs(b[i]))
     with np.errstate(invalid="ignore"):
         err += 2.0 ** -11 * (np.abs(y) + err) + 2.0 ** -24                 # the rounding of y, 2^-25 below the normal numbers
     return y, u, err, err_u
@@ -51,7 +53,9 @@ def gradients(scale, v, low, ids, count):
         rows = np.flatnonzero(np.asarray(ids) == i)
         if rows.size:
             out[i] = scale[i] * (low[rows].T @ v[rows])
-            err[i] = abs(scale[i]) * (_sum_steps(rows.size) * STEP32 + 2.0 ** -21) * (np.abs(low[rows]).T @ np.abs(v[rows]))
+            # low enters as two fp16 parts of a power of two of its rank (see adapted): to 2^-39 of that rank's largest entry at worst
+            size = np.abs(low[rows]).max(axis=0)
+            err[i] = abs(scale[i]) * ((_sum_steps(rows.size) * STEP32 + 2.0 ** -21) * (np.abs(low[rows]).T @ np.abs(v[rows])) + 2.0 ** -39 * np.outer(size, np.abs(v[rows]).sum(axis=0)))
     return out, err + 1e-37
 
 

@@ -23,20 +23,25 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], float b0, float b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(__float_as_uint(b0)), "r"(__float_as_uint(b1)));
+// fp32 operands of MMAs with fp16 ones.  Values that share a power of two are scaled so that the largest lies in [2^14, 2^15), then each is the sum of two fp16
+// values: 22 bits of it, or all bits down to 2^-40 of the largest where that is less.  (tf32 MMAs, two per operand part, have twice the number for the
+// same products, and their fp16 operand has to be converted: 4096 x 11008, rank 64, 4096 tokens took 150 us for the gradients and 118 for widen_kernel.)
+__device__ __forceinline__ void range_of(float largest, float& to, float& back) {   // to * largest in [2^14, 2^15); back = 1 / to
+    const uint32_t e = max(__float_as_uint(largest) >> 23, 15u);
+    to = __uint_as_float((268u - e) << 23);
+    back = __uint_as_float((e - 14u) << 23);
 }
-// An fp32 value as the sum of two tf32 values: its top 11 bits, and the top 11 bits of the rest (off by less than 2^-21 of it).  What is exact in
-// the first part has no second one, infinities among it.
-__device__ __forceinline__ void split_tf32(float v, uint32_t& hi, uint32_t& lo) {
-    hi = __float_as_uint(v) & 0xFFFFE000u;
-    const float top = __uint_as_float(hi);
-    lo = top == v ? 0u : __float_as_uint(v - top) & 0xFFFFE000u;
+__device__ __forceinline__ float finite_size(float v) {                         // |v|; 0 for what has no size
+    const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+    return b < 0x7F800000u ? __uint_as_float(b) : 0.f;
 }
-__device__ __forceinline__ float half_of(uint32_t pair, int upper) {
-    return __half2float(__ushort_as_half((unsigned short)(upper ? pair >> 16 : pair)));
+__device__ __forceinline__ void split_f16(float v, float to, __half& hi, __half& lo) {
+    v *= to;
+    hi = __float2half_rn(v);
+    const float rest = v - __half2float(hi);
+    lo = __float2half_rn(finite_size(v) == fabsf(v) ? rest : 0.f);              // (an infinity has no rest, a NaN is one in hi)
 }
+__device__ __forceinline__ float2 floats_of(uint32_t pair) { return __half22float2(*reinterpret_cast<const __half2*>(&pair)); }
 
 constexpr int kMaxCluster = 8;
 // Elements 4 e .. 4 e + 3 of `values` (the same place in every CTA of the cluster), added up in the order of the CTAs.  The loads go out together: one after
@@ -385,28 +390,44 @@ struct WidenParams {
 constexpr int kWidenRows = 64, kWidenCols = 32 * kWarps;
 template <int R16>
 struct Widen {
-    static constexpr int kRanks = 16 * R16, kStride = kRanks + 4, kBytes = 2 * kWidenRows * kStride * 4;
+    static constexpr int kRanks = 16 * R16, kTiles = kWidenRows / 16, kFours = kRanks / 4;
+    static constexpr int kStride = kFours + 1;                                  // 16-byte pieces of a row of u as operand: the rows that a load touches meet in no bank
+    static constexpr int kRing = 2 * kTiles, kRingBytes = kWarps * kRing * 2 * 32 * 16;   // y of so many 16-row tiles ahead: what a lane copied it reads back itself
+    static constexpr int kUBytes = kWidenRows * kRanks * 4;
+    static constexpr int kBytes = kRingBytes + kUBytes + kWidenRows * kStride * 16 + kWidenRows * 4, kPerSm = kBytes <= 112 * 1024 ? 2 : 1;
+    static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
 };
-
-// 16 rows by 32 columns by 16 ranks: `u` the lane's four ranks of row gq, `u8` words further those of row gq + 8; f the factor's fragments of four column tiles.
-__device__ __forceinline__ void widen_step(float (&acc)[4][4], const float* u, int u8, const uint32_t (&f)[4][2]) {
-    const float4 ua = *reinterpret_cast<const float4*>(u), ub = *reinterpret_cast<const float4*>(u + u8);
-    uint32_t hi[2][4], lo[2][4];
-    split_tf32(ua.x, hi[0][0], lo[0][0]); split_tf32(ub.x, hi[0][1], lo[0][1]); split_tf32(ua.y, hi[0][2], lo[0][2]); split_tf32(ub.y, hi[0][3], lo[0][3]);
-    split_tf32(ua.z, hi[1][0], lo[1][0]); split_tf32(ub.z, hi[1][1], lo[1][1]); split_tf32(ua.w, hi[1][2], lo[1][2]); split_tf32(ub.w, hi[1][3], lo[1][3]);
+// Four neighbours of a row of u, whose other parts the next LANES - 1 lanes hold, as the row's operand: four first parts, four second parts.  Returns the
+// factor that takes products back.
+template <int LANES>
+__device__ __forceinline__ float split_row(uint4* at, const float4& v) {
+    float largest = fmaxf(fmaxf(finite_size(v.x), finite_size(v.y)), fmaxf(finite_size(v.z), finite_size(v.w)));
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-        float w[4][2];
+    for (int d = 1; d < LANES; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
+    float to, back;
+    range_of(largest, to, back);
+    __half h[8];
+    split_f16(v.x, to, h[0], h[4]);
+    split_f16(v.y, to, h[1], h[5]);
+    split_f16(v.z, to, h[2], h[6]);
+    split_f16(v.w, to, h[3], h[7]);
+    uint32_t w[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            w[q][0] = half_of(f[q][p], 0);
-            w[q][1] = half_of(f[q][p], 1);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) mma_tf32(acc[q], hi[p], w[q][0], w[q][1]);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) mma_tf32(acc[q], lo[p], w[q][0], w[q][1]);
+    for (int q = 0; q < 4; ++q) {
+        const __half2 two = __halves2half2(h[2 * q], h[2 * q + 1]);
+        w[q] = *reinterpret_cast<const uint32_t*>(&two);
     }
+    *at = make_uint4(w[0], w[1], w[2], w[3]);
+    return back;
+}
+// 16 rows by 32 columns by 16 ranks: at `u` the lane's four ranks of row gq, at u8 those of row gq + 8; f the factor's fragments of four column tiles:
+// ranks 4 tq and 4 tq + 1, the two behind them.
+__device__ __forceinline__ void widen_step(float (&acc)[4][4], const uint4* u, const uint4* u8, const uint32_t (&f)[4][2]) {
+    const uint4 a = *u, b = *u8;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) mma_f16(acc[q], a.x, b.x, a.y, b.y, f[q][0], f[q][1]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) mma_f16(acc[q], a.z, b.z, a.w, b.w, f[q][0], f[q][1]);
 }
 // Row gq (h = 0) or gq + 8 (h = 1) of those products on top of the 8 columns of y that were read as `old`
 template <bool VEC>
@@ -414,7 +435,8 @@ __device__ __forceinline__ void widen_store(__half* y, int n, const uint4& old, 
     uint32_t v[4] = {old.x, old.y, old.z, old.w};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], half_of(v[q], 0)), fmaf(scale, acc[q][2 * h + 1], half_of(v[q], 1)));
+        const float2 was = floats_of(v[q]);
+        const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], was.x), fmaf(scale, acc[q][2 * h + 1], was.y));
         v[q] = *reinterpret_cast<const uint32_t*>(&r);
     }
     if (VEC) {
@@ -440,18 +462,21 @@ struct DecodeParams {
 };
 constexpr int kDecodeRows = 64;                                                 // most rows of a batch
 
-// A CTA takes 256 columns, a warp 32 of them, and blocks of 64 rows one after the other: rows by columns as m16n8k8 MMAs over the rank, the factor's fragments in
-// registers for all rows, u split into two tf32 parts (fp16 parts would need a common exponent per row, which a large entry beside small ones spoils).
-// The order of columns in MMA tiles and of ranks is free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor
+// A CTA takes 256 columns, a warp 32 of them, and blocks of 64 rows one after the other: rows by columns as m16n8k16 MMAs over the rank, the factor's fragments in
+// registers for all rows, a row of u as two fp16 parts of a common power of two.  The order of columns in MMA tiles and of ranks is free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor
 // entries come from 16-byte loads, its u entries are four consecutive ones.  A row belongs to one adapter, so y is read and written once; y, u
-// and ids of the next block are on their way while this one is multiplied.
+// and ids of the next block are on their way while this one is multiplied (copies to shared memory: registers do not hold enough of y for the latency).
 // Bound: y, in and out; from rank 64 on the MMAs.
 template <int R16, bool VEC>
-__global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const __grid_constant__ WidenParams P) {
+__global__ void __launch_bounds__(kThreads, Widen<R16>::kPerSm) widen_kernel(const __grid_constant__ WidenParams P) {
     using W = Widen<R16>;
-    constexpr int kRanks = W::kRanks, kStride = W::kStride, kTiles = kWidenRows / 16;
-    extern __shared__ __align__(16) float us_all[];                             // two blocks of u
+    constexpr int kRanks = W::kRanks, kStride = W::kStride, kTiles = W::kTiles;
+    extern __shared__ __align__(16) unsigned char widen_smem[];                 // rings of y | a block of u | one as operand | its rows' factors
+    float* u_block = reinterpret_cast<float*>(widen_smem + W::kRingBytes);
+    uint4* us = reinterpret_cast<uint4*>(widen_smem + W::kRingBytes + W::kUBytes);
+    float* backs = reinterpret_cast<float*>(us + kWidenRows * kStride);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
+    uint4* ring = reinterpret_cast<uint4*>(widen_smem) + warp * (W::kRing * 2 * 32) + lane;
     const WidenLayer& L = P.layer[blockIdx.z];
     const int col0 = blockIdx.x * kWidenCols + warp * 32, m_all = L.m, rank = L.rank;
     const int first_row = (int)blockIdx.y * P.blocks * kWidenRows;
@@ -461,15 +486,27 @@ __global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const bool fours = rank % 4 == 0;
-    auto stage_u = [&](int blk) {
+    const int c = col0 + 8 * tq;                                                // the lane's columns in y
+    // u of a block and the lane's part of y of the same rows: one group of copies
+    auto fetch = [&](int blk) {
         const int row0 = first_row + blk * kWidenRows;
-        float* us = us_all + (blk & 1) * (kWidenRows * kStride);
         if (blk < blocks) {
+#pragma unroll
+            for (int mt = 0; mt < kTiles; ++mt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = row0 + 16 * mt + 8 * h + gq;
+                    const bool in = r < P.batch && c < m_all;
+                    const __half* src = in ? L.y + (size_t)r * m_all + c : L.y;
+                    uint4* dst = ring + ((blk & 1) * kTiles + mt) * 64 + h * 32;
+                    if (VEC) copy_async_16(dst, src, in);
+                    else *dst = load_8<false>(src, in ? m_all - c : 0);
+                }
             for (int i = threadIdx.x; i < kWidenRows * (kRanks / 4); i += kThreads) {
                 const int r = i / (kRanks / 4), j = i % (kRanks / 4) * 4;
                 const float* src = L.u + (size_t)(row0 + r) * rank + j;
                 const bool in = row0 + r < P.batch;
-                float* dst = us + r * kStride + j;
+                float* dst = u_block + 4 * i;
                 if (fours) {
                     copy_async_16(dst, in && j < rank ? src : L.u, in && j < rank);
                 } else {
@@ -494,15 +531,6 @@ __global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const
         const int at = __ffsll(left) - 1;
         return at < 32 ? __shfl_sync(0xFFFFFFFFu, id[0], at) : __shfl_sync(0xFFFFFFFFu, id[1], at - 32);
     };
-    const int c = col0 + 8 * tq;                                                // the lane's columns in y
-    uint4 old[kTiles][2];
-    auto load_y = [&](int mt, int blk) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = first_row + blk * kWidenRows + 16 * mt + 8 * h + gq;
-            old[mt][h] = load_8<VEC>(L.y + (size_t)r * m_all + c, blk < blocks && r < P.batch ? m_all - c : 0);
-        }
-    };
     uint32_t f[R16][4][2];                                                      // [16 ranks][column tile]: ranks 4 tq and 4 tq + 1, the two behind them
     auto load_factor = [&](int cur) {
         const int cf = col0 + 8 * (gq >> 1);
@@ -523,10 +551,8 @@ __global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const
         }
     };
 
+    fetch(0);
     load_ids(next_id, 0);
-    stage_u(0);
-#pragma unroll
-    for (int mt = 0; mt < kTiles; ++mt) load_y(mt, 0);
     int held = -1;                                                              // the adapter whose factor the registers hold
     for (int blk = 0; blk < blocks; ++blk) {
         const int row0 = first_row + blk * kWidenRows;
@@ -537,30 +563,31 @@ __global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const
         if (cur != held) load_factor(held = cur);
         load_ids(next_id, blk + 1);
         copy_async_wait<0>();
-        __syncthreads();                                                        // u of this block is there, and nobody reads the one before any more
-        stage_u(blk + 1);
-        const float* us = us_all + (blk & 1) * (kWidenRows * kStride);
-        for (unsigned long long left = named;;) {
-            const unsigned long long match = left ? rows_of(cur) : 0ULL;
+        __syncthreads();                                                        // this block is there, and nobody reads the one before any more
+        for (int i = threadIdx.x; i < kWidenRows * W::kFours; i += kThreads) {
+            const float back = split_row<W::kFours>(us + i / W::kFours * kStride + i % W::kFours, reinterpret_cast<const float4*>(u_block)[i]);
+            if (i % W::kFours == 0) backs[i / W::kFours] = back;
+        }
+        __syncthreads();
+        fetch(blk + 1);
+        const uint4* old = ring + (blk & 1) * kTiles * 64;
+        for (unsigned long long left = named; left != 0ULL;) {
+            if (cur != held) load_factor(held = cur);
+            const unsigned long long match = rows_of(cur);
             left &= ~match;
-            const float scale = match ? L.scale[cur] : 0.f;
-            const bool last = left == 0ULL;
+            const float scale = L.scale[cur];
 #pragma unroll
             for (int mt = 0; mt < kTiles; ++mt) {
                 const uint32_t hits = (uint32_t)(match >> (16 * mt)) & 0xFFFFu;
-                if (hits != 0u) {
-                    float acc[4][4] = {};
+                if (hits == 0u) continue;
+                float acc[4][4] = {};
 #pragma unroll
-                    for (int k = 0; k < R16; ++k) widen_step(acc, us + (16 * mt + gq) * kStride + 16 * k + 4 * tq, 8 * kStride, f[k]);
+                for (int k = 0; k < R16; ++k) widen_step(acc, us + (16 * mt + gq) * kStride + 4 * k + tq, us + (16 * mt + 8 + gq) * kStride + 4 * k + tq, f[k]);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        if (((hits >> (8 * h + gq)) & 1u) && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 16 * mt + 8 * h + gq) * m_all + c, m_all - c, old[mt][h], acc, h, scale);
-                }
-                if (last) load_y(mt, blk + 1);
+                for (int h = 0; h < 2; ++h)
+                    if (((hits >> (8 * h + gq)) & 1u) && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 16 * mt + 8 * h + gq) * m_all + c, m_all - c, old[mt * 64 + h * 32], acc, h, scale * backs[16 * mt + 8 * h + gq]);
             }
-            if (last) break;
-            cur = first_of(left);
-            load_factor(held = cur);
+            if (left != 0ULL) cur = first_of(left);
         }
     }
     copy_async_wait<0>();
@@ -575,11 +602,12 @@ __global__ void __launch_bounds__(kThreads, R16 <= 4 ? 2 : 1) widen_kernel(const
 // Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y).
 template <int R16, bool VEC>
 __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(const __grid_constant__ DecodeParams P) {
-    constexpr int kRows = kNarrowRows, kRanks = 16 * R16, NR = 2 * R16, kStride = kRanks + 4;
+    constexpr int kRows = kNarrowRows, kRanks = 16 * R16, NR = 2 * R16, kFours = kRanks / 4, kStride = kFours + 1;
     extern __shared__ __align__(16) float decode_smem[];
     float* red = decode_smem;                                                   // [kWarps][kRows][kRanks]: the warps' sums
     float* inbox = red + kWarps * kRows * kRanks;                               // [kMaxCluster][kRows][kRanks]: the CTAs' sums
-    float* us = inbox + kMaxCluster * kRows * kRanks;                           // [kRows][kStride]: u
+    uint4* us = reinterpret_cast<uint4*>(inbox + kMaxCluster * kRows * kRanks); // [kRows][kStride]: u as operand, then its rows' factors
+    float* backs = reinterpret_cast<float*>(us + kRows * kStride);
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
@@ -699,7 +727,8 @@ __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(cons
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
         const int row = e / (kRanks / 4), j = e % (kRanks / 4) * 4;
-        *reinterpret_cast<float4*>(us + row * kStride + j) = s;
+        const float back = split_row<kFours>(us + row * kStride + j / 4, s);
+        if (j == 0) backs[row] = back;
         if (part == 0 && j < rank && ((match >> row) & 1u)) store_4(L.u + (size_t)(row0 + row) * rank + j, s, rank - j, rank % 4 == 0);
     }
     __syncthreads();
@@ -722,10 +751,10 @@ __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(cons
         load_factor(g + step);
         float sum[4][4] = {};
 #pragma unroll
-        for (int k = 0; k < R16; ++k) widen_step(sum, us + gq * kStride + 16 * k + 4 * tq, 8 * kStride, f[k]);
+        for (int k = 0; k < R16; ++k) widen_step(sum, us + gq * kStride + 4 * k + tq, us + (8 + gq) * kStride + 4 * k + tq, f[k]);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (has[h] && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 8 * h + gq) * m_all + c, m_all - c, old[h], sum, h, scale);
+            if (has[h] && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 8 * h + gq) * m_all + c, m_all - c, old[h], sum, h, scale * backs[8 * h + gq]);
     }
 }
 
@@ -743,23 +772,30 @@ struct FactorParams {
     const float* scale;
     int batch, rank, accumulate;
 };
-constexpr int kFactorRows = 32, kFactorStages = 3, kFactorList = 1024, kFactorChunk = 64;
+constexpr int kFactorRows = 32, kFactorList = 1024, kFactorChunk = 64;
 
 template <int GROUPS>
-struct Factor {                                                                 // a stage: rows of v, rows of low; behind the stages the list of rows; sums over all of it at the end
-    static constexpr int kRanks = 16 * GROUPS, kCols = 64 * (kWarps / GROUPS);
-    static constexpr int kVStride = kCols * 2 + 32, kLowStride = kRanks + 8;    // bytes, words: no two of the rows that a fragment load touches meet in a bank
+struct Factor {                                                                 // GROUPS * 16 ranks by COLS * 64 columns, HALVES groups of warps for the halves of a tile's rows
+    static constexpr int kRanks = 16 * GROUPS, kHalves = GROUPS == 1 ? 2 : 1, kColWarps = kWarps / (GROUPS * kHalves), kCols = 64 * kColWarps;
+    static constexpr int kVStride = kCols * 2 + 16, kLowStride = kRanks + 8, kAStride = kFactorRows * 2 + 16;   // bytes, words, bytes: rows that are read together meet in no bank
     static constexpr int kVBytes = kFactorRows * kVStride, kStageBytes = kVBytes + kFactorRows * kLowStride * 4;
-    static constexpr int kBytes = kFactorStages * kStageBytes + kFactorList * 4;
-    static_assert(kRanks * kCols * 4 <= kBytes && 2 * (kBytes + 1024 + 128) <= 228 * 1024, "the sums fit, two CTAs per SM");
+    static constexpr int kStages = GROUPS == 8 ? 3 : 4, kABytes = kRanks * kAStride;
+    static constexpr int kAAt = kStages * kStageBytes, kBackAt = kAAt + 4 * kABytes, kListAt = kBackAt + 2 * kRanks * 4, kBytes = kListAt + kFactorList * 4;
+    static_assert(kHalves * kRanks * kCols * 4 <= kBytes && 2 * (kBytes + 1024 + 128) <= 228 * 1024, "the sums fit, two CTAs per SM");
 };
+__device__ __forceinline__ void ldmatrix(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_trans(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
 
-// Ranks by columns as m16n8k8 MMAs over the rows, low split into two tf32 parts (as in widen_kernel), v exact.  A warp takes 16 ranks and 64 columns, GROUPS warps
-// the same columns: of a row a lane reads 8 consecutive columns, one for each of 8 MMA tiles.  The rows of a cluster's adapter are dealt out to its CTAs in
-// chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor multiplied by zero (0 * NaN), then streams
-// them through a ring of three stages of 32 rows.
+// Ranks by columns as m16n8k16 MMAs over the rows, v as it is, low as two fp16 parts of a power of two per rank and tile of 32 rows (v and low meet as matrices
+// with the rows inside, so low is turned when it is split).  A warp takes 16 ranks and 64 columns, GROUPS warps the same columns.  The rows of a
+// cluster's adapter are dealt out to its CTAs in chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor
+// multiplied by zero (0 * NaN), then streams them through a ring of stages; the next tile is split beside the MMAs of the one at hand.
 // Sums of 32 rows are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
-// Bound: v from memory, tf32 MMAs from rank 32 on.
+// Bound: v from memory; from rank 64 on the MMAs.
 template <int GROUPS, bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_constant__ FactorParams P) {
     using F = Factor<GROUPS>;
@@ -768,13 +804,18 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
-    const int group = warp % GROUPS, wc = warp / GROUPS;
+    const int group = warp % GROUPS, wc = warp / GROUPS % F::kColWarps, half = warp / (GROUPS * F::kColWarps);
     int block = (int)blockIdx.x / parts;
     const FactorSide& S = P.s[block < P.s[0].blocks ? 0 : 1];
     if (block >= P.s[0].blocks) block -= P.s[0].blocks;
     const int adapter = blockIdx.y, side = S.side, first = block * F::kCols, rank = P.rank;
     const bool fours = rank % 4 == 0;
-    int* list = reinterpret_cast<int*>(smem + kFactorStages * F::kStageBytes);
+    int* list = reinterpret_cast<int*>(smem + F::kListAt);
+    float* backs = reinterpret_cast<float*>(smem + F::kBackAt);                 // [2][kRanks]
+    const uint32_t smem32 = (uint32_t)__cvta_generic_to_shared(smem);
+    // the lane's row of the 8 x 8 matrices that it names: of v rows of the tile by columns, of low ranks by rows of the tile
+    const uint32_t v_at = smem32 + (uint32_t)((lane & 15) * F::kVStride + (wc * 64 + (lane >> 4) * 8) * 2);
+    const uint32_t a_at = smem32 + (uint32_t)(F::kAAt + (group * 16 + (lane & 15)) * F::kAStride + (lane >> 4) * 16);
     float sum[8][4] = {};
     for (long long base = 0; base < P.batch; base += (long long)kFactorList * parts) {
         // the rows of this round that are the adapter's, in order
@@ -797,7 +838,7 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
         }
         const int n_tiles = (n_list + kFactorRows - 1) / kFactorRows;
         auto fetch = [&](int tile) {
-            unsigned char* stage = smem + tile % kFactorStages * F::kStageBytes;
+            unsigned char* stage = smem + tile % F::kStages * F::kStageBytes;
             if (tile < n_tiles) {
                 constexpr int kPieces = F::kCols / 8;                           // 16 bytes of a row each
 #pragma unroll
@@ -826,55 +867,82 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
             }
             copy_async_commit();
         };
-        fetch(0);
-        fetch(1);
+        // low of a tile as operand: kThreads / kRanks neighbouring lanes share a rank's 32 rows, two neighbouring rows at a time
+        auto split = [&](int tile) {
+            if (tile >= n_tiles) return;
+            constexpr int kShare = kThreads / F::kRanks, kPairs = kFactorRows / 2 / kShare;
+            const float* low = reinterpret_cast<const float*>(smem + tile % F::kStages * F::kStageBytes + F::kVBytes);
+            const int j = threadIdx.x / kShare, sub = threadIdx.x % kShare;
+            float v[kPairs][2], largest = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    v[i][e] = low[(2 * (sub + kShare * i) + e) * F::kLowStride + j];
+                    largest = fmaxf(largest, finite_size(v[i][e]));
+                }
+#pragma unroll
+            for (int d = 1; d < kShare; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
+            float to, back;
+            range_of(largest, to, back);
+            if (sub == 0) backs[(tile & 1) * F::kRanks + j] = back;
+            unsigned char* out = smem + F::kAAt + (tile & 1) * 2 * F::kABytes + j * F::kAStride;
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                __half h[2], l[2];
+                split_f16(v[i][0], to, h[0], l[0]);
+                split_f16(v[i][1], to, h[1], l[1]);
+                *reinterpret_cast<__half2*>(out + (sub + kShare * i) * 4) = __halves2half2(h[0], h[1]);
+                *reinterpret_cast<__half2*>(out + F::kABytes + (sub + kShare * i) * 4) = __halves2half2(l[0], l[1]);
+            }
+        };
+#pragma unroll
+        for (int tile = 0; tile < F::kStages - 1; ++tile) fetch(tile);
+        copy_async_wait<F::kStages - 2>();
+        __syncthreads();
+        split(0);
         for (int tile = 0; tile < n_tiles; ++tile) {
-            copy_async_wait<1>();
-            __syncthreads();                                                    // everybody's copies of this tile are there, and the slot of the one before is free
-            fetch(tile + 2);
-            const unsigned char* stage = smem + tile % kFactorStages * F::kStageBytes;
-            const float* low = reinterpret_cast<const float*>(stage + F::kVBytes) + tq * F::kLowStride + group * 16 + gq;
-            const unsigned char* v = stage + tq * F::kVStride + (wc * 64 + 8 * gq) * 2;
+            copy_async_wait<F::kStages - 3>();
+            __syncthreads();                                                    // the next tile is there, this one is split, and the slots of the one before are free
+            fetch(tile + F::kStages - 1);
+            split(tile + 1);
+            const uint32_t v = v_at + (uint32_t)(tile % F::kStages * F::kStageBytes), a = a_at + (uint32_t)((tile & 1) * 2 * F::kABytes);
             float acc[8][4] = {};
 #pragma unroll
-            for (int s = 0; s < kFactorRows / 8; ++s) {
+            for (int s0 = 0; s0 < 2 / F::kHalves; ++s0) {
+                const int s = F::kHalves == 2 ? half : s0;                      // 16 rows of the tile
                 uint32_t hi[4], lo[4];
-                const float* at = low + 8 * s * F::kLowStride;
-                split_tf32(at[0], hi[0], lo[0]);
-                split_tf32(at[8], hi[1], lo[1]);
-                split_tf32(at[4 * F::kLowStride], hi[2], lo[2]);
-                split_tf32(at[4 * F::kLowStride + 8], hi[3], lo[3]);
-                const uint4 v0 = *reinterpret_cast<const uint4*>(v + 8 * s * F::kVStride), v1 = *reinterpret_cast<const uint4*>(v + (8 * s + 4) * F::kVStride);
-                const uint32_t w[2][4] = {{v0.x, v0.y, v0.z, v0.w}, {v1.x, v1.y, v1.z, v1.w}};
+                ldmatrix(hi, a + (uint32_t)(s * 32));
+                ldmatrix(lo, a + (uint32_t)(F::kABytes + s * 32));
 #pragma unroll
-                for (int q0 = 0; q0 < 8; q0 += 4) {
-                    float b[4][2];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        b[q][0] = half_of(w[0][(q0 + q) >> 1], q & 1);
-                        b[q][1] = half_of(w[1][(q0 + q) >> 1], q & 1);
-                    }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q0 + q], hi, b[q][0], b[q][1]);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) mma_tf32(acc[q0 + q], lo, b[q][0], b[q][1]);
+                for (int q = 0; q < 8; q += 2) {
+                    uint32_t b[4];
+                    ldmatrix_trans(b, v + (uint32_t)(s * 16 * F::kVStride + q * 16));
+                    mma_f16(acc[q], hi[0], hi[1], hi[2], hi[3], b[0], b[1]);
+                    mma_f16(acc[q + 1], hi[0], hi[1], hi[2], hi[3], b[2], b[3]);
+                    mma_f16(acc[q], lo[0], lo[1], lo[2], lo[3], b[0], b[1]);
+                    mma_f16(acc[q + 1], lo[0], lo[1], lo[2], lo[3], b[2], b[3]);
                 }
             }
+            const float back0 = backs[(tile & 1) * F::kRanks + group * 16 + gq], back1 = backs[(tile & 1) * F::kRanks + group * 16 + 8 + gq];
 #pragma unroll
             for (int q = 0; q < 8; ++q)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[q][e] += acc[q][e];
+                for (int e = 0; e < 4; ++e) sum[q][e] = fmaf(e < 2 ? back0 : back1, acc[q][e], sum[q][e]);
         }
         copy_async_wait<0>();
         __syncthreads();                                                        // (the list is written again)
     }
-    // the CTA's sums [rank][column of the block], then over the cluster.  Column of MMA column n of tile q: 8 n + q.
+    // the CTA's sums [half][rank][column of the block], then over the cluster
     float* sums = reinterpret_cast<float*>(smem);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        float* at = sums + (group * 16 + gq + 8 * (e >> 1)) * F::kCols + wc * 64 + 8 * (2 * tq + (e & 1));
+    for (int q = 0; q < 8; ++q)
 #pragma unroll
-        for (int q = 0; q < 8; q += 4) *reinterpret_cast<float4*>(at + q) = make_float4(sum[q][e], sum[q + 1][e], sum[q + 2][e], sum[q + 3][e]);
+        for (int e = 0; e < 4; e += 2)
+            *reinterpret_cast<float2*>(sums + (half * F::kRanks + group * 16 + gq + 4 * e) * F::kCols + wc * 64 + 8 * q + 2 * tq) = make_float2(sum[q][e], sum[q][e + 1]);
+    if (F::kHalves == 2) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < F::kRanks * F::kCols; e += kThreads) sums[e] += sums[F::kRanks * F::kCols + e];
     }
     cluster.sync();
     const float scale = P.scale[adapter];
@@ -971,7 +1039,7 @@ cudaError_t launch_widen(WidenParams P, int n_layers, int max_rank, int max_m, b
 cudaError_t launch_decode(const DecodeParams& P, int n_layers, int max_rank, bool vec, cudaStream_t stream) {
     const int tiles = (P.batch + kNarrowRows - 1) / kNarrowRows, shares = std::min(P.batch, kNarrowRows);
     const dim3 grid((unsigned)(tiles * kMaxCluster), (unsigned)shares, (unsigned)n_layers);
-    auto go = [&](auto kernel, int r16) { return launch(kernel, grid, kMaxCluster, ((kWarps + kMaxCluster) * 16 * r16 + 16 * r16 + 4) * kNarrowRows * 4, true, P, stream); };
+    auto go = [&](auto kernel, int r16) { return launch(kernel, grid, kMaxCluster, ((kWarps + kMaxCluster) * 16 * r16 * 4 + (4 * r16 + 1) * 16 + 4) * kNarrowRows, true, P, stream); };
     if (vec) return max_rank <= 16 ? go(decode_kernel<1, true>, 1) : max_rank <= 32 ? go(decode_kernel<2, true>, 2) : max_rank <= 64 ? go(decode_kernel<4, true>, 4) : go(decode_kernel<8, true>, 8);
     return max_rank <= 16 ? go(decode_kernel<1, false>, 1) : max_rank <= 32 ? go(decode_kernel<2, false>, 2) : max_rank <= 64 ? go(decode_kernel<4, false>, 4) : go(decode_kernel<8, false>, 8);
 }
