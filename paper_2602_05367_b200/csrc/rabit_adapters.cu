@@ -23,6 +23,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the same on top of zero
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // fp32 operands of MMAs with fp16 ones.  Values that share a power of two are scaled so that the largest lies in [2^14, 2^15), then each is the sum of two fp16
 // values: 22 bits of it, or all bits down to 2^-40 of the largest where that is less.  (tf32 MMAs, two per operand part, have twice the number for the
 // same products, and their fp16 operand has to be converted: 4096 x 11008, rank 64, 4096 tokens took 150 us for the gradients and 118 for widen_kernel.)
@@ -68,6 +73,9 @@ __device__ __forceinline__ void store_4(float* at, const float4& v, int n, bool 
         if (n > 3) at[3] = v.w;
     }
 }
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // ---- u[t] = A[id_t] x[t] -----------------------------------------------------------------------------------
 
@@ -387,48 +395,68 @@ struct WidenParams {
     const int* ids;
     int batch, blocks;                                                          // row blocks of a CTA, one after the other
 };
-constexpr int kWidenRows = 64, kWidenCols = 32 * kWarps;
+// 16-byte pieces of a row (pair) of u as operand: half as many again are 4 more than a multiple of 8 from pair to pair, so that two pairs that a load touches, 64
+// bytes each, meet in no bank
+__host__ __device__ constexpr int operand_stride(int fours) { return fours + 2; }
+constexpr int kWidenRows = 32;
+// u as operand of an MMA of 16 rows and 16 ranks: four registers that lie behind one another, ranks 4 tq, 4 tq + 1 of row gq and of row gq + 8, then the two ranks
+// behind those; one 16-byte piece in shared memory for the first parts, `kPair` pieces further one for the second (put together in registers, every
+// operand would cost four moves).  [pair of rows][first, second][ranks / 4], the pairs of a 16-row tile 8 to a block.
 template <int R16>
-struct Widen {
-    static constexpr int kRanks = 16 * R16, kTiles = kWidenRows / 16, kFours = kRanks / 4;
-    static constexpr int kStride = kFours + 1;                                  // 16-byte pieces of a row of u as operand: the rows that a load touches meet in no bank
-    static constexpr int kRing = 2 * kTiles, kRingBytes = kWarps * kRing * 2 * 32 * 16;   // y of so many 16-row tiles ahead: what a lane copied it reads back itself
-    static constexpr int kUBytes = kWidenRows * kRanks * 4;
-    static constexpr int kBytes = kRingBytes + kUBytes + kWidenRows * kStride * 16 + kWidenRows * 4, kPerSm = kBytes <= 112 * 1024 ? 2 : 1;
-    static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
+struct Operand {
+    static constexpr int kFours = 4 * R16, kSecond = operand_stride(kFours), kPair = 2 * kSecond;
+    static __host__ __device__ constexpr int pieces(int rows) { return rows / 2 * kPair; }
+    // where rows `row` and row ^ 8 lie
+    static __device__ __forceinline__ int at(int row) { return ((row >> 4) * 8 + (row & 7)) * kPair; }
 };
-// Four neighbours of a row of u, whose other parts the next LANES - 1 lanes hold, as the row's operand: four first parts, four second parts.  Returns the
-// factor that takes products back.
-template <int LANES>
-__device__ __forceinline__ float split_row(uint4* at, const float4& v) {
+// Four neighbours of row `row` of u, whose other parts the next kFours - 1 lanes hold, into the operand.  Returns the factor that takes products back.
+template <int R16>
+__device__ __forceinline__ float split_row(uint4* operand, int row, int four, const float4& v) {
+    using O = Operand<R16>;
     float largest = fmaxf(fmaxf(finite_size(v.x), finite_size(v.y)), fmaxf(finite_size(v.z), finite_size(v.w)));
 #pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
+    for (int d = 1; d < O::kFours; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
     float to, back;
     range_of(largest, to, back);
-    __half h[8];
-    split_f16(v.x, to, h[0], h[4]);
-    split_f16(v.y, to, h[1], h[5]);
-    split_f16(v.z, to, h[2], h[6]);
-    split_f16(v.w, to, h[3], h[7]);
-    uint32_t w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const __half2 two = __halves2half2(h[2 * q], h[2 * q + 1]);
-        w[q] = *reinterpret_cast<const uint32_t*>(&two);
-    }
-    *at = make_uint4(w[0], w[1], w[2], w[3]);
+    __half h[4], l[4];
+    split_f16(v.x, to, h[0], l[0]);
+    split_f16(v.y, to, h[1], l[1]);
+    split_f16(v.z, to, h[2], l[2]);
+    split_f16(v.w, to, h[3], l[3]);
+    __half2* hi = reinterpret_cast<__half2*>(operand + O::at(row) + four) + ((row >> 3) & 1);
+    __half2* lo = hi + 4 * O::kSecond;
+    hi[0] = __halves2half2(h[0], h[1]);
+    hi[2] = __halves2half2(h[2], h[3]);
+    lo[0] = __halves2half2(l[0], l[1]);
+    lo[2] = __halves2half2(l[2], l[3]);
     return back;
 }
-// 16 rows by 32 columns by 16 ranks: at `u` the lane's four ranks of row gq, at u8 those of row gq + 8; f the factor's fragments of four column tiles:
-// ranks 4 tq and 4 tq + 1, the two behind them.
-__device__ __forceinline__ void widen_step(float (&acc)[4][4], const uint4* u, const uint4* u8, const uint32_t (&f)[4][2]) {
-    const uint4 a = *u, b = *u8;
+// 16 rows by GROUPS * 32 columns by 16 ranks: `u` the lane's piece of the operand, `second` pieces further its second part; f the factor's fragments of the groups' four
+// column tiles: ranks 4 tq and 4 tq + 1, the two behind them.
+template <int GROUPS>
+__device__ __forceinline__ void widen_step(float (&acc)[GROUPS][4][4], bool first, const uint4* u, int second, const uint32_t (&f)[GROUPS][4][2]) {
+    const uint4 a = u[0], b = u[second];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) mma_f16(acc[q], a.x, b.x, a.y, b.y, f[q][0], f[q][1]);
+    for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) mma_f16(acc[q], a.z, b.z, a.w, b.w, f[q][0], f[q][1]);
+        for (int q = 0; q < 4; ++q) {
+            if (first) mma_f16_first(acc[g][q], a.x, a.y, a.z, a.w, f[g][q][0], f[g][q][1]);
+            else mma_f16(acc[g][q], a.x, a.y, a.z, a.w, f[g][q][0], f[g][q][1]);
+        }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mma_f16(acc[g][q], b.x, b.y, b.z, b.w, f[g][q][0], f[g][q][1]);
 }
+template <int R16, bool VEC>
+struct Widen {
+    static constexpr int kRanks = 16 * R16, kTiles = kWidenRows / 16, kFours = kRanks / 4;
+    static constexpr int kGroups = R16 <= 4 && VEC ? 2 : 1, kCols = 32 * kGroups * kWarps;      // of 32 columns to a warp
+    static constexpr int kBlockPieces = kTiles * 2 * kGroups * 32;              // 16-byte pieces of y of a warp in a block; what a lane copied it reads back itself
+    static constexpr int kRingBytes = 2 * kWarps * kBlockPieces * 16, kUBytes = kWidenRows * kRanks * 4;
+    static constexpr int kBytes = kRingBytes + kUBytes + Operand<R16>::pieces(kWidenRows) * 16 + kWidenRows * 4;
+    static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs per SM");
+};
 // Row gq (h = 0) or gq + 8 (h = 1) of those products on top of the 8 columns of y that were read as `old`
 template <bool VEC>
 __device__ __forceinline__ void widen_store(__half* y, int n, const uint4& old, const float (&acc)[4][4], int h, float scale) {
@@ -460,301 +488,348 @@ struct DecodeParams {
     const int* ids;
     int batch;
 };
-constexpr int kDecodeRows = 64;                                                 // most rows of a batch
+constexpr int kDecodeRows = 256, kDecodeRowsOdd = 64;            // most rows of a batch; of one whose outputs are not 16-byte pieces
 
-// A CTA takes 256 columns, a warp 32 of them, and blocks of 64 rows one after the other: rows by columns as m16n8k16 MMAs over the rank, the factor's fragments in
-// registers for all rows, a row of u as two fp16 parts of a common power of two.  The order of columns in MMA tiles and of ranks is free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor
-// entries come from 16-byte loads, its u entries are four consecutive ones.  A row belongs to one adapter, so y is read and written once; y, u
-// and ids of the next block are on their way while this one is multiplied (copies to shared memory: registers do not hold enough of y for the latency).
-// Bound: y, in and out; from rank 64 on the MMAs.
+// A CTA takes 512 columns (256 beyond rank 64), a warp 64 (32) of them, and blocks of 32 rows one after the other: rows by columns as m16n8k16 MMAs over the rank, the
+// factor's fragments in registers for all rows, a row of u as two fp16 parts of a common power of two.  The order of columns in MMA tiles and of ranks is
+// free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor entries come from 16-byte loads, its u entries
+// are four consecutive ones.  A row belongs to one adapter, so y is read and written once; y, u and ids of the next block are on their way while this
+// one is multiplied (copies to shared memory: registers do not hold enough of y for the latency).
+// Bound: y, in and out; the instructions around the MMAs are as many as that leaves room for, which is why a warp takes 64 columns.
 template <int R16, bool VEC>
-__global__ void __launch_bounds__(kThreads, Widen<R16>::kPerSm) widen_kernel(const __grid_constant__ WidenParams P) {
-    using W = Widen<R16>;
-    constexpr int kRanks = W::kRanks, kStride = W::kStride, kTiles = W::kTiles;
-    extern __shared__ __align__(16) unsigned char widen_smem[];                 // rings of y | a block of u | one as operand | its rows' factors
+__global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constant__ WidenParams P) {
+    using W = Widen<R16, VEC>;
+    using O = Operand<R16>;
+    constexpr int kTiles = W::kTiles, G = W::kGroups;
+    extern __shared__ __align__(16) unsigned char widen_smem[];                 // rings of y | a block of u | the same as operand | its rows' factors
+    uint4* ring = reinterpret_cast<uint4*>(widen_smem);
     float* u_block = reinterpret_cast<float*>(widen_smem + W::kRingBytes);
     uint4* us = reinterpret_cast<uint4*>(widen_smem + W::kRingBytes + W::kUBytes);
-    float* backs = reinterpret_cast<float*>(us + kWidenRows * kStride);
+    float* backs = reinterpret_cast<float*>(us + O::pieces(kWidenRows));
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
-    uint4* ring = reinterpret_cast<uint4*>(widen_smem) + warp * (W::kRing * 2 * 32) + lane;
     const WidenLayer& L = P.layer[blockIdx.z];
-    const int col0 = blockIdx.x * kWidenCols + warp * 32, m_all = L.m, rank = L.rank;
+    const int col0 = blockIdx.x * W::kCols + warp * (32 * G), m_all = L.m, rank = L.rank, batch = P.batch;
     const int first_row = (int)blockIdx.y * P.blocks * kWidenRows;
-    const int blocks = min(P.blocks, (P.batch - first_row + kWidenRows - 1) / kWidenRows);
+    const int blocks = min(P.blocks, (batch - first_row + kWidenRows - 1) / kWidenRows);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if ((int)blockIdx.x * kWidenCols >= m_all) return;
+    if ((int)blockIdx.x * W::kCols >= m_all) return;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const bool fours = rank % 4 == 0;
-    const int c = col0 + 8 * tq;                                                // the lane's columns in y
+    const int c = col0 + 8 * tq;                                                // the lane's columns in y: 8 here and 8 in each further group
+    ring += warp * W::kBlockPieces + lane;
+    __half* y = L.y + (size_t)(first_row + gq) * m_all + c;                     // the lane's part of row gq of the block at hand
+    const size_t eight = (size_t)8 * m_all;
     // u of a block and the lane's part of y of the same rows: one group of copies
-    auto fetch = [&](int blk) {
+    auto fetch = [&](int blk, const __half* from) {
         const int row0 = first_row + blk * kWidenRows;
         if (blk < blocks) {
+            uint4* dst = ring + (blk & 1) * (kWarps * W::kBlockPieces);
 #pragma unroll
-            for (int mt = 0; mt < kTiles; ++mt)
+            for (int t = 0; t < 2 * kTiles; ++t) {
+                const bool row_in = row0 + 8 * t + gq < batch;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int r = row0 + 16 * mt + 8 * h + gq;
-                    const bool in = r < P.batch && c < m_all;
-                    const __half* src = in ? L.y + (size_t)r * m_all + c : L.y;
-                    uint4* dst = ring + ((blk & 1) * kTiles + mt) * 64 + h * 32;
-                    if (VEC) copy_async_16(dst, src, in);
-                    else *dst = load_8<false>(src, in ? m_all - c : 0);
+                for (int g = 0; g < G; ++g) {
+                    const bool in = row_in && c + 32 * g < m_all;
+                    if (VEC) copy_async_16(dst + (t * G + g) * 32, in ? from + 32 * g : L.y, in);
+                    else dst[(t * G + g) * 32] = load_8<false>(from + 32 * g, in ? m_all - c - 32 * g : 0);
                 }
-            for (int i = threadIdx.x; i < kWidenRows * (kRanks / 4); i += kThreads) {
-                const int r = i / (kRanks / 4), j = i % (kRanks / 4) * 4;
+                from += eight;
+            }
+            for (int i = threadIdx.x; i < kWidenRows * W::kFours; i += kThreads) {
+                const int r = i / W::kFours, j = i % W::kFours * 4;
                 const float* src = L.u + (size_t)(row0 + r) * rank + j;
-                const bool in = row0 + r < P.batch;
-                float* dst = u_block + 4 * i;
+                const bool in = row0 + r < batch;
+                float* to = u_block + 4 * i;
                 if (fours) {
-                    copy_async_16(dst, in && j < rank ? src : L.u, in && j < rank);
+                    copy_async_16(to, in && j < rank ? src : L.u, in && j < rank);
                 } else {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) copy_async_4(dst + q, in && j + q < rank ? src + q : L.u, in && j + q < rank);
+                    for (int q = 0; q < 4; ++q) copy_async_4(to + q, in && j + q < rank ? src + q : L.u, in && j + q < rank);
                 }
             }
         }
         copy_async_commit();
     };
-    int id[2] = {-1, -1}, next_id[2];
-    auto load_ids = [&](int (&to)[2], int blk) {
-        const int row0 = first_row + blk * kWidenRows;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int v = blk < blocks && row0 + 32 * h + lane < P.batch ? P.ids[row0 + 32 * h + lane] : -1;
-            to[h] = v < L.count ? v : -1;
-        }
+    auto load_id = [&](int blk) {
+        const int r = first_row + blk * kWidenRows + lane, v = blk < blocks && r < batch ? P.ids[r] : -1;
+        return v < L.count ? v : -1;
     };
-    auto rows_of = [&](int cur) { return __ballot_sync(0xFFFFFFFFu, id[0] == cur) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id[1] == cur) << 32); };
-    auto first_of = [&](unsigned long long left) {
-        const int at = __ffsll(left) - 1;
-        return at < 32 ? __shfl_sync(0xFFFFFFFFu, id[0], at) : __shfl_sync(0xFFFFFFFFu, id[1], at - 32);
-    };
-    uint32_t f[R16][4][2];                                                      // [16 ranks][column tile]: ranks 4 tq and 4 tq + 1, the two behind them
+    uint32_t f[R16][G][4][2];                                                   // [16 ranks][32 columns][column tile]: ranks 4 tq and 4 tq + 1, the two behind them
     auto load_factor = [&](int cur) {
-        const int cf = col0 + 8 * (gq >> 1);
         const uint32_t pick = gq & 1 ? 0x7632u : 0x5410u;
-        const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + cf;
 #pragma unroll
-        for (int k = 0; k < R16; ++k) {
-            uint4 v[4];
+        for (int g = 0; g < G; ++g) {
+            const int cf = col0 + 32 * g + 8 * (gq >> 1);
+            const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + cf;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all, 16 * k + 4 * tq + i < rank ? m_all - cf : 0);
+            for (int k = 0; k < R16; ++k) {
+                uint4 v[4];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                f[k][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
-                f[k][1][p] = __byte_perm(v[2 * p].y, v[2 * p + 1].y, pick);
-                f[k][2][p] = __byte_perm(v[2 * p].z, v[2 * p + 1].z, pick);
-                f[k][3][p] = __byte_perm(v[2 * p].w, v[2 * p + 1].w, pick);
+                for (int i = 0; i < 4; ++i) v[i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all, 16 * k + 4 * tq + i < rank ? m_all - cf : 0);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    f[k][g][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
+                    f[k][g][1][p] = __byte_perm(v[2 * p].y, v[2 * p + 1].y, pick);
+                    f[k][g][2][p] = __byte_perm(v[2 * p].z, v[2 * p + 1].z, pick);
+                    f[k][g][3][p] = __byte_perm(v[2 * p].w, v[2 * p + 1].w, pick);
+                }
             }
         }
     };
 
-    fetch(0);
-    load_ids(next_id, 0);
-    int held = -1;                                                              // the adapter whose factor the registers hold
+    fetch(0, y);
+    int next_id = load_id(0), held = -1;                                        // held: the adapter whose factor the registers hold
     for (int blk = 0; blk < blocks; ++blk) {
-        const int row0 = first_row + blk * kWidenRows;
-        id[0] = next_id[0];
-        id[1] = next_id[1];
-        const unsigned long long named = __ballot_sync(0xFFFFFFFFu, id[0] >= 0) | ((unsigned long long)__ballot_sync(0xFFFFFFFFu, id[1] >= 0) << 32);
-        int cur = named ? first_of(named) : held;
+        const int id = next_id;
+        uint32_t left = __ballot_sync(0xFFFFFFFFu, id >= 0);
+        int cur = left ? __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1) : held;
         if (cur != held) load_factor(held = cur);
-        load_ids(next_id, blk + 1);
+        next_id = load_id(blk + 1);
         copy_async_wait<0>();
         __syncthreads();                                                        // this block is there, and nobody reads the one before any more
         for (int i = threadIdx.x; i < kWidenRows * W::kFours; i += kThreads) {
-            const float back = split_row<W::kFours>(us + i / W::kFours * kStride + i % W::kFours, reinterpret_cast<const float4*>(u_block)[i]);
+            const float back = split_row<R16>(us, i / W::kFours, i % W::kFours, reinterpret_cast<const float4*>(u_block)[i]);
             if (i % W::kFours == 0) backs[i / W::kFours] = back;
         }
         __syncthreads();
-        fetch(blk + 1);
-        const uint4* old = ring + (blk & 1) * kTiles * 64;
-        for (unsigned long long left = named; left != 0ULL;) {
+        fetch(blk + 1, y + 4 * eight);
+        const uint4* old = ring + (blk & 1) * (kWarps * W::kBlockPieces);
+        while (left != 0u) {
             if (cur != held) load_factor(held = cur);
-            const unsigned long long match = rows_of(cur);
+            const uint32_t match = __ballot_sync(0xFFFFFFFFu, id == cur);
             left &= ~match;
             const float scale = L.scale[cur];
 #pragma unroll
             for (int mt = 0; mt < kTiles; ++mt) {
-                const uint32_t hits = (uint32_t)(match >> (16 * mt)) & 0xFFFFu;
+                const uint32_t hits = (match >> (16 * mt)) & 0xFFFFu;
                 if (hits == 0u) continue;
-                float acc[4][4] = {};
+                float acc[G][4][4];
 #pragma unroll
-                for (int k = 0; k < R16; ++k) widen_step(acc, us + (16 * mt + gq) * kStride + 4 * k + tq, us + (16 * mt + 8 + gq) * kStride + 4 * k + tq, f[k]);
+                for (int k = 0; k < R16; ++k) widen_step<G>(acc, k == 0, us + O::at(16 * mt + gq) + 4 * k + tq, O::kSecond, f[k]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (((hits >> (8 * h + gq)) & 1u) && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 16 * mt + 8 * h + gq) * m_all + c, m_all - c, old[mt * 64 + h * 32], acc, h, scale * backs[16 * mt + 8 * h + gq]);
+                for (int h = 0; h < 2; ++h) {
+                    if (!((hits >> (8 * h + gq)) & 1u)) continue;
+                    const float factor = scale * backs[16 * mt + 8 * h + gq];
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+                        if (c + 32 * g < m_all) widen_store<VEC>(y + (2 * mt + h) * eight + 32 * g, m_all - c - 32 * g, old[((2 * mt + h) * G + g) * 32], acc[g], h, factor);
+                }
             }
-            if (left != 0ULL) cur = first_of(left);
+            if (left != 0u) cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
         }
+        y += 4 * eight;
     }
     copy_async_wait<0>();
 }
 
 // ---- both steps in one launch, up to 64 rows -------------------------------------------------------------------
 
-// Single tokens of many requests: behind the layer, one cluster of CTAs per tile of 16 rows and adapter that occurs in it (the blockIdx.y-th; a tile has no more
-// than gridDim.y), which makes u as narrow_kernel does and adds its part to y as widen_kernel does, the CTAs taking columns in turn.  The CTAs
-// send their sums of u to one another, so one cluster barrier lies between the two; the first factor entries of the second are
-// fetched before it.  One launch instead of two around the layer saves a launch's latency and the way of u through memory.
-// Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y).
-template <int R16, bool VEC>
+// Up to 256 rows.  Behind the layer, clusters of CTAs take one adapter and up to 16 of its rows at a time: up to 64 rows (GATHER) the rows of an adapter are put
+// together wherever they stand, the items being found by one match over the batch; beyond that, where rows come as prompts, a cluster stays with 16
+// neighbouring rows and the adapters among them.  A cluster makes u of the rows as narrow_kernel does and adds their part to y as widen_kernel does, the
+// CTAs taking columns in turn.  The CTAs send their sums of u to one another, so one cluster barrier lies between the two steps; the factor's first entries
+// and y of the second are fetched before it.  One launch instead of two around the layer saves a launch's latency and the way of u through memory.
+// Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y): few instructions on the way count, not bytes.
+constexpr int kGatherRows = 64;
+template <int R16>
+struct Decode {
+    static constexpr int kRows = 16, kRanks = 16 * R16, kCluster = R16 == 8 ? 8 : 16;   // (most CTAs of a cluster)
+    static constexpr int kBytes = (kWarps + kCluster) * kRows * kRanks * 4 + Operand<R16>::pieces(kRows) * 16 + kRows * 4 + kWarps * kRows * 4;
+    static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
+};
+template <int R16, bool VEC, bool GATHER>
 __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(const __grid_constant__ DecodeParams P) {
-    constexpr int kRows = kNarrowRows, kRanks = 16 * R16, NR = 2 * R16, kFours = kRanks / 4, kStride = kFours + 1;
-    extern __shared__ __align__(16) float decode_smem[];
-    float* red = decode_smem;                                                   // [kWarps][kRows][kRanks]: the warps' sums
-    float* inbox = red + kWarps * kRows * kRanks;                               // [kMaxCluster][kRows][kRanks]: the CTAs' sums
-    uint4* us = reinterpret_cast<uint4*>(inbox + kMaxCluster * kRows * kRanks); // [kRows][kStride]: u as operand, then its rows' factors
-    float* backs = reinterpret_cast<float*>(us + kRows * kStride);
+    using D = Decode<R16>;
+    using O = Operand<R16>;
+    constexpr int kRows = D::kRows, kRanks = D::kRanks, NR = 2 * R16;
+    constexpr uint32_t kAll = 0xFFFFFFFFu;
+    extern __shared__ __align__(16) unsigned char decode_smem[];
+    float* red = reinterpret_cast<float*>(decode_smem);                         // [kWarps][kRows][kRanks]: the warps' sums
+    float* inbox = red + kWarps * kRows * kRanks;                               // [kCluster][kRows][kRanks]: the CTAs' sums
+    uint4* us = reinterpret_cast<uint4*>(inbox + D::kCluster * kRows * kRanks); // u as operand, then its rows' factors
+    float* backs = reinterpret_cast<float*>(us + O::pieces(kRows));
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
+    int* rows = reinterpret_cast<int*>(backs + kRows) + warp * kRows;           // the rows at hand (-1: none), every warp for itself
     const DecodeLayer& L = P.layer[blockIdx.z];
-    const int row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, m_all = L.m, rank = L.rank;
+    const int n = L.n, m_all = L.m, rank = L.rank, batch = P.batch;
+    const int groups = (m_all + 31) / 32, step = parts * kWarps;                // of 32 columns
+    const uint32_t pick = gq & 1 ? 0x7632u : 0x5410u, before = (1u << lane) - 1u;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int id = lane < kRows && row0 + lane < P.batch ? P.ids[row0 + lane] : -1;
+    // GATHER: row `lane` and row 32 + lane of the batch; otherwise row `lane` of the cluster's 16
+    const int row0 = GATHER ? 0 : (int)(blockIdx.x / parts) * kRows;
+    int id = lane < (GATHER ? 32 : kRows) && row0 + lane < batch ? P.ids[row0 + lane] : -1, id1 = GATHER && 32 + lane < batch ? P.ids[32 + lane] : -1;
     if (id >= L.count) id = -1;
-    uint32_t left = __ballot_sync(0xFFFFFFFFu, id >= 0);
-    if (blockIdx.y == 0 && part == 0) {                                         // rows without adapter: u is zero
-        const uint32_t bare = ~left;
-        for (int e = threadIdx.x; e < kRows * rank; e += kThreads)
-            if (row0 + e / rank < P.batch && ((bare >> (e / rank)) & 1u)) L.u[(size_t)row0 * rank + e] = 0.f;
+    if (id1 >= L.count) id1 = -1;
+    uint32_t same = __match_any_sync(kAll, id), same1 = 0u;                     // rows of the same adapter: in the first 32, in the second
+    bool leads = id >= 0 && (same & before) == 0u, leads1 = false;              // the adapter's first row
+    uint32_t same_of1 = 0u, same1_of1 = 0u;
+    if (GATHER && batch > 32) {
+        same1_of1 = __match_any_sync(kAll, id1);
+        for (int q = 0; q < 32; ++q) {
+            if (__shfl_sync(kAll, id1, q) == id) same1 |= 1u << q;
+            if (__shfl_sync(kAll, id, q) == id1) same_of1 |= 1u << q;
+        }
+        leads1 = id1 >= 0 && same_of1 == 0u && (same1_of1 & before) == 0u;
     }
-    uint32_t match = 0u;
-    int cur = -1;
-    for (int turn = 0; left != 0u && turn <= (int)blockIdx.y; ++turn) {
-        cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
-        match = __ballot_sync(0xFFFFFFFFu, id == cur);
-        left &= ~match;
-        if (turn < (int)blockIdx.y) match = 0u;
+    // items: 16 rows of an adapter each, in the order of the adapters' first rows
+    int items = leads ? (__popc(same) + __popc(same1) + kRows - 1) / kRows : 0, items1 = leads1 ? (__popc(same1_of1) + kRows - 1) / kRows : 0;
+    int end = items, end1 = items1;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(kAll, end, d), v1 = __shfl_up_sync(kAll, end1, d);
+        if (lane >= d) { end += v; end1 += v1; }
     }
-    if (match == 0u) return;                                                    // fewer adapters than clusters (the whole cluster agrees)
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // (all CTAs of the cluster run before any writes to another's memory)
-    const float scale = L.scale[cur];
-    const bool has[2] = {(match >> gq & 1u) != 0u, (match >> (8 + gq) & 1u) != 0u};
+    const int total0 = __shfl_sync(kAll, end, 31), total = total0 + __shfl_sync(kAll, end1, 31);
+    end1 += total0;
+    if ((int)blockIdx.y < total) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (all CTAs of the cluster run before any writes to another's memory)
+    for (int turn = blockIdx.y; turn < total; turn += (int)gridDim.y) {
+        const uint32_t at = __ballot_sync(kAll, turn >= end - items && turn < end), at1 = __ballot_sync(kAll, turn >= end1 - items1 && turn < end1);
+        const int who = __ffs(at ? at : at1) - 1;
+        const int cur = __shfl_sync(kAll, at ? id : id1, who), skip = (turn - __shfl_sync(kAll, at ? end - items : end1 - items1, who)) * kRows;
+        const uint32_t mask = __shfl_sync(kAll, at ? same : 0u, who), mask1 = __shfl_sync(kAll, at ? same1 : same1_of1, who);
+        __syncwarp();
+        if (lane < kRows) rows[lane] = -1;
+        __syncwarp();
+        const int place = __popc(mask & before) - skip, place1 = __popc(mask) + __popc(mask1 & before) - skip;
+        if ((mask >> lane & 1u) && place >= 0 && place < kRows) rows[place] = row0 + lane;
+        if ((mask1 >> lane & 1u) && place1 >= 0 && place1 < kRows) rows[place1] = 32 + lane;
+        __syncwarp();
+        const bool has[2] = {rows[gq] >= 0, rows[8 + gq] >= 0};
+        const size_t row[2] = {(size_t)max(rows[gq], 0), (size_t)max(rows[8 + gq], 0)};
+        const float scale = L.scale[cur];
 
-    float acc[NR][4] = {};
-    {
-        const int units = n / 32, worker = part * kWarps + warp, workers = parts * kWarps;
-        const int u0 = (int)((long long)units * worker / workers), u1 = (int)((long long)units * (worker + 1) / workers);
-        const __half* a = L.a + ((size_t)cur * rank + gq) * n + 8 * tq;
-        const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
-        struct Loads {
-            uint4 x[2], a[NR];
-        };
-        auto load = [&](Loads& l, int u) {
-            const bool in = u < u1;
-            const size_t col = (size_t)u * 32;
+        float acc[NR][4] = {};
+        {
+            const int units = n / 32, worker = part * kWarps + warp, workers = parts * kWarps;
+            const int u0 = (int)((long long)units * worker / workers), u1 = (int)((long long)units * (worker + 1) / workers);
+            const __half* a = L.a + ((size_t)cur * rank + gq) * n + 8 * tq;
+            const __half* x[2] = {L.x + row[0] * n + 8 * tq, L.x + row[1] * n + 8 * tq};
+            struct Loads {
+                uint4 x[2], a[NR];
+            };
+            auto load = [&](Loads& l, int u) {
+                const bool in = u < u1;
+                const size_t col = (size_t)u * 32;
 #pragma unroll
-            for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m) * n + col) : make_uint4(0u, 0u, 0u, 0u);
+                for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? *reinterpret_cast<const uint4*>(x[m] + col) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-            for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
-        };
-        auto multiply = [&](const Loads& l) {
-#pragma unroll
-            for (int j = 0; j < NR; ++j) {
-                mma_f16(acc[j], l.x[0].x, l.x[1].x, l.x[0].y, l.x[1].y, l.a[j].x, l.a[j].y);
-                mma_f16(acc[j], l.x[0].z, l.x[1].z, l.x[0].w, l.x[1].w, l.a[j].z, l.a[j].w);
-            }
-        };
-        float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;       // the lane's sums: rows gq and gq + 8, ranks 8 j + 2 tq and the next
-        auto flush = [&](bool first) {                                          // (the tensor core truncates: chains of at most 16 MMAs)
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
+                for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
+            };
+            auto multiply = [&](const Loads& l) {
 #pragma unroll
                 for (int j = 0; j < NR; ++j) {
-                    float2* at = reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j);
-                    float2 v = make_float2(acc[j][2 * m], acc[j][2 * m + 1]);
-                    if (!first) {
-                        const float2 old = *at;
-                        v.x += old.x;
-                        v.y += old.y;
-                    }
-                    *at = v;
-                    acc[j][2 * m] = acc[j][2 * m + 1] = 0.f;
+                    mma_f16(acc[j], l.x[0].x, l.x[1].x, l.x[0].y, l.x[1].y, l.a[j].x, l.a[j].y);
+                    mma_f16(acc[j], l.x[0].z, l.x[1].z, l.x[0].w, l.x[1].w, l.a[j].z, l.a[j].w);
                 }
-        };
-        Loads even, odd;
-        load(even, u0);
-        int pairs = 0;
+            };
+            float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;   // the lane's sums: rows gq and gq + 8, ranks 8 j + 2 tq and the next
+            auto flush = [&](bool first) {                                  // (the tensor core truncates: chains of at most 16 MMAs)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int j = 0; j < NR; ++j) {
+                        float2* at = reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j);
+                        float2 v = make_float2(acc[j][2 * m], acc[j][2 * m + 1]);
+                        if (!first) {
+                            const float2 old = *at;
+                            v.x += old.x;
+                            v.y += old.y;
+                        }
+                        *at = v;
+                        acc[j][2 * m] = acc[j][2 * m + 1] = 0.f;
+                    }
+            };
+            Loads even, odd;
+            load(even, u0);
+            int pairs = 0;
 #pragma unroll 1
-        for (int u = u0; u < u1; u += 2) {
-            load(odd, u + 1);
-            multiply(even);
-            load(even, u + 2);
-            multiply(odd);
-            if (++pairs % 4 == 0) flush(pairs == 4);
-        }
-        if (pairs % 4 != 0 || pairs == 0) flush(pairs < 4);
-    }
-
-    // the second factor's entries of the warp's first 32 columns are on their way while u is put together
-    const int groups = (m_all + 31) / 32, step = parts * kWarps;
-    int g = warp * parts + part;                                                // neighbouring columns to different SMs
-    const uint32_t pick = gq & 1 ? 0x7632u : 0x5410u;
-    const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + 8 * (gq >> 1);
-    uint4 raw[R16][4];
-    auto load_factor = [&](int g) {
-        const int cf = 32 * g + 8 * (gq >> 1);
-#pragma unroll
-        for (int k = 0; k < R16; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) raw[k][i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all + 32 * g, g < groups && 16 * k + 4 * tq + i < rank ? m_all - cf : 0);
-    };
-    load_factor(g);
-    __syncthreads();
-    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-    for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
-        float4 s = reinterpret_cast<const float4*>(red)[e];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) {
-            const float4 v = reinterpret_cast<const float4*>(red)[w * (kRows * kRanks / 4) + e];
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-#pragma unroll
-        for (int q = 0; q < kMaxCluster; ++q)
-            if (q < parts) reinterpret_cast<float4*>(cluster.map_shared_rank(inbox, q))[part * (kRows * kRanks / 4) + e] = s;
-    }
-    cluster.sync();                                                             // (nobody writes to another's memory behind it)
-    for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
-        float4 s = reinterpret_cast<const float4*>(inbox)[e];
-        for (int q = 1; q < parts; ++q) {
-            const float4 v = reinterpret_cast<const float4*>(inbox)[q * (kRows * kRanks / 4) + e];
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        const int row = e / (kRanks / 4), j = e % (kRanks / 4) * 4;
-        const float back = split_row<kFours>(us + row * kStride + j / 4, s);
-        if (j == 0) backs[row] = back;
-        if (part == 0 && j < rank && ((match >> row) & 1u)) store_4(L.u + (size_t)(row0 + row) * rank + j, s, rank - j, rank % 4 == 0);
-    }
-    __syncthreads();
-
-    uint32_t f[R16][4][2];
-    uint4 old[2];
-    for (; g < groups; g += step) {
-        const int c = 32 * g + 8 * tq;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) old[h] = load_8<VEC>(L.y + (size_t)(row0 + 8 * h + gq) * m_all + c, has[h] ? m_all - c : 0);
-#pragma unroll
-        for (int k = 0; k < R16; ++k)
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                f[k][0][p] = __byte_perm(raw[k][2 * p].x, raw[k][2 * p + 1].x, pick);
-                f[k][1][p] = __byte_perm(raw[k][2 * p].y, raw[k][2 * p + 1].y, pick);
-                f[k][2][p] = __byte_perm(raw[k][2 * p].z, raw[k][2 * p + 1].z, pick);
-                f[k][3][p] = __byte_perm(raw[k][2 * p].w, raw[k][2 * p + 1].w, pick);
+            for (int u = u0; u < u1; u += 2) {
+                load(odd, u + 1);
+                multiply(even);
+                load(even, u + 2);
+                multiply(odd);
+                if (++pairs % 4 == 0) flush(pairs == 4);
             }
-        load_factor(g + step);
-        float sum[4][4] = {};
+            if (pairs % 4 != 0 || pairs == 0) flush(pairs < 4);
+        }
+
+        // the second factor's entries and y of the warp's first 32 columns are on their way while u is put together
+        const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + 8 * (gq >> 1);
+        __half* y[2] = {L.y + row[0] * m_all + 8 * tq, L.y + row[1] * m_all + 8 * tq};
+        int g = warp * parts + part;                                        // neighbouring columns to different SMs
+        uint4 raw[R16][4], ahead[2];
+        auto load_columns = [&](int g) {
+            const int in_b = g < groups ? m_all - 32 * g - 8 * (gq >> 1) : 0, in_y = g < groups ? m_all - 32 * g - 8 * tq : 0;
 #pragma unroll
-        for (int k = 0; k < R16; ++k) widen_step(sum, us + gq * kStride + 4 * k + tq, us + (8 + gq) * kStride + 4 * k + tq, f[k]);
+            for (int k = 0; k < R16; ++k)
 #pragma unroll
+                for (int i = 0; i < 4; ++i) raw[k][i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all + 32 * g, 16 * k + 4 * tq + i < rank ? in_b : 0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) ahead[h] = load_8<VEC>(y[h] + 32 * g, has[h] ? in_y : 0);
+        };
+        load_columns(g);
+        __syncthreads();
+        cluster_wait();
+        for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
+            float4 s = reinterpret_cast<const float4*>(red)[e];
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) {
+                const float4 v = reinterpret_cast<const float4*>(red)[w * (kRows * kRanks / 4) + e];
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+#pragma unroll 4
+            for (int q = 0; q < D::kCluster; ++q)
+                if (q < parts) reinterpret_cast<float4*>(cluster.map_shared_rank(inbox, q))[part * (kRows * kRanks / 4) + e] = s;
+        }
+        cluster.sync();
+        for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
+            float4 s = reinterpret_cast<const float4*>(inbox)[e];
+            for (int q = 1; q < parts; ++q) {
+                const float4 v = reinterpret_cast<const float4*>(inbox)[q * (kRows * kRanks / 4) + e];
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            const int r = e / (kRanks / 4), j = e % (kRanks / 4) * 4;
+            const float back = split_row<R16>(us, r, j / 4, s);
+            if (j == 0) backs[r] = back;
+            if (part == 0 && j < rank && rows[r] >= 0) store_4(L.u + (size_t)rows[r] * rank + j, s, rank - j, rank % 4 == 0);
+        }
+        __syncthreads();
+        if (turn + (int)gridDim.y < total) cluster_arrive();                // the inbox has been read: sums of the next item may come
+
+        for (; g < groups; g += step) {
+            uint32_t f[R16][1][4][2];
+#pragma unroll
+            for (int k = 0; k < R16; ++k)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    f[k][0][0][p] = __byte_perm(raw[k][2 * p].x, raw[k][2 * p + 1].x, pick);
+                    f[k][0][1][p] = __byte_perm(raw[k][2 * p].y, raw[k][2 * p + 1].y, pick);
+                    f[k][0][2][p] = __byte_perm(raw[k][2 * p].z, raw[k][2 * p + 1].z, pick);
+                    f[k][0][3][p] = __byte_perm(raw[k][2 * p].w, raw[k][2 * p + 1].w, pick);
+                }
+            const uint4 old[2] = {ahead[0], ahead[1]};
+            load_columns(g + step);
+            float sum[1][4][4];
+#pragma unroll
+            for (int k = 0; k < R16; ++k) widen_step<1>(sum, k == 0, us + O::at(gq) + 4 * k + tq, O::kSecond, f[k]);
+            const int left_cols = m_all - 32 * g - 8 * tq;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (has[h] && left_cols > 0) widen_store<VEC>(y[h] + 32 * g, left_cols, old[h], sum[0], h, scale * backs[8 * h + gq]);
+        }
+    }
+    if (blockIdx.y == 0 && part == 0) {                                         // rows without adapter: u is zero
+        uint32_t bare[2] = {__ballot_sync(kAll, id < 0 && lane < (GATHER ? 32 : kRows) && row0 + lane < batch), __ballot_sync(kAll, GATHER && id1 < 0 && 32 + lane < batch)};
+        int turn = 0;
         for (int h = 0; h < 2; ++h)
-            if (has[h] && c < m_all) widen_store<VEC>(L.y + (size_t)(row0 + 8 * h + gq) * m_all + c, m_all - c, old[h], sum, h, scale * backs[8 * h + gq]);
+            for (; bare[h] != 0u; bare[h] &= bare[h] - 1u)
+                if (turn++ % kWarps == warp)
+                    for (int j = lane; j < rank; j += 32) L.u[(size_t)(row0 + 32 * h + __ffs(bare[h]) - 1) * rank + j] = 0.f;
     }
 }
 
@@ -772,16 +847,17 @@ struct FactorParams {
     const float* scale;
     int batch, rank, accumulate;
 };
-constexpr int kFactorRows = 32, kFactorList = 1024, kFactorChunk = 64;
+constexpr int kFactorThreads = 512, kFactorWarps = kFactorThreads / 32, kFactorList = 1024, kFactorChunk = 64;
 
 template <int GROUPS>
-struct Factor {                                                                 // GROUPS * 16 ranks by COLS * 64 columns, HALVES groups of warps for the halves of a tile's rows
-    static constexpr int kRanks = 16 * GROUPS, kHalves = GROUPS == 1 ? 2 : 1, kColWarps = kWarps / (GROUPS * kHalves), kCols = 64 * kColWarps;
-    static constexpr int kVStride = kCols * 2 + 16, kLowStride = kRanks + 8, kAStride = kFactorRows * 2 + 16;   // bytes, words, bytes: rows that are read together meet in no bank
-    static constexpr int kVBytes = kFactorRows * kVStride, kStageBytes = kVBytes + kFactorRows * kLowStride * 4;
-    static constexpr int kStages = GROUPS == 8 ? 3 : 4, kABytes = kRanks * kAStride;
+struct Factor {                                                                 // GROUPS warps side by side for the ranks, kColWarps for the columns, kSlices for the rows of a tile
+    static constexpr int kRanks = 16 * GROUPS, kRows = GROUPS == 8 ? 32 : 64, kColWarps = GROUPS == 8 ? 2 : 4, kSlices = kFactorWarps / (GROUPS * kColWarps);
+    static constexpr int kCols = 64 * kColWarps, kSteps = kRows / 16 / kSlices; // MMAs of 16 rows of a warp in a tile
+    static constexpr int kVStride = kCols * 2 + 16, kLowStride = kRanks + 4, kAStride = kRows * 2 + 16;         // bytes, words, bytes: rows that are read together meet in few banks
+    static constexpr int kVBytes = kRows * kVStride, kStageBytes = kVBytes + kRows * kLowStride * 4;
+    static constexpr int kStages = GROUPS == 8 ? 4 : 3, kABytes = kRanks * kAStride;
     static constexpr int kAAt = kStages * kStageBytes, kBackAt = kAAt + 4 * kABytes, kListAt = kBackAt + 2 * kRanks * 4, kBytes = kListAt + kFactorList * 4;
-    static_assert(kHalves * kRanks * kCols * 4 <= kBytes && 2 * (kBytes + 1024 + 128) <= 228 * 1024, "the sums fit, two CTAs per SM");
+    static_assert(kSteps >= 1 && kSlices * kRanks * kCols * 4 <= kBytes && kBytes <= 226 * 1024, "the sums fit, one CTA per SM");
 };
 __device__ __forceinline__ void ldmatrix(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -790,21 +866,22 @@ __device__ __forceinline__ void ldmatrix_trans(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
 
-// Ranks by columns as m16n8k16 MMAs over the rows, v as it is, low as two fp16 parts of a power of two per rank and tile of 32 rows (v and low meet as matrices
-// with the rows inside, so low is turned when it is split).  A warp takes 16 ranks and 64 columns, GROUPS warps the same columns.  The rows of a
+// Ranks by columns as m16n8k16 MMAs over the rows, v as it is, low as two fp16 parts of a power of two per rank and tile of 64 rows (v and low meet as matrices
+// with the rows inside, so low is turned when it is split).  A warp takes 16 ranks and 64 columns, GROUPS warps the same columns; 16 warps, because what a
+// tile costs beside its MMAs (copies, splitting, barriers) is then shared by 256 columns.  The rows of a
 // cluster's adapter are dealt out to its CTAs in chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor
 // multiplied by zero (0 * NaN), then streams them through a ring of stages; the next tile is split beside the MMAs of the one at hand.
-// Sums of 32 rows are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
+// Sums of a tile are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
 // Bound: v from memory; from rank 64 on the MMAs.
 template <int GROUPS, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_constant__ FactorParams P) {
+__global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_constant__ FactorParams P) {
     using F = Factor<GROUPS>;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int counts[kWarps];
+    __shared__ int counts[kFactorWarps];
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
-    const int group = warp % GROUPS, wc = warp / GROUPS % F::kColWarps, half = warp / (GROUPS * F::kColWarps);
+    const int group = warp % GROUPS, wc = warp / GROUPS % F::kColWarps, slice = warp / (GROUPS * F::kColWarps);
     int block = (int)blockIdx.x / parts;
     const FactorSide& S = P.s[block < P.s[0].blocks ? 0 : 1];
     if (block >= P.s[0].blocks) block -= P.s[0].blocks;
@@ -816,11 +893,12 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
     // the lane's row of the 8 x 8 matrices that it names: of v rows of the tile by columns, of low ranks by rows of the tile
     const uint32_t v_at = smem32 + (uint32_t)((lane & 15) * F::kVStride + (wc * 64 + (lane >> 4) * 8) * 2);
     const uint32_t a_at = smem32 + (uint32_t)(F::kAAt + (group * 16 + (lane & 15)) * F::kAStride + (lane >> 4) * 16);
+    const bool split_first = (warp & 4) != 0;                                   // half of a scheduler's warps split while the others multiply
     float sum[8][4] = {};
     for (long long base = 0; base < P.batch; base += (long long)kFactorList * parts) {
         // the rows of this round that are the adapter's, in order
         int n_list = 0;
-        for (int at = 0; at < kFactorList; at += kThreads) {
+        for (int at = 0; at < kFactorList; at += kFactorThreads) {
             const int pos = at + (int)threadIdx.x;
             const long long t = base + ((long long)(pos / kFactorChunk) * parts + part) * kFactorChunk + pos % kFactorChunk;
             if (base + (long long)(at / kFactorChunk) * parts * kFactorChunk >= P.batch) break;
@@ -829,21 +907,21 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
             if (lane == 0) counts[warp] = __popc(hits);
             __syncthreads();
             int before = n_list;
-            for (int w = 0; w < kWarps; ++w) {
+            for (int w = 0; w < kFactorWarps; ++w) {
                 if (w < warp) before += counts[w];
                 n_list += counts[w];
             }
             if (hit) list[before + __popc(hits & ((1u << lane) - 1u))] = (int)t;
             __syncthreads();
         }
-        const int n_tiles = (n_list + kFactorRows - 1) / kFactorRows;
+        const int n_tiles = (n_list + F::kRows - 1) / F::kRows;
         auto fetch = [&](int tile) {
             unsigned char* stage = smem + tile % F::kStages * F::kStageBytes;
             if (tile < n_tiles) {
                 constexpr int kPieces = F::kCols / 8;                           // 16 bytes of a row each
 #pragma unroll
-                for (int i0 = 0; i0 < kFactorRows * kPieces; i0 += kThreads) {
-                    const int i = i0 + (int)threadIdx.x, r = i / kPieces, col = first + i % kPieces * 8, at = tile * kFactorRows + r;
+                for (int i0 = 0; i0 < F::kRows * kPieces; i0 += kFactorThreads) {
+                    const int i = i0 + (int)threadIdx.x, r = i / kPieces, col = first + i % kPieces * 8, at = tile * F::kRows + r;
                     const bool in = at < n_list && col < side;
                     const __half* src = in ? S.v + (size_t)list[at] * side + col : S.v;
                     unsigned char* dst = stage + r * F::kVStride + i % kPieces * 16;
@@ -852,8 +930,8 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
                 }
                 float* low = reinterpret_cast<float*>(stage + F::kVBytes);
                 constexpr int kFours = F::kRanks / 4;
-                for (int i = threadIdx.x; i < kFactorRows * kFours; i += kThreads) {
-                    const int r = i / kFours, j = i % kFours * 4, at = tile * kFactorRows + r;
+                for (int i = threadIdx.x; i < F::kRows * kFours; i += kFactorThreads) {
+                    const int r = i / kFours, j = i % kFours * 4, at = tile * F::kRows + r;
                     const bool in = at < n_list;
                     const float* src = in ? S.low + (size_t)list[at] * rank + j : S.low;
                     float* dst = low + r * F::kLowStride + j;
@@ -867,34 +945,26 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
             }
             copy_async_commit();
         };
-        // low of a tile as operand: kThreads / kRanks neighbouring lanes share a rank's 32 rows, two neighbouring rows at a time
+        // low of a tile as operand: neighbouring lanes share a rank's rows
         auto split = [&](int tile) {
             if (tile >= n_tiles) return;
-            constexpr int kShare = kThreads / F::kRanks, kPairs = kFactorRows / 2 / kShare;
+            constexpr int kShare = kFactorThreads / F::kRanks, kEach = F::kRows / kShare;
             const float* low = reinterpret_cast<const float*>(smem + tile % F::kStages * F::kStageBytes + F::kVBytes);
             const int j = threadIdx.x / kShare, sub = threadIdx.x % kShare;
-            float v[kPairs][2], largest = 0.f;
+            float v[kEach], largest = 0.f;
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    v[i][e] = low[(2 * (sub + kShare * i) + e) * F::kLowStride + j];
-                    largest = fmaxf(largest, finite_size(v[i][e]));
-                }
+            for (int i = 0; i < kEach; ++i) {
+                v[i] = low[(sub + kShare * i) * F::kLowStride + j];
+                largest = fmaxf(largest, finite_size(v[i]));
+            }
 #pragma unroll
             for (int d = 1; d < kShare; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
             float to, back;
             range_of(largest, to, back);
             if (sub == 0) backs[(tile & 1) * F::kRanks + j] = back;
-            unsigned char* out = smem + F::kAAt + (tile & 1) * 2 * F::kABytes + j * F::kAStride;
+            __half* out = reinterpret_cast<__half*>(smem + F::kAAt + (tile & 1) * 2 * F::kABytes + j * F::kAStride) + sub;
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                __half h[2], l[2];
-                split_f16(v[i][0], to, h[0], l[0]);
-                split_f16(v[i][1], to, h[1], l[1]);
-                *reinterpret_cast<__half2*>(out + (sub + kShare * i) * 4) = __halves2half2(h[0], h[1]);
-                *reinterpret_cast<__half2*>(out + F::kABytes + (sub + kShare * i) * 4) = __halves2half2(l[0], l[1]);
-            }
+            for (int i = 0; i < kEach; ++i) split_f16(v[i], to, out[kShare * i], out[F::kABytes / 2 + kShare * i]);
         };
 #pragma unroll
         for (int tile = 0; tile < F::kStages - 1; ++tile) fetch(tile);
@@ -905,50 +975,56 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
             copy_async_wait<F::kStages - 3>();
             __syncthreads();                                                    // the next tile is there, this one is split, and the slots of the one before are free
             fetch(tile + F::kStages - 1);
-            split(tile + 1);
+            if (split_first) split(tile + 1);
             const uint32_t v = v_at + (uint32_t)(tile % F::kStages * F::kStageBytes), a = a_at + (uint32_t)((tile & 1) * 2 * F::kABytes);
-            float acc[8][4] = {};
+            float acc[8][4];
 #pragma unroll
-            for (int s0 = 0; s0 < 2 / F::kHalves; ++s0) {
-                const int s = F::kHalves == 2 ? half : s0;                      // 16 rows of the tile
-                uint32_t hi[4], lo[4];
+            for (int s0 = 0; s0 < F::kSteps; ++s0) {
+                const int s = slice * F::kSteps + s0;                           // 16 rows of the tile
+                uint32_t hi[4], lo[4], b[4][4];
                 ldmatrix(hi, a + (uint32_t)(s * 32));
+#pragma unroll
+                for (int q = 0; q < 4; ++q) ldmatrix_trans(b[q], v + (uint32_t)(s * 16 * F::kVStride + q * 32));
                 ldmatrix(lo, a + (uint32_t)(F::kABytes + s * 32));
 #pragma unroll
-                for (int q = 0; q < 8; q += 2) {
-                    uint32_t b[4];
-                    ldmatrix_trans(b, v + (uint32_t)(s * 16 * F::kVStride + q * 16));
-                    mma_f16(acc[q], hi[0], hi[1], hi[2], hi[3], b[0], b[1]);
-                    mma_f16(acc[q + 1], hi[0], hi[1], hi[2], hi[3], b[2], b[3]);
-                    mma_f16(acc[q], lo[0], lo[1], lo[2], lo[3], b[0], b[1]);
-                    mma_f16(acc[q + 1], lo[0], lo[1], lo[2], lo[3], b[2], b[3]);
+                for (int q = 0; q < 8; ++q) {
+                    if (s0 == 0) mma_f16_first(acc[q], hi[0], hi[1], hi[2], hi[3], b[q >> 1][2 * (q & 1)], b[q >> 1][2 * (q & 1) + 1]);
+                    else mma_f16(acc[q], hi[0], hi[1], hi[2], hi[3], b[q >> 1][2 * (q & 1)], b[q >> 1][2 * (q & 1) + 1]);
                 }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) mma_f16(acc[q], lo[0], lo[1], lo[2], lo[3], b[q >> 1][2 * (q & 1)], b[q >> 1][2 * (q & 1) + 1]);
             }
             const float back0 = backs[(tile & 1) * F::kRanks + group * 16 + gq], back1 = backs[(tile & 1) * F::kRanks + group * 16 + 8 + gq];
 #pragma unroll
             for (int q = 0; q < 8; ++q)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[q][e] = fmaf(e < 2 ? back0 : back1, acc[q][e], sum[q][e]);
+            if (!split_first) split(tile + 1);
         }
         copy_async_wait<0>();
         __syncthreads();                                                        // (the list is written again)
     }
-    // the CTA's sums [half][rank][column of the block], then over the cluster
+    // the CTA's sums [slice][rank][column of the block], then over the cluster
     float* sums = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int q = 0; q < 8; ++q)
 #pragma unroll
         for (int e = 0; e < 4; e += 2)
-            *reinterpret_cast<float2*>(sums + (half * F::kRanks + group * 16 + gq + 4 * e) * F::kCols + wc * 64 + 8 * q + 2 * tq) = make_float2(sum[q][e], sum[q][e + 1]);
-    if (F::kHalves == 2) {
+            *reinterpret_cast<float2*>(sums + (slice * F::kRanks + group * 16 + gq + 4 * e) * F::kCols + wc * 64 + 8 * q + 2 * tq) = make_float2(sum[q][e], sum[q][e + 1]);
+    if (F::kSlices > 1) {
         __syncthreads();
-        for (int e = threadIdx.x; e < F::kRanks * F::kCols; e += kThreads) sums[e] += sums[F::kRanks * F::kCols + e];
+        for (int e = threadIdx.x; e < F::kRanks * F::kCols; e += kFactorThreads) {
+            float total = sums[e];
+#pragma unroll
+            for (int q = 1; q < F::kSlices; ++q) total += sums[q * F::kRanks * F::kCols + e];
+            sums[e] = total;
+        }
     }
     cluster.sync();
     const float scale = P.scale[adapter];
     const int cols = min(F::kCols, side - first);
     const bool side_fours = side % 4 == 0;
-    for (int e = part * kThreads + threadIdx.x; e < rank * F::kCols / 4; e += parts * kThreads) {
+    for (int e = part * kFactorThreads + threadIdx.x; e < rank * F::kCols / 4; e += parts * kFactorThreads) {
         const int j = e / (F::kCols / 4), c = e % (F::kCols / 4) * 4;
         if (c >= cols) continue;
         float4 total = cluster_sum(cluster, sums, parts, e);
@@ -973,14 +1049,18 @@ __global__ void __launch_bounds__(kThreads, 2) factor_kernel(const __grid_consta
 // ---- launches ----------------------------------------------------------------------------------------------
 
 template <typename Params>
-cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, bool dependent, const Params& P, cudaStream_t stream) {
+cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, bool dependent, const Params& P, cudaStream_t stream, int threads = kThreads) {
     if (smem > 48 * 1024) {                                                     // (an attribute of the function on the current device; setting it again is cheap)
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
     }
+    if (cluster > 8) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -1023,25 +1103,27 @@ cudaError_t launch_narrow(const NarrowParams& P, int n_layers, int max_rank, cud
          : max_rank <= 64 ? go(narrow_tile_kernel<8, 8>, Tile<8, 8>::kBytes) : go(narrow_tile_kernel<16, 8>, Tile<16, 8>::kBytes);
 }
 
-cudaError_t launch_widen(WidenParams P, int n_layers, int max_rank, int max_m, bool vec, cudaStream_t stream) {
+template <int R16, bool VEC>
+cudaError_t launch_widen(WidenParams& P, int n_layers, int max_m, cudaStream_t stream) {
     // as many row blocks to a CTA as leave two CTAs for every SM (296; one more would be a second wave)
-    const long long cols = (max_m + kWidenCols - 1) / kWidenCols, row_blocks = (P.batch + kWidenRows - 1) / kWidenRows;
+    using W = Widen<R16, VEC>;
+    const long long cols = (max_m + W::kCols - 1) / W::kCols, row_blocks = (P.batch + kWidenRows - 1) / kWidenRows;
     const long long along = std::min(std::max(296 / (cols * n_layers), 1LL), 65535LL);
     P.blocks = (int)((row_blocks + along - 1) / along);
     const dim3 grid((unsigned)cols, (unsigned)((row_blocks + P.blocks - 1) / P.blocks), (unsigned)n_layers);
-    auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, 0, bytes, true, P, stream); };
-    if (vec) return max_rank <= 16 ? go(widen_kernel<1, true>, Widen<1>::kBytes) : max_rank <= 32 ? go(widen_kernel<2, true>, Widen<2>::kBytes)
-                  : max_rank <= 64 ? go(widen_kernel<4, true>, Widen<4>::kBytes) : go(widen_kernel<8, true>, Widen<8>::kBytes);
-    return max_rank <= 16 ? go(widen_kernel<1, false>, Widen<1>::kBytes) : max_rank <= 32 ? go(widen_kernel<2, false>, Widen<2>::kBytes)
-         : max_rank <= 64 ? go(widen_kernel<4, false>, Widen<4>::kBytes) : go(widen_kernel<8, false>, Widen<8>::kBytes);
+    return launch(widen_kernel<R16, VEC>, grid, 0, W::kBytes, true, P, stream);
 }
 
-cudaError_t launch_decode(const DecodeParams& P, int n_layers, int max_rank, bool vec, cudaStream_t stream) {
-    const int tiles = (P.batch + kNarrowRows - 1) / kNarrowRows, shares = std::min(P.batch, kNarrowRows);
-    const dim3 grid((unsigned)(tiles * kMaxCluster), (unsigned)shares, (unsigned)n_layers);
-    auto go = [&](auto kernel, int r16) { return launch(kernel, grid, kMaxCluster, ((kWarps + kMaxCluster) * 16 * r16 * 4 + (4 * r16 + 1) * 16 + 4) * kNarrowRows, true, P, stream); };
-    if (vec) return max_rank <= 16 ? go(decode_kernel<1, true>, 1) : max_rank <= 32 ? go(decode_kernel<2, true>, 2) : max_rank <= 64 ? go(decode_kernel<4, true>, 4) : go(decode_kernel<8, true>, 8);
-    return max_rank <= 16 ? go(decode_kernel<1, false>, 1) : max_rank <= 32 ? go(decode_kernel<2, false>, 2) : max_rank <= 64 ? go(decode_kernel<4, false>, 4) : go(decode_kernel<8, false>, 8);
+template <int R16, bool VEC>
+cudaError_t launch_decode(const DecodeParams& P, int n_layers, int max_count, cudaStream_t stream) {
+    // up to 64 rows an item for every adapter that they can name, and one for every 16 rows beyond that; more rows are prompts, with few adapters to 16 of
+    // them.  Clusters as large as leave about three CTAs to an SM, of which those without an item end at once.
+    const bool gather = P.batch <= kGatherRows;
+    const int items = gather ? std::min(P.batch, max_count) + P.batch / 16 : (P.batch + 15) / 16 * 4;
+    int c = Decode<R16>::kCluster;
+    while (c > 2 && (long long)items * n_layers * c > 444) c /= 2;
+    const dim3 grid((unsigned)(gather ? c : items / 4 * c), (unsigned)(gather ? items : 4), (unsigned)n_layers);
+    return gather ? launch(decode_kernel<R16, VEC, true>, grid, c, Decode<R16>::kBytes, true, P, stream) : launch(decode_kernel<R16, VEC, false>, grid, c, Decode<R16>::kBytes, true, P, stream);
 }
 
 template <int GROUPS>
@@ -1050,10 +1132,16 @@ cudaError_t launch_factor(FactorParams& P, int count, cudaStream_t stream) {
     for (FactorSide& s : P.s) s.blocks = (s.side + F::kCols - 1) / F::kCols;
     const bool vec = P.s[0].side % 8 == 0 && P.s[1].side % 8 == 0;
     const long long blocks = (long long)P.s[0].blocks + P.s[1].blocks;
-    int c = cluster_for(blocks * count);
-    while (c > 1 && (P.batch + kFactorChunk - 1) / kFactorChunk < c) c /= 2;    // (a CTA without rows would only take part in the sum)
+    // the cluster whose waves of one CTA per SM take least; what a CTA does before and after its tiles takes as long as about five of them
+    const long long tiles = (P.batch + F::kRows - 1) / F::kRows;
+    int c = 1;
+    double least = 1e300;
+    for (int q = 1; q <= kMaxCluster && q <= tiles; ++q) {
+        const double cost = (double)((blocks * count * q + 147) / 148) * (5.0 + (double)((tiles + q - 1) / q) / count);
+        if (cost < least) { least = cost; c = q; }
+    }
     const dim3 grid((unsigned)(blocks * c), (unsigned)count);
-    return vec ? launch(factor_kernel<GROUPS, true>, grid, c, F::kBytes, false, P, stream) : launch(factor_kernel<GROUPS, false>, grid, c, F::kBytes, false, P, stream);
+    return vec ? launch(factor_kernel<GROUPS, true>, grid, c, F::kBytes, false, P, stream, kFactorThreads) : launch(factor_kernel<GROUPS, false>, grid, c, F::kBytes, false, P, stream, kFactorThreads);
 }
 
 int check_pool(const char* who, const rabit_adapters* A) {
@@ -1142,8 +1230,11 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         return e;
     };
     if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
+    bool vec = true;
+    for (int l = 0; l < n_layers; ++l) vec = vec && (!adapters[l] || adapters[l]->n_out % 8 == 0);
+    const bool decode = batch <= (vec ? kDecodeRows : kDecodeRowsOdd);
     cudaError_t e = cudaSuccess;
-    if (batch > kDecodeRows) {
+    if (!decode) {
         e = each_group([&] {
             NarrowParams P{};
             P.ids = ids;
@@ -1165,17 +1256,23 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         WidenParams P{};
         P.ids = D.ids = ids;
         P.batch = D.batch = batch;
-        int max_rank = 0, max_m = 0;
-        bool vec = true;
+        int max_rank = 0, max_m = 0, max_count = 0;
         for (int i = 0; i < n; ++i) {
             const rabit_adapters* A = adapters[at[i]];
             P.layer[i] = WidenLayer{(const __half*)A->b, us[at[i]], A->scale, (__half*)ys[at[i]], A->n_out, A->rank, A->count};
             D.layer[i] = DecodeLayer{(const __half*)xs[at[i]], (const __half*)A->a, (const __half*)A->b, A->scale, us[at[i]], (__half*)ys[at[i]], A->n_in, A->n_out, A->rank, A->count};
             max_rank = std::max(max_rank, A->rank);
             max_m = std::max(max_m, A->n_out);
-            vec = vec && A->n_out % 8 == 0;
+            max_count = std::max(max_count, A->count);
         }
-        return batch > kDecodeRows ? launch_widen(P, n, max_rank, max_m, vec, st) : launch_decode(D, n, max_rank, vec, st);
+        if (decode && vec) return max_rank <= 16 ? launch_decode<1, true>(D, n, max_count, st) : max_rank <= 32 ? launch_decode<2, true>(D, n, max_count, st)
+                                : max_rank <= 64 ? launch_decode<4, true>(D, n, max_count, st) : launch_decode<8, true>(D, n, max_count, st);
+        if (decode) return max_rank <= 16 ? launch_decode<1, false>(D, n, max_count, st) : max_rank <= 32 ? launch_decode<2, false>(D, n, max_count, st)
+                         : max_rank <= 64 ? launch_decode<4, false>(D, n, max_count, st) : launch_decode<8, false>(D, n, max_count, st);
+        if (vec) return max_rank <= 16 ? launch_widen<1, true>(P, n, max_m, st) : max_rank <= 32 ? launch_widen<2, true>(P, n, max_m, st)
+                      : max_rank <= 64 ? launch_widen<4, true>(P, n, max_m, st) : launch_widen<8, true>(P, n, max_m, st);
+        return max_rank <= 16 ? launch_widen<1, false>(P, n, max_m, st) : max_rank <= 32 ? launch_widen<2, false>(P, n, max_m, st)
+             : max_rank <= 64 ? launch_widen<4, false>(P, n, max_m, st) : launch_widen<8, false>(P, n, max_m, st);
     });
     if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return RABIT_OK;
