@@ -114,7 +114,7 @@ except ImportError as e:
                       "`python paper_2602_05367_b200/build.py`") from e
 _native.init(RabitError, *(ctypes.cast(getattr(_lib, name), _c_void_p).value for name in
                            ("rabit_linear", "rabit_linear_group", "rabit_linear_group_host", "rabit_layer_M", "rabit_layer_N", "rabit_last_error",
-                            "rabit_linear_adapted", "rabit_linear_group_adapted")))
+                            "rabit_linear_adapted", "rabit_linear_group_adapted", "rabit_adapter_gradients", "rabit_clip_gradients")))
 
 
 def _stream_of(device, stream: Optional[int]) -> int:
@@ -394,7 +394,8 @@ class RabitAdapters:
         self.a, self.b, self.scale = a, b, scale
         self.count, self.rank, self.N, self.M = a.shape[0], a.shape[1], a.shape[2], b.shape[2]
         self._struct = _AdaptersStruct(a.data_ptr(), b.data_ptr(), scale.data_ptr(), self.count, self.rank, self.N, self.M)
-        self._addr = ctypes.addressof(self._struct)
+        self._addr = ctypes.addressof(self._struct)     # for the native module
+        self._device = a.device.index
 
     def transposed(self) -> "RabitAdapters":
         """The same adapters beside the transposed layer (rabit_transpose): the factors exchanged, no copy."""
@@ -429,31 +430,11 @@ def rabit_transpose(layer: RabitLayer, stream: Optional[int] = None) -> RabitLay
     return RabitLayer(out.value, buf, K, M, N)
 
 
-def _dense(name, t, dtype, shape, device):
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != int(np.prod(shape)) or t.device != device:
-        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of {'*'.join(map(str, shape))} elements on the adapters' device")
-    return t.data_ptr()
-
-
 def rabit_adapter_gradients(adapters: RabitAdapters, x, u, dy, p, ids, da=None, db=None, accumulate: bool = False, stream: Optional[int] = None):
     """Gradients of the factors: da[i] = scale[i] * sum of p[t]^T x[t] and db[i] = scale[i] * sum of u[t]^T dy[t] over the rows t with
     ids[t] = i.  x float16 [batch][N] and u float32 [batch][rank] of the forward call, dy float16 [batch][M] and p float32 [batch][rank]
     of the backward call on the transposed layer.  da, db: CUDA float32 like a and b, overwritten or, with `accumulate`, added to."""
-    A, dev = adapters, adapters.a.device
-    batch = ids.numel()
-    if accumulate and (da is None or db is None):
-        raise ValueError("accumulate needs da and db")
-    if da is None:
-        da = torch.empty(A.a.shape, dtype=torch.float32, device=dev)
-    if db is None:
-        db = torch.empty(A.b.shape, dtype=torch.float32, device=dev)
-    args = [_dense("x", x, torch.float16, (batch, A.N), dev), _dense("u", u, torch.float32, (batch, A.rank), dev), _dense("dy", dy, torch.float16, (batch, A.M), dev),
-            _dense("p", p, torch.float32, (batch, A.rank), dev), _dense("ids", ids, torch.int32, (batch,), dev), _dense("da", da, torch.float32, A.a.shape, dev),
-            _dense("db", db, torch.float32, A.b.shape, dev)]
-    st = _stream_of(dev, stream)
-    with torch.cuda.device(dev):
-        _check(_lib.rabit_adapter_gradients(_c_void_p(A._addr), *map(_c_void_p, args), batch, 1 if accumulate else 0, _c_void_p(st)))
-    return da, db
+    return _native.adapter_gradients(adapters, x, u, dy, p, ids, da, db, accumulate, stream)
 
 
 class RabitGradients:
@@ -474,23 +455,18 @@ class RabitGradients:
         dst = None if outs is None else (_c_void_p * n)(*[t.data_ptr() for t in outs])
         self._keep = (tensors, outs)
         nbytes = int(_lib.rabit_gradients_bytes(counts, n))
-        self._handle = None
+        self._addr = None                               # the descriptor, for the native module; None once freed
+        self._device = dev.index
         self.dev_buf = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         out = _c_void_p()
         with torch.cuda.device(dev):
             _check(_lib.rabit_gradients_bind(src, dst, counts, n, _c_void_p(self.dev_buf.data_ptr()), nbytes, _c_void_p(_stream_of(dev, stream)), ctypes.byref(out)))
-        self._handle = out
-
-    @property
-    def handle(self) -> ctypes.c_void_p:
-        if self._handle is None:
-            raise RabitError(-1, "gradients already freed")
-        return self._handle
+        self._addr = out.value
 
     def free(self) -> None:
-        if self._handle is not None:
-            _lib.rabit_gradients_free(self._handle)
-            self._handle = self._keep = self.dev_buf = None
+        if self._addr is not None:
+            _lib.rabit_gradients_free(_c_void_p(self._addr))
+            self._addr = self._keep = self.dev_buf = None
 
     def __del__(self):  # pragma: no cover
         try:
@@ -501,15 +477,7 @@ class RabitGradients:
 
 def rabit_clip_gradients(gradients: RabitGradients, max_norm: float, norm=None, stream: Optional[int] = None):
     """Every gradient times min(1, max_norm / (norm + 1e-6)) with the norm over all of them; returns the norm (CUDA float32 [1])."""
-    handle, dev = gradients.handle, gradients.dev_buf.device
-    if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device=dev)
-    else:
-        _dense("norm", norm, torch.float32, (1,), dev)
-    st = _stream_of(dev, stream)
-    with torch.cuda.device(dev):
-        _check(_lib.rabit_clip_gradients(handle, max_norm, _c_void_p(norm.data_ptr()), _c_void_p(st)))
-    return norm
+    return _native.clip(gradients, max_norm, norm, stream)
 
 
 def rabit_free(layer: RabitLayer) -> None:

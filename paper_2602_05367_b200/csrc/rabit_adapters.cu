@@ -1295,6 +1295,12 @@ int gradients_call(const rabit_adapters* A, const void* x, const float* u, const
     for (const Range& o : outs)
         for (const Range& i : ins)
             if (o.meets(i)) return rabit_fail(RABIT_INVALID_ARG, "%s: a gradient overlaps an input", who);
+    int dev = -1;
+    cudaPointerAttributes attr;
+    RABIT_CUDA_TRY(cudaGetDevice(&dev));
+    RABIT_CUDA_TRY(cudaPointerGetAttributes(&attr, da));
+    if (attr.type != cudaMemoryTypeManaged && (attr.type != cudaMemoryTypeDevice || attr.device != dev))
+        return rabit_fail(RABIT_INVALID_ARG, "%s: da is not memory of the current device %d", who, dev);
     if (A->count > 65535) return rabit_fail(RABIT_UNSUPPORTED_SHAPE, "%s: at most 65535 adapters (got %d)", who, A->count);
     cudaStream_t st = (cudaStream_t)stream;
     FactorParams P{};

@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/Functions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -27,6 +28,8 @@ typedef int (*GroupFn)(const void* const*, const void* const*, void* const*, int
 typedef int (*GroupHostFn)(const void* const*, const void* const*, void* const*, int, int, void*, size_t, void*);
 typedef int (*AdaptedFn)(const void*, const rabit_adapters*, const void*, const int*, void*, float*, int, void*);
 typedef int (*GroupAdaptedFn)(const void* const*, const rabit_adapters* const*, const void* const*, const int*, void* const*, float* const*, int, int, void*);
+typedef int (*FactorFn)(const rabit_adapters*, const void*, const float*, const void*, const float*, const int*, float*, float*, int, int, void*);
+typedef int (*ClipFn)(const void*, float, float*, void*);
 typedef int (*DimFn)(const void*);
 typedef const char* (*ErrorFn)();
 
@@ -35,10 +38,14 @@ GroupFn p_group = nullptr;
 GroupHostFn p_group_host = nullptr;
 AdaptedFn p_adapted = nullptr;
 GroupAdaptedFn p_group_adapted = nullptr;
+FactorFn p_factor = nullptr;
+ClipFn p_clip = nullptr;
 DimFn p_M = nullptr, p_N = nullptr;
 ErrorFn p_error = nullptr;
 PyObject* g_error_type = nullptr;      // RabitError
 PyObject* g_addr_name = nullptr;       // "_addr": the descriptor's address on a RabitLayer, None once freed; on a RabitAdapters that of its rabit_adapters
+
+PyObject* g_device_name = nullptr;     // "_device": the index of the device that a RabitAdapters or RabitGradients lives on
 
 constexpr Py_ssize_t kInline = 16;     // layers of a group whose pointers need no allocation
 
@@ -162,6 +169,21 @@ PyObject* linear_group(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// the device of a RabitAdapters or RabitGradients; -1 with an exception set if it has none
+long device_of(PyObject* o) {
+    THPObjectPtr d(PyObject_GetAttr(o, g_device_name));
+    return d ? PyLong_AsLong(d.get()) : -1;
+}
+const rabit_adapters* adapters_on(PyObject* o, c10::DeviceIndex device) {
+    const rabit_adapters* A = (const rabit_adapters*)layer_handle(o);
+    if (!A) return nullptr;
+    const long d = device_of(o);
+    if (d == -1 && PyErr_Occurred()) return nullptr;
+    if (d == device) return A;
+    PyErr_Format(PyExc_ValueError, "the adapters live on device %ld, the activations on device %d", d, (int)device);
+    return nullptr;
+}
+
 // What the rows' adapters and low-rank products need: ids [batch] int32 and u [batch][rank] fp32 on the activations' device.
 inline bool is_cuda(PyObject* o, at::ScalarType type, int64_t n, c10::DeviceIndex device) {
     if (!THPVariable_Check(o)) return false;
@@ -184,9 +206,9 @@ PyObject* linear_adapted(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!is_cuda_half(args[2])) return PyErr_Format(PyExc_ValueError, "x must be a contiguous CUDA float16 tensor");
     const void* h = layer_handle(args[0]);
     if (!h) return nullptr;
-    const rabit_adapters* A = (const rabit_adapters*)layer_handle(args[1]);
-    if (!A) return nullptr;
     const at::Tensor& x = THPVariable_Unpack(args[2]);
+    const rabit_adapters* A = adapters_on(args[1], x.device().index());
+    if (!A) return nullptr;
     const int64_t M = p_M(h), N = p_N(h);
     const bool flat = x.dim() != 2;
     const int64_t batch = flat ? 1 : x.size(0), cols = flat ? x.numel() : x.size(1);
@@ -255,7 +277,6 @@ PyObject* linear_group_adapted(PyObject*, PyObject* const* args, Py_ssize_t narg
         hp[l] = layer_handle(PySequence_Fast_GET_ITEM(ls.get(), l));
         if (!hp[l]) return nullptr;
         ap[l] = up[l] = nullptr;
-        if (ao != Py_None && !(ap[l] = layer_handle(ao))) return nullptr;
         if (l == 0) {
             if (!THPVariable_Check(xo) || !THPVariable_Unpack(xo).is_cuda()) return PyErr_Format(PyExc_ValueError, "every x must be a contiguous CUDA float16 tensor of batch*N elements");
             const at::Tensor& x0 = THPVariable_Unpack(xo);
@@ -263,6 +284,7 @@ PyObject* linear_group_adapted(PyObject*, PyObject* const* args, Py_ssize_t narg
             device = x0.device().index();
             if (!stream_of(args[6], device, &stream)) return nullptr;
         }
+        if (ao != Py_None && !(ap[l] = (void*)adapters_on(ao, device))) return nullptr;
         if (!is_cuda(xo, at::kHalf, batch * p_N(hp[l]), device)) return PyErr_Format(PyExc_ValueError, "every x must be a contiguous CUDA float16 tensor of batch*N elements, all on one device");
         if (!is_cuda(yo, at::kHalf, batch * p_M(hp[l]), device)) return PyErr_Format(PyExc_ValueError, "every y must be a contiguous CUDA float16 tensor of batch*M elements, all on one device");
         xp[l] = THPVariable_Unpack(xo).data_ptr();
@@ -286,6 +308,75 @@ PyObject* linear_group_adapted(PyObject*, PyObject* const* args, Py_ssize_t narg
     if (rc != 0) return raise_code(rc, batch > INT32_MAX ? "batch too large" : p_error());
     Py_INCREF(args[4]);
     return args[4];
+    END_HANDLE_TH_ERRORS
+}
+
+// adapter_gradients(adapters, x, u, dy, p, ids, da | None, db | None, accumulate, stream | None) -> (da, db)
+PyObject* adapter_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 10) return PyErr_Format(PyExc_TypeError, "adapter_gradients takes 10 arguments");
+    HANDLE_TH_ERRORS
+    const rabit_adapters* A = (const rabit_adapters*)layer_handle(args[0]);
+    if (!A) return nullptr;
+    const long d = device_of(args[0]);
+    if (d == -1 && PyErr_Occurred()) return nullptr;
+    const c10::DeviceIndex device = (c10::DeviceIndex)d;
+    const int64_t batch = THPVariable_Check(args[5]) ? THPVariable_Unpack(args[5]).numel() : 0;
+    struct { int at; const char* name; at::ScalarType type; int64_t n; } want[] = {
+        {5, "ids", at::kInt, batch}, {1, "x", at::kHalf, batch * A->n_in}, {2, "u", at::kFloat, batch * A->rank}, {3, "dy", at::kHalf, batch * A->n_out}, {4, "p", at::kFloat, batch * A->rank},
+        {6, "da", at::kFloat, (int64_t)A->count * A->rank * A->n_in}, {7, "db", at::kFloat, (int64_t)A->count * A->rank * A->n_out}};
+    for (const auto& w : want)
+        if (!(w.at >= 6 && args[w.at] == Py_None) && !is_cuda(args[w.at], w.type, w.n, device))
+            return PyErr_Format(PyExc_ValueError, "%s must be a contiguous CUDA %s tensor of %lld elements on the adapters' device", w.name, w.type == at::kHalf ? "float16" : w.type == at::kInt ? "int32" : "float32", (long long)w.n);
+    const int accumulate = PyObject_IsTrue(args[8]);
+    if (accumulate < 0) return nullptr;
+    if (accumulate && (args[6] == Py_None || args[7] == Py_None)) return PyErr_Format(PyExc_ValueError, "accumulate needs da and db");
+    void* stream;
+    if (!stream_of(args[9], device, &stream)) return nullptr;
+    if (batch > INT32_MAX) return raise_code(RABIT_INVALID_ARG, "batch too large");
+    c10::cuda::CUDAGuard guard(device);
+    THPObjectPtr made[2];
+    float* out[2];
+    for (int i = 0; i < 2; ++i) {
+        if (args[6 + i] == Py_None) made[i] = THPVariable_Wrap(at::empty({A->count, A->rank, i == 0 ? A->n_in : A->n_out}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, device)));
+        else made[i] = Py_NewRef(args[6 + i]);
+        out[i] = THPVariable_Unpack(made[i].get()).data_ptr<float>();
+    }
+    auto ptr = [&](int i) { return THPVariable_Unpack(args[i]).data_ptr(); };
+    const void *x = ptr(1), *dy = ptr(3);
+    const float *u = (const float*)ptr(2), *p = (const float*)ptr(4);
+    const int* ids = (const int*)ptr(5);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = p_factor(A, x, u, dy, p, ids, out[0], out[1], (int)batch, accumulate, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != 0) return raise_code(rc, p_error());
+    return PyTuple_Pack(2, made[0].get(), made[1].get());
+    END_HANDLE_TH_ERRORS
+}
+
+// clip(gradients, max_norm, norm | None, stream | None) -> norm
+PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 4) return PyErr_Format(PyExc_TypeError, "clip takes 4 arguments");
+    HANDLE_TH_ERRORS
+    const void* h = layer_handle(args[0]);
+    if (!h) return nullptr;
+    const long d = device_of(args[0]);
+    if (d == -1 && PyErr_Occurred()) return nullptr;
+    const c10::DeviceIndex device = (c10::DeviceIndex)d;
+    const double max_norm = PyFloat_AsDouble(args[1]);
+    if (max_norm == -1.0 && PyErr_Occurred()) return nullptr;
+    if (args[2] != Py_None && !is_cuda(args[2], at::kFloat, 1, device)) return PyErr_Format(PyExc_ValueError, "norm must be a CUDA float32 tensor of one element on the gradients' device");
+    void* stream;
+    if (!stream_of(args[3], device, &stream)) return nullptr;
+    c10::cuda::CUDAGuard guard(device);
+    THPObjectPtr norm(args[2] == Py_None ? THPVariable_Wrap(at::empty({1}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, device))) : Py_NewRef(args[2]));
+    float* out = THPVariable_Unpack(norm.get()).data_ptr<float>();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = p_clip(h, (float)max_norm, out, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != 0) return raise_code(rc, p_error());
+    return norm.release();
     END_HANDLE_TH_ERRORS
 }
 
@@ -317,11 +408,12 @@ PyObject* current_stream(PyObject*, PyObject* arg) {
     END_HANDLE_TH_ERRORS
 }
 
-// init(error type, address of rabit_linear, _linear_group, _linear_group_host, _layer_M, _layer_N, _last_error, _linear_adapted, _linear_group_adapted)
+// init(error type, address of rabit_linear, _linear_group, _linear_group_host, _layer_M, _layer_N, _last_error, _linear_adapted, _linear_group_adapted,
+// _adapter_gradients, _clip_gradients)
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    if (nargs != 9) return PyErr_Format(PyExc_TypeError, "init takes 9 arguments");
-    void* v[8];
-    for (int i = 0; i < 8; ++i) v[i] = PyLong_AsVoidPtr(args[1 + i]);
+    if (nargs != 11) return PyErr_Format(PyExc_TypeError, "init takes 11 arguments");
+    void* v[10];
+    for (int i = 0; i < 10; ++i) v[i] = PyLong_AsVoidPtr(args[1 + i]);
     if (PyErr_Occurred()) return nullptr;
     p_linear = (LinearFn)v[0];
     p_group = (GroupFn)v[1];
@@ -331,6 +423,8 @@ PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     p_error = (ErrorFn)v[5];
     p_adapted = (AdaptedFn)v[6];
     p_group_adapted = (GroupAdaptedFn)v[7];
+    p_factor = (FactorFn)v[8];
+    p_clip = (ClipFn)v[9];
     Py_XSETREF(g_error_type, Py_NewRef(args[0]));
     Py_RETURN_NONE;
 }
@@ -341,6 +435,8 @@ PyMethodDef methods[] = {
     {"linear_group", (PyCFunction)(void (*)(void))linear_group, METH_FASTCALL, nullptr},
     {"linear_adapted", (PyCFunction)(void (*)(void))linear_adapted, METH_FASTCALL, nullptr},
     {"linear_group_adapted", (PyCFunction)(void (*)(void))linear_group_adapted, METH_FASTCALL, nullptr},
+    {"adapter_gradients", (PyCFunction)(void (*)(void))adapter_gradients, METH_FASTCALL, nullptr},
+    {"clip", (PyCFunction)(void (*)(void))clip, METH_FASTCALL, nullptr},
     {"group_host", (PyCFunction)(void (*)(void))group_host, METH_FASTCALL, nullptr},
     {"current_stream", current_stream, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
@@ -351,5 +447,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rabit_binding", nullptr, -1, meth
 
 PyMODINIT_FUNC PyInit__rabit_binding(void) {
     g_addr_name = PyUnicode_InternFromString("_addr");
-    return g_addr_name ? PyModule_Create(&module) : nullptr;
+    g_device_name = PyUnicode_InternFromString("_device");
+    return g_addr_name && g_device_name ? PyModule_Create(&module) : nullptr;
 }
