@@ -20,12 +20,12 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxGroup = 8;                           // layers in one launch
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // the same on top of zero
 __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // fp32 operands of MMAs with fp16 ones.  Values that share a power of two are scaled so that the largest lies in [2^14, 2^15), then each is the sum of two fp16
@@ -87,14 +87,14 @@ struct NarrowLayer {
 struct NarrowParams {
     NarrowLayer layer[kMaxGroup];
     const int* ids;
-    int batch;
+    int batch, shares;                                                          // clusters that share the adapters of a tile of rows; the later ones are mostly idle, so they come last
 };
 
 // Up to 256 rows.  A cluster takes a tile of 16 rows and cuts the contraction into one part per warp of its CTAs; parts meet in shared memory, then over the
 // cluster, in a fixed order.  Products are m16n8k16 MMAs of fp16 operands, rows by ranks.  The order of a contraction is free, so a lane takes 8 consecutive
 // columns of each of its rows (one 16-byte load, no detour through shared memory) as the four operand words of two MMAs; the loads of the next columns
 // are in flight beside the MMAs.
-// Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own.  gridDim.y clusters share
+// Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own.  Several clusters share
 // the adapters of a tile, so that a batch of single tokens with an adapter each does not read them one after the other.
 // The tensor core truncates when it accumulates: after at most 16 MMAs the sums go to fp32 words in shared memory.
 // Bound: latencies (launch, ids, x and factor, the sum over the cluster).
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, NR <= 2 ? 3 : NR <= 4 ? 2 : 1) narro
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
     const NarrowLayer& L = P.layer[blockIdx.z];
-    const int row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, rank = L.rank;
+    const int share = blockIdx.y, row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, rank = L.rank;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;           // the lane's sums: rows gq and gq + 8, ranks 8 j + 2 tq and the next
 #pragma unroll
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, NR <= 2 ? 3 : NR <= 4 ? 2 : 1) narro
         const int cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
         const uint32_t match = __ballot_sync(0xFFFFFFFFu, id == cur);
         left &= ~match;
-        if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
+        if (turn % P.shares != share) continue;
         mine |= match;
         const __half* a = L.a + ((size_t)cur * rank + gq) * n + 8 * tq;
         const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
@@ -146,10 +146,9 @@ __global__ void __launch_bounds__(kThreads, NR <= 2 ? 3 : NR <= 4 ? 2 : 1) narro
         };
         auto multiply = [&](const Loads& l) {
 #pragma unroll
-            for (int j = 0; j < NR; ++j) {
-                mma_f16(acc[j], l.x[0].x, l.x[1].x, l.x[0].y, l.x[1].y, l.a[j].x, l.a[j].y);
-                mma_f16(acc[j], l.x[0].z, l.x[1].z, l.x[0].w, l.x[1].w, l.a[j].z, l.a[j].w);
-            }
+            for (int j = 0; j < NR; ++j) mma_f16(acc[j], l.x[0].x, l.x[1].x, l.x[0].y, l.x[1].y, l.a[j].x, l.a[j].y);
+#pragma unroll
+            for (int j = 0; j < NR; ++j) mma_f16(acc[j], l.x[0].z, l.x[1].z, l.x[0].w, l.x[1].w, l.a[j].z, l.a[j].w);
         };
         auto flush = [&]() {
 #pragma unroll
@@ -177,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, NR <= 2 ? 3 : NR <= 4 ? 2 : 1) narro
         }
         if (pairs % 4 != 0) flush();
     }
-    const uint32_t bare = blockIdx.y == 0 ? ~named : 0u;                        // their u is zero: the first cluster's
+    const uint32_t bare = share == 0 ? ~named : 0u;                        // their u is zero: the first cluster's
     if (mine == 0u && bare == 0u) return;                                       // (the whole cluster agrees)
     __syncthreads();
     for (int e = threadIdx.x; e < kRows * kRanks; e += kThreads) {
@@ -227,8 +226,8 @@ __device__ __forceinline__ uint4 load_8(const __half* src, int n) {
 // ---- u[t] = A[id_t] x[t], more rows ----------------------------------------------------------------------------
 
 // The same for more rows: a CTA takes 16 * WM of them, WM warps side by side, so that the factor's columns in shared memory serve all; 8 / WM such groups of warps
-// and the CTAs of a cluster cut the contraction.  x and the factor come through a ring of asynchronous copies, 64 columns per group of warps and
-// stage: a lane reads back the x that it copied itself.
+// and the CTAs of a cluster cut the contraction.  x and the factor come through a ring of asynchronous copies, 64 columns (a line of memory) per group of
+// warps and stage; what bounds such copies is the number of lines that an instruction touches.
 // Bound: x from memory; from rank 64 on the reads of the factor from shared memory as well.
 template <int NR, int WM>
 struct Tile {
@@ -246,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3, wm = warp % WM, wk = warp / WM;
     const NarrowLayer& L = P.layer[blockIdx.z];
-    const int tile0 = (int)(blockIdx.x / parts) * T::kRows, n = L.n, rank = L.rank, row0 = tile0 + 16 * wm;
+    const int share = blockIdx.y, tile0 = (int)(blockIdx.x / parts) * T::kRows, n = L.n, rank = L.rank, row0 = tile0 + 16 * wm;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -282,34 +281,47 @@ __global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_
             const uint32_t match = __ballot_sync(0xFFFFFFFFu, id[w] == cur);
             left[w] &= ~match;
             any = any || left[w] != 0u;
-            if (turn % (int)gridDim.y == (int)blockIdx.y) {
+            if (turn % P.shares == share) {
                 mine[w] |= match;
                 if (w == wm / 2) own = (match >> (16 * (wm & 1))) & 0xFFFFu;
             }
         }
-        if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
+        if (turn % P.shares != share) continue;
         const bool has[2] = {(own >> gq & 1u) != 0u, (own >> (8 + gq) & 1u) != 0u};
         const __half* a = L.a + (size_t)cur * rank * n;
-        const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
+        // What a thread copies lies at fixed places of a stage: 16-byte pieces of the factor's rows, 8 to a row and group of warps (odd rows have their two halves
+        // exchanged, for the banks), and pieces of its warp's rows of x.
+        constexpr int kCopies = (T::WK * T::kRanks * 8 + kThreads - 1) / kThreads;
+        const int piece = threadIdx.x & 7, j0 = threadIdx.x >> 3;
+        const bool all_copy = T::WK * T::kRanks * 8 >= kThreads || (int)threadIdx.x < T::WK * T::kRanks * 8;
+        const __half* a0 = a + (size_t)(j0 % T::kRanks) * n + (c0 + j0 / T::kRanks) * 64 + piece * 8;
+        const int x_row = lane >> 3;                                            // of four rows to a copy of the warp: 128 bytes of each, whole lines
+        const __half* x0 = L.x + (size_t)(row0 + x_row) * n + (size_t)(c0 + wk) * 64 + (lane & 7) * 8;
+        const size_t rows32 = (size_t)32 * n, rows4 = (size_t)4 * n;
         auto fetch = [&](int it) {
             unsigned char* stage = smem + it % T::kStages * T::kStageBytes;
             if (it < iters) {
+                const int chunk0 = c0 + it * T::WK;
+                const bool whole = chunk0 + T::WK <= c1 && (chunk0 + T::WK) * 64 <= n;   // (all but the last)
+                if (all_copy) {
 #pragma unroll
-                for (int i0 = 0; i0 < T::WK * T::kRanks * 8; i0 += kThreads) {  // 8 pieces of 16 bytes per row; odd rows have their two halves exchanged (banks)
-                    const int i = i0 + (int)threadIdx.x, piece = i & 7, j = (i >> 3) % T::kRanks, k = (i >> 3) / T::kRanks, chunk = c0 + it * T::WK + k, col = chunk * 64 + piece * 8;
-                    if (T::WK * T::kRanks * 8 % kThreads != 0 && i >= T::WK * T::kRanks * 8) break;
-                    const bool in = chunk < c1 && col < n && j < rank;
-                    copy_async_16(stage + (k * T::kRanks + j) * 128 + ((piece ^ ((j & 1) << 2)) << 4), in ? a + (size_t)j * n + col : L.a, in);
+                    for (int i = 0; i < kCopies; ++i) {
+                        constexpr int kPer = T::kRanks >= 32 ? T::kRanks / 32 : 1;      // copies of 32 rows to a group of warps
+                        const int k = T::kRanks >= 32 ? i / kPer : j0 / T::kRanks, j = (T::kRanks >= 32 ? i % kPer * 32 : 0) + j0 % T::kRanks;
+                        const bool in = j < rank && (whole || (chunk0 + k < c1 && (chunk0 + k) * 64 + piece * 8 < n));
+                        const __half* src = a0 + (size_t)it * (T::WK * 64) + (T::kRanks >= 32 ? (size_t)(i % kPer) * rows32 + i / kPer * 64 : 0);
+                        copy_async_16(stage + (k * T::kRanks + j) * 128 + ((piece ^ ((j & 1) << 2)) << 4), in ? src : L.a, in);
+                    }
                 }
                 if (own != 0u) {
-                    const int chunk = c0 + it * T::WK + wk;
+                    const __half* src = x0 + (size_t)it * (T::WK * 64);
+                    const bool col_in = whole || (chunk0 + wk < c1 && (chunk0 + wk) * 64 + (lane & 7) * 8 < n);
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const bool in = chunk < c1 && chunk * 64 + s * 32 < n && has[m];
-                            copy_async_16(stage + T::kABytes + ((warp * 4 + 2 * s + m) * 32 + lane) * 16, in ? x + (size_t)(8 * m) * n + chunk * 64 + s * 32 : L.x, in);
-                        }
+                    for (int m = 0; m < 4; ++m) {
+                        const int r = 4 * m + x_row;
+                        const bool in = col_in && (own >> r & 1u);
+                        copy_async_16(stage + T::kABytes + (warp * 16 + r) * 128 + (((lane & 7) ^ ((r & 1) << 2)) << 4), in ? src + m * rows4 : L.x, in);
+                    }
                 }
             }
             copy_async_commit();
@@ -334,13 +346,19 @@ __global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_
             const unsigned char* stage = smem + it % T::kStages * T::kStageBytes;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const uint4 x0 = *reinterpret_cast<const uint4*>(stage + T::kABytes + ((warp * 4 + 2 * s) * 32 + lane) * 16), x1 = *reinterpret_cast<const uint4*>(stage + T::kABytes + ((warp * 4 + 2 * s + 1) * 32 + lane) * 16);
-                const unsigned char* at = stage + (wk * T::kRanks + gq) * 128 + ((s ^ (gq & 1)) << 6) + tq * 16;
+                const int swizzled = ((s ^ (gq & 1)) << 6) + tq * 16;
+                const unsigned char *x_at = stage + T::kABytes + (warp * 16 + gq) * 128 + swizzled, *at = stage + (wk * T::kRanks + gq) * 128 + swizzled;
+                const uint4 x0 = *reinterpret_cast<const uint4*>(x_at), x1 = *reinterpret_cast<const uint4*>(x_at + 8 * 128);
 #pragma unroll
-                for (int j = 0; j < NR; ++j) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(at + j * 8 * 128);
-                    mma_f16(acc[j], x0.x, x1.x, x0.y, x1.y, w.x, w.y);
-                    mma_f16(acc[j], x0.z, x1.z, x0.w, x1.w, w.z, w.w);
+                for (int j0 = 0; j0 < NR; j0 += 8) {                            // (products on top of one another far apart: an MMA takes about four others' time to finish)
+                    constexpr int kJ = NR < 8 ? NR : 8;
+                    uint4 w[kJ];
+#pragma unroll
+                    for (int j = 0; j < kJ; ++j) w[j] = *reinterpret_cast<const uint4*>(at + (j0 + j) * 8 * 128);
+#pragma unroll
+                    for (int j = 0; j < kJ; ++j) mma_f16(acc[j0 + j], x0.x, x1.x, x0.y, x1.y, w[j].x, w[j].y);
+#pragma unroll
+                    for (int j = 0; j < kJ; ++j) mma_f16(acc[j0 + j], x0.z, x1.z, x0.w, x1.w, w[j].z, w[j].w);
                 }
             }
             if (it % 4 == 3) flush();
@@ -349,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_
         copy_async_wait<0>();
         __syncthreads();                                                        // (the next adapter fills the same stages)
     }
-    bool taken = blockIdx.y == 0;                                               // rows without adapter: u is zero, the first cluster's
+    bool taken = share == 0;                                               // rows without adapter: u is zero, the first cluster's
 #pragma unroll
     for (int w = 0; w < kWords; ++w) taken = taken || mine[w] != 0u;
     if (!taken) return;                                                         // (the whole cluster agrees)
@@ -375,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_
         uint32_t word = 0u;
 #pragma unroll
         for (int w = 0; w < kWords; ++w)
-            if (row / 32 == w) word = mine[w] | (blockIdx.y == 0 ? ~named[w] : 0u);
+            if (row / 32 == w) word = mine[w] | (share == 0 ? ~named[w] : 0u);
         if (j >= rank || tile0 + row >= P.batch || !((word >> (row & 31)) & 1u)) continue;
         store_4(L.u + (size_t)(tile0 + row) * rank + j, cluster_sum(cluster, red, parts, e), rank - j, rank % 4 == 0);
     }
@@ -451,8 +469,10 @@ __device__ __forceinline__ void widen_step(float (&acc)[GROUPS][4][4], bool firs
 template <int R16, bool VEC>
 struct Widen {
     static constexpr int kRanks = 16 * R16, kTiles = kWidenRows / 16, kFours = kRanks / 4;
-    static constexpr int kGroups = R16 <= 4 && VEC ? 2 : 1, kCols = 32 * kGroups * kWarps;      // of 32 columns to a warp
-    static constexpr int kBlockPieces = kTiles * 2 * kGroups * 32;              // 16-byte pieces of y of a warp in a block; what a lane copied it reads back itself
+    static constexpr int kGroups = R16 <= 2 && VEC ? 2 : 1, kCols = 32 * kGroups * kWarps;      // of 32 columns to a warp
+    static constexpr int kLanes = 4 * kGroups, kBlockPieces = kWidenRows * kLanes;   // 16-byte pieces of a warp's row of y, of its block
+    // place of piece p of row r: two rows that a load touches, 64 bytes each, meet in no bank
+    static __device__ __forceinline__ int piece(int r, int p) { return r * kLanes + (kLanes == 8 ? p ^ ((r & 1) << 2) : p); }
     static constexpr int kRingBytes = 2 * kWarps * kBlockPieces * 16, kUBytes = kWidenRows * kRanks * 4;
     static constexpr int kBytes = kRingBytes + kUBytes + Operand<R16>::pieces(kWidenRows) * 16 + kWidenRows * 4;
     static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs per SM");
@@ -517,24 +537,23 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
 
     const bool fours = rank % 4 == 0;
     const int c = col0 + 8 * tq;                                                // the lane's columns in y: 8 here and 8 in each further group
-    ring += warp * W::kBlockPieces + lane;
+    ring += warp * W::kBlockPieces;
     __half* y = L.y + (size_t)(first_row + gq) * m_all + c;                     // the lane's part of row gq of the block at hand
+    const __half* y_from = L.y + (size_t)(first_row + lane / W::kLanes) * m_all + col0 + lane % W::kLanes * 8;   // what it copies first
     const size_t eight = (size_t)8 * m_all;
     // u of a block and the lane's part of y of the same rows: one group of copies
     auto fetch = [&](int blk, const __half* from) {
         const int row0 = first_row + blk * kWidenRows;
         if (blk < blocks) {
+            // rows of 8 * kLanes columns, kLanes lanes side by side: whole lines of memory where a warp has 64 columns
             uint4* dst = ring + (blk & 1) * (kWarps * W::kBlockPieces);
 #pragma unroll
-            for (int t = 0; t < 2 * kTiles; ++t) {
-                const bool row_in = row0 + 8 * t + gq < batch;
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const bool in = row_in && c + 32 * g < m_all;
-                    if (VEC) copy_async_16(dst + (t * G + g) * 32, in ? from + 32 * g : L.y, in);
-                    else dst[(t * G + g) * 32] = load_8<false>(from + 32 * g, in ? m_all - c - 32 * g : 0);
-                }
-                from += eight;
+            for (int t = 0; t < kWidenRows; t += 32 / W::kLanes) {
+                const int r = t + lane / W::kLanes, p = lane % W::kLanes, cols = m_all - col0 - 8 * p;
+                const bool in = row0 + r < batch && cols > 0;
+                const __half* src = in ? from + (size_t)t * m_all : L.y;
+                if (VEC) copy_async_16(dst + W::piece(r, p), src, in);
+                else dst[W::piece(r, p)] = load_8<false>(src, in ? cols : 0);
             }
             for (int i = threadIdx.x; i < kWidenRows * W::kFours; i += kThreads) {
                 const int r = i / W::kFours, j = i % W::kFours * 4;
@@ -578,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
         }
     };
 
-    fetch(0, y);
+    fetch(0, y_from);
     int next_id = load_id(0), held = -1;                                        // held: the adapter whose factor the registers hold
     for (int blk = 0; blk < blocks; ++blk) {
         const int id = next_id;
@@ -593,7 +612,8 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
             if (i % W::kFours == 0) backs[i / W::kFours] = back;
         }
         __syncthreads();
-        fetch(blk + 1, y + 4 * eight);
+        y_from += 4 * eight;
+        fetch(blk + 1, y_from);
         const uint4* old = ring + (blk & 1) * (kWarps * W::kBlockPieces);
         while (left != 0u) {
             if (cur != held) load_factor(held = cur);
@@ -613,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
                     const float factor = scale * backs[16 * mt + 8 * h + gq];
 #pragma unroll
                     for (int g = 0; g < G; ++g)
-                        if (c + 32 * g < m_all) widen_store<VEC>(y + (2 * mt + h) * eight + 32 * g, m_all - c - 32 * g, old[((2 * mt + h) * G + g) * 32], acc[g], h, factor);
+                        if (c + 32 * g < m_all) widen_store<VEC>(y + (2 * mt + h) * eight + 32 * g, m_all - c - 32 * g, old[W::piece(16 * mt + 8 * h + gq, 4 * g + tq)], acc[g], h, factor);
                 }
             }
             if (left != 0u) cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
@@ -634,12 +654,13 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
 constexpr int kGatherRows = 64;
 template <int R16>
 struct Decode {
-    static constexpr int kRows = 16, kRanks = 16 * R16, kCluster = R16 == 8 ? 8 : 16;   // (most CTAs of a cluster)
+    static constexpr int kRows = 16, kRanks = 16 * R16, kCluster = 8;   // (most CTAs of a cluster)
+    static constexpr int kSets = R16 <= 4 ? 2 : 1;                              // sets of 32 columns that a warp has on their way
     static constexpr int kBytes = (kWarps + kCluster) * kRows * kRanks * 4 + Operand<R16>::pieces(kRows) * 16 + kRows * 4 + kWarps * kRows * 4;
     static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
 };
 template <int R16, bool VEC, bool GATHER>
-__global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(const __grid_constant__ DecodeParams P) {
+__global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(const __grid_constant__ DecodeParams P) {
     using D = Decode<R16>;
     using O = Operand<R16>;
     constexpr int kRows = D::kRows, kRanks = D::kRanks, NR = 2 * R16;
@@ -670,9 +691,11 @@ __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(cons
     uint32_t same_of1 = 0u, same1_of1 = 0u;
     if (GATHER && batch > 32) {
         same1_of1 = __match_any_sync(kAll, id1);
-        for (int q = 0; q < 32; ++q) {
-            if (__shfl_sync(kAll, id1, q) == id) same1 |= 1u << q;
-            if (__shfl_sync(kAll, id, q) == id1) same_of1 |= 1u << q;
+        for (uint32_t each = __ballot_sync(kAll, id1 >= 0 && (same1_of1 & before) == 0u); each != 0u; each &= each - 1u) {   // the adapters among the second 32 rows
+            const int who = __ffs(each) - 1, v = __shfl_sync(kAll, id1, who);
+            const uint32_t there = __shfl_sync(kAll, same1_of1, who), here = __ballot_sync(kAll, id == v);
+            if (id == v) same1 = there;
+            if (id1 == v) same_of1 = here;
         }
         leads1 = id1 >= 0 && same_of1 == 0u && (same1_of1 & before) == 0u;
     }
@@ -762,17 +785,21 @@ __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(cons
         const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + 8 * (gq >> 1);
         __half* y[2] = {L.y + row[0] * m_all + 8 * tq, L.y + row[1] * m_all + 8 * tq};
         int g = warp * parts + part;                                        // neighbouring columns to different SMs
-        uint4 raw[R16][4], ahead[2];
-        auto load_columns = [&](int g) {
+        struct Columns {
+            uint4 b[R16][4], y[2];
+        };
+        auto load_columns = [&](Columns& l, int g) {
             const int in_b = g < groups ? m_all - 32 * g - 8 * (gq >> 1) : 0, in_y = g < groups ? m_all - 32 * g - 8 * tq : 0;
 #pragma unroll
             for (int k = 0; k < R16; ++k)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) raw[k][i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all + 32 * g, 16 * k + 4 * tq + i < rank ? in_b : 0);
+                for (int i = 0; i < 4; ++i) l.b[k][i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all + 32 * g, 16 * k + 4 * tq + i < rank ? in_b : 0);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) ahead[h] = load_8<VEC>(y[h] + 32 * g, has[h] ? in_y : 0);
+            for (int h = 0; h < 2; ++h) l.y[h] = load_8<VEC>(y[h] + 32 * g, has[h] ? in_y : 0);
         };
-        load_columns(g);
+        Columns sets[D::kSets];
+#pragma unroll
+        for (int q = 0; q < D::kSets; ++q) load_columns(sets[q], g + q * step);
         __syncthreads();
         cluster_wait();
         for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
@@ -801,19 +828,20 @@ __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(cons
         __syncthreads();
         if (turn + (int)gridDim.y < total) cluster_arrive();                // the inbox has been read: sums of the next item may come
 
-        for (; g < groups; g += step) {
+        auto widen_columns = [&](Columns& l, int g) {
+            if (g >= groups) return;
             uint32_t f[R16][1][4][2];
 #pragma unroll
             for (int k = 0; k < R16; ++k)
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
-                    f[k][0][0][p] = __byte_perm(raw[k][2 * p].x, raw[k][2 * p + 1].x, pick);
-                    f[k][0][1][p] = __byte_perm(raw[k][2 * p].y, raw[k][2 * p + 1].y, pick);
-                    f[k][0][2][p] = __byte_perm(raw[k][2 * p].z, raw[k][2 * p + 1].z, pick);
-                    f[k][0][3][p] = __byte_perm(raw[k][2 * p].w, raw[k][2 * p + 1].w, pick);
+                    f[k][0][0][p] = __byte_perm(l.b[k][2 * p].x, l.b[k][2 * p + 1].x, pick);
+                    f[k][0][1][p] = __byte_perm(l.b[k][2 * p].y, l.b[k][2 * p + 1].y, pick);
+                    f[k][0][2][p] = __byte_perm(l.b[k][2 * p].z, l.b[k][2 * p + 1].z, pick);
+                    f[k][0][3][p] = __byte_perm(l.b[k][2 * p].w, l.b[k][2 * p + 1].w, pick);
                 }
-            const uint4 old[2] = {ahead[0], ahead[1]};
-            load_columns(g + step);
+            const uint4 old[2] = {l.y[0], l.y[1]};
+            load_columns(l, g + D::kSets * step);
             float sum[1][4][4];
 #pragma unroll
             for (int k = 0; k < R16; ++k) widen_step<1>(sum, k == 0, us + O::at(gq) + 4 * k + tq, O::kSecond, f[k]);
@@ -821,6 +849,10 @@ __global__ void __launch_bounds__(kThreads, R16 <= 2 ? 2 : 1) decode_kernel(cons
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 if (has[h] && left_cols > 0) widen_store<VEC>(y[h] + 32 * g, left_cols, old[h], sum[0], h, scale * backs[8 * h + gq]);
+        };
+        for (; g < groups; g += D::kSets * step) {
+#pragma unroll
+            for (int q = 0; q < D::kSets; ++q) widen_columns(sets[q], g + q * step);
         }
     }
     if (blockIdx.y == 0 && part == 0) {                                         // rows without adapter: u is zero
@@ -1078,21 +1110,16 @@ cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, boo
     return cudaLaunchKernelEx(&cfg, kernel, P);
 }
 
-// Clusters of 8, 4, 2 or 1 CTAs for `tiles` clusters: as many CTAs as keep the SMs busy once.
-int cluster_for(long long tiles) {
-    int c = 8;
-    while (c > 1 && tiles * c > 400) c /= 2;
-    return c;
-}
-
 // Clusters that share the adapters of a tile of rows: more while there are few tiles.
 int shares_for(int batch) { return batch < 2048 ? 4 : 2; }
 
-cudaError_t launch_narrow(const NarrowParams& P, int n_layers, int max_rank, cudaStream_t stream) {
+cudaError_t launch_narrow(NarrowParams& P, int n_layers, int max_rank, cudaStream_t stream) {
     const int wm = P.batch <= 256 ? 1 : P.batch < 2048 ? 4 : 8;                 // 16, 64 or 128 rows to a tile
     const long long tiles = (P.batch + 16 * wm - 1) / (16 * wm);
-    const int c = cluster_for(tiles * n_layers);
-    const dim3 grid((unsigned)(tiles * c), (unsigned)shares_for(P.batch), (unsigned)n_layers);
+    P.shares = shares_for(P.batch);
+    int c = kMaxCluster;
+    while (c > 1 && tiles * n_layers * c > 400) c /= 2;
+    const dim3 grid((unsigned)(tiles * c), (unsigned)P.shares, (unsigned)n_layers);
     auto small = [&](auto kernel, int nr) { return launch(kernel, grid, c, kWarps * kNarrowRows * 8 * nr * 4, true, P, stream); };
     if (wm == 1) return max_rank <= 16 ? small(narrow_kernel<2>, 2) : max_rank <= 32 ? small(narrow_kernel<4>, 4) : max_rank <= 64 ? small(narrow_kernel<8>, 8) : small(narrow_kernel<16>, 16);
     auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, c, bytes, true, P, stream); };
@@ -1117,11 +1144,11 @@ cudaError_t launch_widen(WidenParams& P, int n_layers, int max_m, cudaStream_t s
 template <int R16, bool VEC>
 cudaError_t launch_decode(const DecodeParams& P, int n_layers, int max_count, cudaStream_t stream) {
     // up to 64 rows an item for every adapter that they can name, and one for every 16 rows beyond that; more rows are prompts, with few adapters to 16 of
-    // them.  Clusters as large as leave about three CTAs to an SM, of which those without an item end at once.
+    // them.  Clusters as large as leave the CTAs of one wave; those without an item end at once.
     const bool gather = P.batch <= kGatherRows;
     const int items = gather ? std::min(P.batch, max_count) + P.batch / 16 : (P.batch + 15) / 16 * 4;
     int c = Decode<R16>::kCluster;
-    while (c > 2 && (long long)items * n_layers * c > 444) c /= 2;
+    while (c > 2 && (long long)items * n_layers * c > (R16 == 1 ? 296 : 222)) c /= 2;
     const dim3 grid((unsigned)(gather ? c : items / 4 * c), (unsigned)(gather ? items : 4), (unsigned)n_layers);
     return gather ? launch(decode_kernel<R16, VEC, true>, grid, c, Decode<R16>::kBytes, true, P, stream) : launch(decode_kernel<R16, VEC, false>, grid, c, Decode<R16>::kBytes, true, P, stream);
 }
@@ -1136,7 +1163,7 @@ cudaError_t launch_factor(FactorParams& P, int count, cudaStream_t stream) {
     const long long tiles = (P.batch + F::kRows - 1) / F::kRows;
     int c = 1;
     double least = 1e300;
-    for (int q = 1; q <= kMaxCluster && q <= tiles; ++q) {
+    for (int q = 1; q <= 8 && q <= tiles; ++q) {
         const double cost = (double)((blocks * count * q + 147) / 148) * (5.0 + (double)((tiles + q - 1) / q) / count);
         if (cost < least) { least = cost; c = q; }
     }
