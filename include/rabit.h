@@ -225,7 +225,7 @@ RABIT_API size_t rabit_gradients_bytes(const size_t* counts, int n);
 RABIT_API int rabit_gradients_bind(const float* const* tensors, float* const* outs, const size_t* counts, int n,
                          void* dev_buf, size_t dev_bytes, void* stream, rabit_gradients** out);
 /*
- *   norm_out  DEVICE fp32, receives the norm before clipping (as it is: infinite or NaN where the gradients are)
+ *   norm_out  DEVICE fp32 outside all of that memory, receives the norm before clipping (as it is: infinite or NaN where the gradients are)
  *   max_norm  > 0 and finite
  * Squares are summed in 64 bits in an order that the sizes fix.  An infinite norm makes the factor 0, a NaN makes it NaN, as the formula says.
  * Calls on one rabit_gradients must not overlap in time (they share its partial sums).

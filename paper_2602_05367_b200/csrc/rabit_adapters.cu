@@ -90,110 +90,6 @@ struct NarrowParams {
     int batch, shares;                                                          // clusters that share the adapters of a tile of rows; the later ones are mostly idle, so they come last
 };
 
-// Up to 256 rows.  A cluster takes a tile of 16 rows and cuts the contraction into one part per warp of its CTAs; parts meet in shared memory, then over the
-// cluster, in a fixed order.  Products are m16n8k16 MMAs of fp16 operands, rows by ranks.  The order of a contraction is free, so a lane takes 8 consecutive
-// columns of each of its rows (one 16-byte load, no detour through shared memory) as the four operand words of two MMAs; the loads of the next columns
-// are in flight beside the MMAs.
-// Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own.  Several clusters share
-// the adapters of a tile, so that a batch of single tokens with an adapter each does not read them one after the other.
-// The tensor core truncates when it accumulates: after at most 16 MMAs the sums go to fp32 words in shared memory.
-// Bound: latencies (launch, ids, x and factor, the sum over the cluster).
-constexpr int kNarrowRows = 16;
-template <int NR>
-__global__ void __launch_bounds__(kThreads, NR <= 2 ? 3 : NR <= 4 ? 2 : 1) narrow_kernel(const __grid_constant__ NarrowParams P) {
-    constexpr int kRows = kNarrowRows, kRanks = 8 * NR;
-    extern __shared__ __align__(16) float red[];                                // [kWarps][kRows][kRanks]
-    cg::cluster_group cluster = cg::this_cluster();
-    const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
-    const NarrowLayer& L = P.layer[blockIdx.z];
-    const int share = blockIdx.y, row0 = (int)(blockIdx.x / parts) * kRows, n = L.n, rank = L.rank;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    float* own = red + ((size_t)warp * kRows + gq) * kRanks + 2 * tq;           // the lane's sums: rows gq and gq + 8, ranks 8 j + 2 tq and the next
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int j = 0; j < NR; ++j) *reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j) = make_float2(0.f, 0.f);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-
-    int id = lane < kRows && row0 + lane < P.batch ? P.ids[row0 + lane] : -1;
-    if (id >= L.count) id = -1;
-    const uint32_t named = __ballot_sync(0xFFFFFFFFu, id >= 0);
-    const int units = n / 32, worker = part * kWarps + warp, workers = parts * kWarps;
-    const int u0 = (int)((long long)units * worker / workers), u1 = (int)((long long)units * (worker + 1) / workers);
-    uint32_t mine = 0u;                                                         // rows whose adapter this cluster has taken
-    int turn = 0;
-    for (uint32_t left = named; left != 0u; ++turn) {
-        const int cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
-        const uint32_t match = __ballot_sync(0xFFFFFFFFu, id == cur);
-        left &= ~match;
-        if (turn % P.shares != share) continue;
-        mine |= match;
-        const __half* a = L.a + ((size_t)cur * rank + gq) * n + 8 * tq;
-        const __half* x = L.x + (size_t)(row0 + gq) * n + 8 * tq;
-        const bool has[2] = {(match >> gq & 1u) != 0u, (match >> (8 + gq) & 1u) != 0u};   // (other rows' x is not needed)
-        float acc[NR][4] = {};
-        struct Loads {
-            uint4 x[2], a[NR];
-        };
-        auto load = [&](Loads& l, int u) {
-            const bool in = u < u1;
-            const size_t col = (size_t)u * 32;
-#pragma unroll
-            for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? *reinterpret_cast<const uint4*>(x + (size_t)(8 * m) * n + col) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
-        };
-        auto multiply = [&](const Loads& l) {
-#pragma unroll
-            for (int j = 0; j < NR; ++j) mma_f16(acc[j], l.x[0].x, l.x[1].x, l.x[0].y, l.x[1].y, l.a[j].x, l.a[j].y);
-#pragma unroll
-            for (int j = 0; j < NR; ++j) mma_f16(acc[j], l.x[0].z, l.x[1].z, l.x[0].w, l.x[1].w, l.a[j].z, l.a[j].w);
-        };
-        auto flush = [&]() {
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int j = 0; j < NR; ++j) {
-                    float2* at = reinterpret_cast<float2*>(own + 8 * m * kRanks + 8 * j);
-                    if (has[m]) {
-                        const float2 old = *at;
-                        *at = make_float2(old.x + acc[j][2 * m], old.y + acc[j][2 * m + 1]);
-                    }
-                    acc[j][2 * m] = acc[j][2 * m + 1] = 0.f;
-                }
-        };
-        Loads even, odd;
-        load(even, u0);
-        int pairs = 0;
-#pragma unroll 1
-        for (int u = u0; u < u1; u += 2) {
-            load(odd, u + 1);
-            multiply(even);
-            load(even, u + 2);
-            multiply(odd);
-            if (++pairs % 4 == 0) flush();
-        }
-        if (pairs % 4 != 0) flush();
-    }
-    const uint32_t bare = share == 0 ? ~named : 0u;                        // their u is zero: the first cluster's
-    if (mine == 0u && bare == 0u) return;                                       // (the whole cluster agrees)
-    __syncthreads();
-    for (int e = threadIdx.x; e < kRows * kRanks; e += kThreads) {
-        float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) s += red[w * kRows * kRanks + e];
-        red[e] = s;                                                             // (nobody else touches element e of any warp's part)
-    }
-    cluster.sync();
-    for (int e = part * kThreads + threadIdx.x; e < kRows * kRanks / 4; e += parts * kThreads) {
-        const int row = e / (kRanks / 4), j = e % (kRanks / 4) * 4;
-        if (j >= rank || row0 + row >= P.batch || !(((mine | bare) >> row) & 1u)) continue;
-        store_4(L.u + (size_t)(row0 + row) * rank + j, cluster_sum(cluster, red, parts, e), rank - j, rank % 4 == 0);
-    }
-    cluster.sync();                                                             // (shared memory stays until all have read it)
-}
-
 // ---- asynchronous copies to shared memory --------------------------------------------------------------------
 
 __device__ __forceinline__ void copy_async_16(void* dst, const void* src, bool valid) {   // (not valid: zeros)
@@ -223,23 +119,25 @@ __device__ __forceinline__ uint4 load_8(const __half* src, int n) {
     }
 }
 
-// ---- u[t] = A[id_t] x[t], more rows ----------------------------------------------------------------------------
-
-// The same for more rows: a CTA takes 16 * WM of them, WM warps side by side, so that the factor's columns in shared memory serve all; 8 / WM such groups of warps
-// and the CTAs of a cluster cut the contraction.  x and the factor come through a ring of asynchronous copies, 64 columns (a line of memory) per group of
-// warps and stage; what bounds such copies is the number of lines that an instruction touches.
-// Bound: x from memory; from rank 64 on the reads of the factor from shared memory as well.
+// A cluster takes a tile of 16 * WM rows; 8 / WM groups of WM warps side by side and the CTAs of the cluster cut the contraction into parts, which meet in shared
+// memory, then over the cluster, in a fixed order.  Products are m16n8k16 MMAs of fp16 operands, rows by ranks.  x and the factor come through a ring of
+// asynchronous copies, 64 columns (a line of memory) per group of warps and stage.  The order of a contraction is free, so a lane takes 8 consecutive columns
+// of each of its rows (one 16-byte read) as the four operand words of two MMAs.
+// Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own; warps without rows of an
+// adapter sit it out.  Several clusters share the adapters of a tile.
+// The tensor core truncates when it accumulates: after 16 MMAs the sums go to other registers.
+// Bound: x from memory; from rank 64 on the reads of the factor from L2 and from shared memory as well.
 template <int NR, int WM>
-struct Tile {
+struct Narrow {
     static constexpr int kRows = 16 * WM, kRanks = 8 * NR, WK = kWarps / WM;
     static constexpr int kABytes = WK * kRanks * 128, kStageBytes = kABytes + kWarps * 4 * 32 * 16;
-    static constexpr int kPerSm = NR <= 8 ? 2 : 1, kStages = kPerSm == 1 || kStageBytes <= 27 * 1024 ? 4 : 3;
+    static constexpr int kPerSm = NR <= 8 ? 2 : 1, kFit = 226 * 1024 / kPerSm / kStageBytes, kStages = kFit < 4 ? kFit : 4;
     static constexpr int kBytes = kStages * kStageBytes;
     static_assert(WK * kRows * kRanks * 4 <= kBytes && kPerSm * (kBytes + 1024) <= 228 * 1024 && kBytes <= 227 * 1024, "the sums fit, and so many CTAs per SM");
 };
 template <int NR, int WM>
-__global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_kernel(const __grid_constant__ NarrowParams P) {
-    using T = Tile<NR, WM>;
+__global__ void __launch_bounds__(kThreads, (Narrow<NR, WM>::kPerSm)) narrow_kernel(const __grid_constant__ NarrowParams P) {
+    using T = Narrow<NR, WM>;
     extern __shared__ __align__(16) unsigned char smem[];
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -307,9 +205,9 @@ __global__ void __launch_bounds__(kThreads, (Tile<NR, WM>::kPerSm)) narrow_tile_
 #pragma unroll
                     for (int i = 0; i < kCopies; ++i) {
                         constexpr int kPer = T::kRanks >= 32 ? T::kRanks / 32 : 1;      // copies of 32 rows to a group of warps
-                        const int k = T::kRanks >= 32 ? i / kPer : j0 / T::kRanks, j = (T::kRanks >= 32 ? i % kPer * 32 : 0) + j0 % T::kRanks;
+                        const int k = T::kRanks >= 32 ? i / kPer : i * (32 / T::kRanks) + j0 / T::kRanks, j = (T::kRanks >= 32 ? i % kPer * 32 : 0) + j0 % T::kRanks;
                         const bool in = j < rank && (whole || (chunk0 + k < c1 && (chunk0 + k) * 64 + piece * 8 < n));
-                        const __half* src = a0 + (size_t)it * (T::WK * 64) + (T::kRanks >= 32 ? (size_t)(i % kPer) * rows32 + i / kPer * 64 : 0);
+                        const __half* src = a0 + (size_t)it * (T::WK * 64) + (T::kRanks >= 32 ? (size_t)(i % kPer) * rows32 + i / kPer * 64 : (size_t)(i * (32 / T::kRanks) * 64));
                         copy_async_16(stage + (k * T::kRanks + j) * 128 + ((piece ^ ((j & 1) << 2)) << 4), in ? src : L.a, in);
                     }
                 }
@@ -821,6 +719,8 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
                 s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
             const int r = e / (kRanks / 4), j = e % (kRanks / 4) * 4;
+            // (beyond the rank an infinite x has met zeros)
+            s = make_float4(j < rank ? s.x : 0.f, j + 1 < rank ? s.y : 0.f, j + 2 < rank ? s.z : 0.f, j + 3 < rank ? s.w : 0.f);
             const float back = split_row<R16>(us, r, j / 4, s);
             if (j == 0) backs[r] = back;
             if (part == 0 && j < rank && rows[r] >= 0) store_4(L.u + (size_t)rows[r] * rank + j, s, rank - j, rank % 4 == 0);
@@ -902,7 +802,7 @@ __device__ __forceinline__ void ldmatrix_trans(uint32_t (&r)[4], uint32_t at) {
 // with the rows inside, so low is turned when it is split).  A warp takes 16 ranks and 64 columns, GROUPS warps the same columns; 16 warps, because what a
 // tile costs beside its MMAs (copies, splitting, barriers) is then shared by 256 columns.  The rows of a
 // cluster's adapter are dealt out to its CTAs in chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor
-// multiplied by zero (0 * NaN), then streams them through a ring of stages; the next tile is split beside the MMAs of the one at hand.
+// multiplied by zero (0 * NaN), then streams them through a ring of stages; the next tile is split beside the MMAs of the one at hand, half of the warps doing the one first, half the other.
 // Sums of a tile are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
 // Bound: v from memory; from rank 64 on the MMAs.
 template <int GROUPS, bool VEC>
@@ -925,7 +825,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
     // the lane's row of the 8 x 8 matrices that it names: of v rows of the tile by columns, of low ranks by rows of the tile
     const uint32_t v_at = smem32 + (uint32_t)((lane & 15) * F::kVStride + (wc * 64 + (lane >> 4) * 8) * 2);
     const uint32_t a_at = smem32 + (uint32_t)(F::kAAt + (group * 16 + (lane & 15)) * F::kAStride + (lane >> 4) * 16);
-    const bool split_first = (warp & 4) != 0;                                   // half of a scheduler's warps split while the others multiply
+    const bool prepare_first = (warp & 4) != 0;                                 // half of a scheduler's warps copy and split while the others multiply
     float sum[8][4] = {};
     for (long long base = 0; base < P.batch; base += (long long)kFactorList * parts) {
         // the rows of this round that are the adapter's, in order
@@ -1006,8 +906,11 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
         for (int tile = 0; tile < n_tiles; ++tile) {
             copy_async_wait<F::kStages - 3>();
             __syncthreads();                                                    // the next tile is there, this one is split, and the slots of the one before are free
-            fetch(tile + F::kStages - 1);
-            if (split_first) split(tile + 1);
+            auto prepare = [&]() {
+                fetch(tile + F::kStages - 1);
+                split(tile + 1);
+            };
+            if (prepare_first) prepare();
             const uint32_t v = v_at + (uint32_t)(tile % F::kStages * F::kStageBytes), a = a_at + (uint32_t)((tile & 1) * 2 * F::kABytes);
             float acc[8][4];
 #pragma unroll
@@ -1031,7 +934,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
             for (int q = 0; q < 8; ++q)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[q][e] = fmaf(e < 2 ? back0 : back1, acc[q][e], sum[q][e]);
-            if (!split_first) split(tile + 1);
+            if (!prepare_first) prepare();
         }
         copy_async_wait<0>();
         __syncthreads();                                                        // (the list is written again)
@@ -1114,20 +1017,21 @@ cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, boo
 int shares_for(int batch) { return batch < 2048 ? 4 : 2; }
 
 cudaError_t launch_narrow(NarrowParams& P, int n_layers, int max_rank, cudaStream_t stream) {
-    const int wm = P.batch <= 256 ? 1 : P.batch < 2048 ? 4 : 8;                 // 16, 64 or 128 rows to a tile
+    const int wm = P.batch * (long long)n_layers <= 512 ? 2 : P.batch < 2048 ? 4 : 8;   // 32, 64 or 128 rows to a tile
     const long long tiles = (P.batch + 16 * wm - 1) / (16 * wm);
     P.shares = shares_for(P.batch);
     int c = kMaxCluster;
     while (c > 1 && tiles * n_layers * c > 400) c /= 2;
     const dim3 grid((unsigned)(tiles * c), (unsigned)P.shares, (unsigned)n_layers);
-    auto small = [&](auto kernel, int nr) { return launch(kernel, grid, c, kWarps * kNarrowRows * 8 * nr * 4, true, P, stream); };
-    if (wm == 1) return max_rank <= 16 ? small(narrow_kernel<2>, 2) : max_rank <= 32 ? small(narrow_kernel<4>, 4) : max_rank <= 64 ? small(narrow_kernel<8>, 8) : small(narrow_kernel<16>, 16);
     auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, c, bytes, true, P, stream); };
+    if (wm == 2)
+        return max_rank <= 16 ? go(narrow_kernel<2, 2>, Narrow<2, 2>::kBytes) : max_rank <= 32 ? go(narrow_kernel<4, 2>, Narrow<4, 2>::kBytes)
+             : max_rank <= 64 ? go(narrow_kernel<8, 2>, Narrow<8, 2>::kBytes) : go(narrow_kernel<16, 2>, Narrow<16, 2>::kBytes);
     if (wm == 4)
-        return max_rank <= 16 ? go(narrow_tile_kernel<2, 4>, Tile<2, 4>::kBytes) : max_rank <= 32 ? go(narrow_tile_kernel<4, 4>, Tile<4, 4>::kBytes)
-             : max_rank <= 64 ? go(narrow_tile_kernel<8, 4>, Tile<8, 4>::kBytes) : go(narrow_tile_kernel<16, 4>, Tile<16, 4>::kBytes);
-    return max_rank <= 16 ? go(narrow_tile_kernel<2, 8>, Tile<2, 8>::kBytes) : max_rank <= 32 ? go(narrow_tile_kernel<4, 8>, Tile<4, 8>::kBytes)
-         : max_rank <= 64 ? go(narrow_tile_kernel<8, 8>, Tile<8, 8>::kBytes) : go(narrow_tile_kernel<16, 8>, Tile<16, 8>::kBytes);
+        return max_rank <= 16 ? go(narrow_kernel<2, 4>, Narrow<2, 4>::kBytes) : max_rank <= 32 ? go(narrow_kernel<4, 4>, Narrow<4, 4>::kBytes)
+             : max_rank <= 64 ? go(narrow_kernel<8, 4>, Narrow<8, 4>::kBytes) : go(narrow_kernel<16, 4>, Narrow<16, 4>::kBytes);
+    return max_rank <= 16 ? go(narrow_kernel<2, 8>, Narrow<2, 8>::kBytes) : max_rank <= 32 ? go(narrow_kernel<4, 8>, Narrow<4, 8>::kBytes)
+         : max_rank <= 64 ? go(narrow_kernel<8, 8>, Narrow<8, 8>::kBytes) : go(narrow_kernel<16, 8>, Narrow<16, 8>::kBytes);
 }
 
 template <int R16, bool VEC>

@@ -6,8 +6,9 @@
 // launch, and scales its share.  Bound: memory (4 bytes in, 4 out per element; the second reading hits L2 up to its size).
 // Squares are taken and summed in 64 bits: an fp32 gradient of 1e20 has no fp32 square, and the conversion and the double add cost less than the bytes.
 #include <algorithm>
-#include <cstring>
+#include <memory>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "rabit_internal.h"
@@ -114,10 +115,16 @@ size_t chunks_of(const size_t* counts, int n) {
 
 }  // namespace
 
+struct Span {
+    uintptr_t at, end;
+    bool written;
+};
+
 struct rabit_gradients {
     int device, n_chunks, grid;
     const Chunk* chunks;
     double* partial;
+    std::vector<Span> spans;                          // all memory of a call, by its start
 };
 
 // table of chunks | one partial sum per CTA
@@ -144,10 +151,6 @@ static int bind_call(const float* const* tensors, float* const* outs, const size
     const size_t need = rabit_gradients_bytes(counts, n), table_bytes = rabit_align256(n_chunks * sizeof(Chunk));
     if (dev_bytes < need) return rabit_fail(RABIT_BUFFER_TOO_SMALL, "%s: dev_buf holds %zu bytes, need %zu", who, dev_bytes, need);
     // what is written overlaps nothing else: a sweep over all ranges by their starts
-    struct Span {
-        uintptr_t at, end;
-        bool written;
-    };
     std::vector<Span> spans;
     spans.push_back({(uintptr_t)dev_buf, (uintptr_t)dev_buf + need, true});
     for (int i = 0; i < n; ++i) {
@@ -177,13 +180,14 @@ static int bind_call(const float* const* tensors, float* const* outs, const size
     if (!table.empty()) RABIT_CUDA_TRY(cudaMemcpyAsync(dev_buf, table.data(), table.size() * sizeof(Chunk), cudaMemcpyHostToDevice, (cudaStream_t)stream));
     int sms = 0;
     RABIT_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, attr.device));
-    rabit_gradients* R = new rabit_gradients;
+    std::unique_ptr<rabit_gradients> R(new rabit_gradients);
     R->device = attr.device;
     R->n_chunks = (int)n_chunks;
     R->grid = (int)std::max<size_t>(1, std::min<size_t>(n_chunks, std::min(8 * sms, kMaxGrid)));
     R->chunks = (const Chunk*)dev_buf;
     R->partial = (double*)((char*)dev_buf + table_bytes);
-    *out = R;
+    R->spans = std::move(spans);
+    *out = R.release();
     return RABIT_OK;
 }
 
@@ -196,6 +200,8 @@ extern "C" int rabit_clip_gradients(const rabit_gradients* R, float max_norm, fl
     rabit_clear_error();
     if (!R || !norm_out || (((uintptr_t)norm_out) & 3u)) return rabit_fail(RABIT_INVALID_ARG, "%s: gradients or norm_out is NULL or misaligned", who);
     if (!(max_norm > 0.f) || !(max_norm <= 3.402823466e38f)) return rabit_fail(RABIT_INVALID_ARG, "%s: max_norm must be positive and finite", who);
+    for (const Span& s : R->spans)
+        if (rabit_ranges_overlap((const void*)s.at, s.end - s.at, norm_out, 4)) return rabit_fail(RABIT_INVALID_ARG, "%s: norm_out lies in a gradient, an output or dev_buf", who);
     int dev = -1;
     RABIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev != R->device) return rabit_fail(RABIT_INVALID_ARG, "%s: the gradients live on device %d but device %d is current", who, R->device, dev);

@@ -47,7 +47,7 @@ def _transposed_planes(L):
 def _within(got, want, bound, what):
     got = got.astype(np.float64)
     assert got.shape == want.shape
-    off = np.abs(got - want) > bound
+    off = ~(np.abs(got - want) <= bound)                                    # (a NaN is off)
     if off.any():
         at = tuple(np.argwhere(off)[0])
         raise AssertionError(f"{what}{list(at)}: {got[at]:.8g}, want {want[at]:.8g}, off {abs(got[at] - want[at]):.3g} > {bound[at]:.3g} ({int(off.sum())} of {off.size})")
@@ -56,7 +56,8 @@ def _within(got, want, bound, what):
 CASES = [(2, 128, 64, 1, 8, 2, "one"), (1, 33, 32, 2, 1, 1, "one"), (2, 100, 160, 3, 3, 4, "mixed"), (3, 129, 1184, 5, 16, 3, "mixed"), (2, 256, 512, 8, 12, 9, "mixed"),
          (2, 1000, 96, 9, 17, 3, "mixed"), (2, 72, 2080, 16, 64, 16, "mixed"), (2, 520, 1024, 17, 16, 4, "prompts"), (1, 1031, 640, 31, 128, 2, "mixed"), (2, 300, 4096, 33, 8, 40, "mixed"),
          (2, 264, 736, 64, 33, 3, "prompts"), (3, 136, 320, 65, 16, 5, "mixed"), (2, 520, 256, 128, 64, 2, "one"), (2, 97, 288, 130, 5, 7, "mixed"), (2, 640, 1056, 257, 16, 3, "prompts"),
-         (2, 200, 544, 515, 100, 2, "prompts"), (1, 64, 8224, 12, 24, 3, "mixed"), (2, 128, 128, 40, 16, 2, "none"), (2, 1032, 64, 300, 128, 5, "mixed")]
+         (2, 200, 544, 515, 100, 2, "prompts"), (1, 64, 8224, 12, 24, 3, "mixed"), (2, 128, 128, 40, 16, 2, "none"), (2, 1032, 64, 300, 128, 5, "mixed"), (2, 96, 160, 2100, 24, 3, "prompts"),
+         (1, 40, 416, 600, 70, 4, "mixed"), (1, 264, 96, 2500, 16, 2, "mixed"), (2, 33, 352, 480, 40, 3, "prompts"), (3, 100, 224, 90, 9, 30, "mixed"), (2, 1000, 288, 48, 20, 50, "mixed")]
 
 
 @pytest.mark.parametrize("K,M,N,batch,r,n,kind", CASES)
@@ -243,6 +244,56 @@ def test_captured_replayed_and_on_another_stream():
     layer.free()
 
 
+def test_offsets_beyond_32_bits():
+    """A pool of 4.4 GB whose last adapter is named, and its gradient of 8.8 GB."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    M, N, r, n = 64, 8192, 64, 4200
+    L = make_layer(M, N, 1, key=(102,))
+    a, b, _ = _pool(M, N, 1, r, 30)
+    big, out = torch.zeros((n, r, N), dtype=torch.float16, device="cuda"), torch.zeros((n, r, M), dtype=torch.float16, device="cuda")
+    big[-1], out[-1] = _cuda(a[0], b[0])
+    scale = torch.full((n,), 1.5, device="cuda")
+    A, layer = rabit.RabitAdapters(big, out, scale), rabit.rabit_pack(L.planes, L.g, L.h)
+    for batch in (3, 70, 300):
+        x = make_x(batch, N, key=(102, batch))
+        ids = np.full(batch, n - 1, np.int32)
+        u = torch.empty((batch, r), dtype=torch.float32, device="cuda")
+        y = rabit.rabit_linear_adapted(layer, A, *_cuda(x, ids), None, u)
+        want, want_u, err, err_u = ao.adapted(L.planes, L.g, L.h, a, b, [1.5], x, np.zeros(batch, np.int32))
+        _within(y.cpu().numpy(), want, err, "y")
+        _within(u.cpu().numpy(), want_u, err_u, "u")
+    rng = np.random.default_rng(31)
+    dy, p = rng.standard_normal((batch, M)).astype(np.float16), rng.standard_normal((batch, r)).astype(np.float32)
+    da, db = rabit.rabit_adapter_gradients(A, *_cuda(x, u.cpu().numpy(), dy, p, ids))
+    _within(da[-1].cpu().numpy()[None], *ao.gradients([1.5], x, p, np.zeros(batch, np.int32), 1), "da")
+    _within(db[-1].cpu().numpy()[None], *ao.gradients([1.5], dy, u.cpu().numpy(), np.zeros(batch, np.int32), 1), "db")
+    assert not da[:-1].any() and not db[:-1].any()
+    layer.free()
+
+
+def test_infinite_x_beside_a_rank_that_is_no_multiple():
+    """One rank, one infinity: y is infinite where the factors are not zero, not NaN."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    M, N = 64, 96
+    L = make_layer(M, N, 1, key=(103,))
+    L.planes[:] = 0
+    a, b, scale = np.ones((1, 1, N), np.float16), np.ones((1, 1, M), np.float16), np.ones(1, np.float32)
+    layer = rabit.rabit_pack(L.planes, L.g, L.h)
+    for batch in (1, 100, 400):
+        x = np.abs(make_x(batch, N, key=(103, batch)))
+        x[0, 0] = np.inf
+        u = torch.empty((batch, 1), dtype=torch.float32, device="cuda")
+        y = rabit.rabit_linear_adapted(layer, _adapters(a, b, scale), *_cuda(x, np.zeros(batch, np.int32)), None, u)
+        base = rabit.rabit_linear(layer, *_cuda(x))
+        torch.cuda.synchronize()
+        assert torch.isinf(u[0]).all() and (u[1:] < 1e5).all()
+        assert torch.isfinite(y[1:]).all() and not torch.isfinite(y[0]).any()
+        assert torch.equal(torch.isnan(y[0]), torch.isnan(base[0]))
+    layer.free()
+
+
 def test_adapted_refusals():
     import torch
     import paper_2602_05367_b200 as rabit
@@ -330,7 +381,8 @@ def test_transpose_refusals():
 
 
 GRADIENT_CASES = [(32, 64, 1, 1, 1, "one"), (64, 32, 3, 8, 2, "mixed"), (1000, 96, 17, 16, 3, "mixed"), (33, 104, 40, 5, 4, "mixed"), (264, 640, 64, 33, 2, "prompts"),
-                  (128, 1056, 77, 64, 3, "mixed"), (136, 320, 300, 128, 2, "prompts"), (256, 520, 1000, 16, 1, "one"), (96, 64, 2500, 12, 5, "prompts"), (72, 200, 513, 17, 9, "mixed"), (64, 64, 20, 16, 2, "none")]
+                  (128, 1056, 77, 64, 3, "mixed"), (136, 320, 300, 128, 2, "prompts"), (256, 520, 1000, 16, 1, "one"), (96, 64, 2500, 12, 5, "prompts"), (72, 200, 513, 17, 9, "mixed"), (64, 64, 20, 16, 2, "none"), (64, 96, 9000, 8, 1, "one"), (40, 72, 9000, 40, 3, "mixed"),
+                  (36, 44, 700, 7, 60, "mixed")]
 
 
 @pytest.mark.parametrize("M,N,batch,r,n,kind", GRADIENT_CASES)
@@ -489,6 +541,9 @@ def test_clipping_replayed_and_refused():
             rabit.RabitGradients(*args)
     with pytest.raises(rabit.RabitError):
         rabit.RabitGradients([src, src[5:]])
+    for inside in (src[5:6], dst[-1:], G.dev_buf[:4].view(torch.float32)):
+        with pytest.raises(rabit.RabitError, match="norm_out"):
+            rabit.rabit_clip_gradients(G, 1.0, inside)
     G.free()
     with pytest.raises(rabit.RabitError):
         rabit.rabit_clip_gradients(G, 1.0)
