@@ -825,6 +825,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
     // the lane's row of the 8 x 8 matrices that it names: of v rows of the tile by columns, of low ranks by rows of the tile
     const uint32_t v_at = smem32 + (uint32_t)((lane & 15) * F::kVStride + (wc * 64 + (lane >> 4) * 8) * 2);
     const uint32_t a_at = smem32 + (uint32_t)(F::kAAt + (group * 16 + (lane & 15)) * F::kAStride + (lane >> 4) * 16);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const bool prepare_first = (warp & 4) != 0;                                 // half of a scheduler's warps copy and split while the others multiply
     float sum[8][4] = {};
     for (long long base = 0; base < P.batch; base += (long long)kFactorList * parts) {
@@ -948,11 +949,15 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
             *reinterpret_cast<float2*>(sums + (slice * F::kRanks + group * 16 + gq + 4 * e) * F::kCols + wc * 64 + 8 * q + 2 * tq) = make_float2(sum[q][e], sum[q][e + 1]);
     if (F::kSlices > 1) {
         __syncthreads();
-        for (int e = threadIdx.x; e < F::kRanks * F::kCols; e += kFactorThreads) {
-            float total = sums[e];
+        float4* fours_of = reinterpret_cast<float4*>(sums);
+        for (int e = threadIdx.x; e < F::kRanks * F::kCols / 4; e += kFactorThreads) {
+            float4 total = fours_of[e];
 #pragma unroll
-            for (int q = 1; q < F::kSlices; ++q) total += sums[q * F::kRanks * F::kCols + e];
-            sums[e] = total;
+            for (int q = 1; q < F::kSlices; ++q) {
+                const float4 v = fours_of[q * (F::kRanks * F::kCols / 4) + e];
+                total.x += v.x; total.y += v.y; total.z += v.z; total.w += v.w;
+            }
+            fours_of[e] = total;
         }
     }
     cluster.sync();
@@ -984,7 +989,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
 // ---- launches ----------------------------------------------------------------------------------------------
 
 template <typename Params>
-cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, bool dependent, const Params& P, cudaStream_t stream, int threads = kThreads) {
+cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, const Params& P, cudaStream_t stream, int threads = kThreads) {
     if (smem > 48 * 1024) {                                                     // (an attribute of the function on the current device; setting it again is cheap)
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
@@ -1005,11 +1010,9 @@ cudaError_t launch(void (*kernel)(Params), dim3 grid, int cluster, int smem, boo
         attr[cfg.numAttrs].val.clusterDim = {(unsigned)cluster, 1, 1};
         ++cfg.numAttrs;
     }
-    if (dependent) {
-        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-        ++cfg.numAttrs;
-    }
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
     return cudaLaunchKernelEx(&cfg, kernel, P);
 }
 
@@ -1023,7 +1026,7 @@ cudaError_t launch_narrow(NarrowParams& P, int n_layers, int max_rank, cudaStrea
     int c = kMaxCluster;
     while (c > 1 && tiles * n_layers * c > 400) c /= 2;
     const dim3 grid((unsigned)(tiles * c), (unsigned)P.shares, (unsigned)n_layers);
-    auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, c, bytes, true, P, stream); };
+    auto go = [&](auto kernel, int bytes) { return launch(kernel, grid, c, bytes, P, stream); };
     if (wm == 2)
         return max_rank <= 16 ? go(narrow_kernel<2, 2>, Narrow<2, 2>::kBytes) : max_rank <= 32 ? go(narrow_kernel<4, 2>, Narrow<4, 2>::kBytes)
              : max_rank <= 64 ? go(narrow_kernel<8, 2>, Narrow<8, 2>::kBytes) : go(narrow_kernel<16, 2>, Narrow<16, 2>::kBytes);
@@ -1042,7 +1045,7 @@ cudaError_t launch_widen(WidenParams& P, int n_layers, int max_m, cudaStream_t s
     const long long along = std::min(std::max(296 / (cols * n_layers), 1LL), 65535LL);
     P.blocks = (int)((row_blocks + along - 1) / along);
     const dim3 grid((unsigned)cols, (unsigned)((row_blocks + P.blocks - 1) / P.blocks), (unsigned)n_layers);
-    return launch(widen_kernel<R16, VEC>, grid, 0, W::kBytes, true, P, stream);
+    return launch(widen_kernel<R16, VEC>, grid, 0, W::kBytes, P, stream);
 }
 
 template <int R16, bool VEC>
@@ -1054,7 +1057,7 @@ cudaError_t launch_decode(const DecodeParams& P, int n_layers, int max_count, cu
     int c = Decode<R16>::kCluster;
     while (c > 2 && (long long)items * n_layers * c > (R16 == 1 ? 296 : 222)) c /= 2;
     const dim3 grid((unsigned)(gather ? c : items / 4 * c), (unsigned)(gather ? items : 4), (unsigned)n_layers);
-    return gather ? launch(decode_kernel<R16, VEC, true>, grid, c, Decode<R16>::kBytes, true, P, stream) : launch(decode_kernel<R16, VEC, false>, grid, c, Decode<R16>::kBytes, true, P, stream);
+    return gather ? launch(decode_kernel<R16, VEC, true>, grid, c, Decode<R16>::kBytes, P, stream) : launch(decode_kernel<R16, VEC, false>, grid, c, Decode<R16>::kBytes, P, stream);
 }
 
 template <int GROUPS>
@@ -1072,7 +1075,7 @@ cudaError_t launch_factor(FactorParams& P, int count, cudaStream_t stream) {
         if (cost < least) { least = cost; c = q; }
     }
     const dim3 grid((unsigned)(blocks * c), (unsigned)count);
-    return vec ? launch(factor_kernel<GROUPS, true>, grid, c, F::kBytes, false, P, stream, kFactorThreads) : launch(factor_kernel<GROUPS, false>, grid, c, F::kBytes, false, P, stream, kFactorThreads);
+    return vec ? launch(factor_kernel<GROUPS, true>, grid, c, F::kBytes, P, stream, kFactorThreads) : launch(factor_kernel<GROUPS, false>, grid, c, F::kBytes, P, stream, kFactorThreads);
 }
 
 int check_pool(const char* who, const rabit_adapters* A) {

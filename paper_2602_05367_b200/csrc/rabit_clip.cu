@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Chunk* __restri
     __shared__ double warps[kThreads / 32];
     double sum = 0.0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     Chunk next = (int)blockIdx.x < n_chunks ? chunks[blockIdx.x] : Chunk{};
     for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
         const Chunk ch = next;
@@ -206,8 +207,6 @@ extern "C" int rabit_clip_gradients(const rabit_gradients* R, float max_norm, fl
     RABIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev != R->device) return rabit_fail(RABIT_INVALID_ARG, "%s: the gradients live on device %d but device %d is current", who, R->device, dev);
     cudaStream_t st = (cudaStream_t)stream;
-    squares_kernel<<<R->grid, kThreads, 0, st>>>(R->chunks, R->n_chunks, R->partial);
-    cudaError_t e = cudaGetLastError();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)R->grid);
     cfg.blockDim = dim3(kThreads);
@@ -217,6 +216,7 @@ extern "C" int rabit_clip_gradients(const rabit_gradients* R, float max_norm, fl
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, squares_kernel, R->chunks, R->n_chunks, R->partial);
     if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, scale_kernel, R->chunks, R->n_chunks, (const double*)R->partial, (double)max_norm, norm_out);
     if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return RABIT_OK;
