@@ -406,7 +406,7 @@ struct DecodeParams {
     const int* ids;
     int batch;
 };
-constexpr int kDecodeRows = 256, kDecodeRowsOdd = 64;            // most rows of a batch; of one whose outputs are not 16-byte pieces
+constexpr int kDecodeRows = 256, kGatherRows = 64;                              // most rows of a batch; of one whose rows are put together by adapter
 
 // A CTA takes 512 columns (256 beyond rank 64), a warp 64 (32) of them, and blocks of 32 rows one after the other: rows by columns as m16n8k16 MMAs over the rank, the
 // factor's fragments in registers for all rows, a row of u as two fp16 parts of a common power of two.  The order of columns in MMA tiles and of ranks is
@@ -549,7 +549,6 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
 // CTAs taking columns in turn.  The CTAs send their sums of u to one another, so one cluster barrier lies between the two steps; the factor's first entries
 // and y of the second are fetched before it.  One launch instead of two around the layer saves a launch's latency and the way of u through memory.
 // Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y): few instructions on the way count, not bytes.
-constexpr int kGatherRows = 64;
 template <int R16>
 struct Decode {
     static constexpr int kRows = 16, kRanks = 16 * R16, kCluster = 8;   // (most CTAs of a cluster)
@@ -1164,9 +1163,19 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         return e;
     };
     if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
+    // One launch behind the layer, or two around it?  The one reads the second factor again for every 16 rows, so rows times outputs decide (B200, us beyond the
+    // layer alone, one launch against two: 200 rows of 4096 x 4096 rank 16 to 32 9.8 / 15.1, 256 rows 9.9 / 11.8, 200 rows of 14336 x 4096 23 / 12; rank 64, 130 rows of
+    // 4096 x 4096 15.0 / 17.7, 65 rows of 14336 x 4096 17.9 / 13.3).  Outputs that are not 16-byte pieces are slow in the one: up to 64 rows only.
     bool vec = true;
-    for (int l = 0; l < n_layers; ++l) vec = vec && (!adapters[l] || adapters[l]->n_out % 8 == 0);
-    const bool decode = batch <= (vec ? kDecodeRows : kDecodeRowsOdd);
+    long long outputs = 0;
+    int most_rank = 0;
+    for (int l = 0; l < n_layers; ++l) {
+        if (!adapters[l]) continue;
+        vec = vec && adapters[l]->n_out % 8 == 0;
+        outputs += adapters[l]->n_out;
+        most_rank = std::max(most_rank, adapters[l]->rank);
+    }
+    const bool decode = batch <= kGatherRows || (vec && batch <= kDecodeRows && batch * outputs <= (most_rank <= 32 ? 1LL << 20 : 3LL << 18));
     cudaError_t e = cudaSuccess;
     if (!decode) {
         e = each_group([&] {
