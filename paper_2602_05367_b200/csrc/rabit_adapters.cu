@@ -3,7 +3,10 @@
 //   u[t] = A[id_t] x[t],   y[t] = layer(x[t]) + scale[id_t] * B[id_t]^T u[t]
 //   da[i] = scale[i] * sum_{t: id_t = i} p[t] x[t]^T,   db[i] = scale[i] * sum_{t: id_t = i} u[t] dy[t]^T
 //
-// Every factor is `rank` rows along a side of the layer, so both products of the forward pass and of the input gradient are the same two kernels.
+// Every factor is `rank` rows along a side of the layer, so both products of the forward pass and of the input gradient are the same kernels: narrow_kernel (a
+// side to the rank) and widen_kernel (the rank to a side) around the layer, or decode_kernel, both in one behind it, for few rows; the gradients are
+// factor_kernel.  All are MMAs of mma.sync: their products are a few per cent of the layer's, their inner or outer size is the rank (1 to 128),
+// and what bounds them is memory, latency or the instructions around the MMAs, not the tensor pipe (mma.sync reaches 537 TFLOP/s here).
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
@@ -105,17 +108,75 @@ template <int N>
 __device__ __forceinline__ void copy_async_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// 8 halves at src, of which those before `n` are inside; VEC: src is 16-byte aligned and all or none are
+// 8 halves at any place, of which those before `n` are inside their row, from the one or two aligned 16-byte pieces that hold them
+__device__ __forceinline__ uint4 extract_8(const uint4& lo, const uint4& hi, const __half* src, int n) {
+    const uint32_t skip = (uint32_t)(reinterpret_cast<uintptr_t>(src) >> 1) & 7u;   // halves of the first piece before src
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = skip & 4u ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = skip & 2u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = skip & 1u ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+        if (n < 8) w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? w[i] & 0xFFFFu : 0u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Both pieces to shared memory (`second` 16-byte units apart), asynchronously: what lies beyond `end`, the end of the buffer, or is not needed arrives as zeros and is
+// not read.
+__device__ __forceinline__ void copy_async_pieces(uint4* dst, int second, const __half* src, int n, const __half* end) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(src), piece = at & ~(uintptr_t)15, last = reinterpret_cast<uintptr_t>(end);
+    const bool two = n > 0 && (int)((at >> 1) & 7u) + min(n, 8) > 8;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uintptr_t from = piece + 16 * h;
+        const uint32_t size = (h == 0 ? n > 0 : two) ? (uint32_t)min((long long)16, (long long)(last - from)) : 0u;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + h * second)), "l"(size ? from : piece), "r"(size) : "memory");
+    }
+}
+// 8 halves at src, of which those before `n` are inside their row; `end` is the end of the buffer, which starts on 16 bytes.  VEC: src lies on 16 bytes and all or
+// none are inside.  Otherwise (rows of any length) aligned pieces are read, two loads instead of eight; halves one by one where a piece would reach
+// beyond the buffer.
 template <bool VEC>
-__device__ __forceinline__ uint4 load_8(const __half* src, int n) {
+__device__ __forceinline__ uint4 load_8(const __half* src, int n, const __half* end) {
     if constexpr (VEC) {
         return n > 0 ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
     } else {
-        uint32_t w[4] = {};
+        if (n <= 0) return make_uint4(0u, 0u, 0u, 0u);
+        const uintptr_t at = reinterpret_cast<uintptr_t>(src);
+        const uint4* piece = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+        const bool two = (int)((at >> 1) & 7u) + min(n, 8) > 8;
+        if (reinterpret_cast<const __half*>(piece + (two ? 2 : 1)) > end) {
+            uint32_t v[4] = {};
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (q < n) w[q >> 1] |= (uint32_t)__half_as_ushort(src[q]) << (16 * (q & 1));
-        return make_uint4(w[0], w[1], w[2], w[3]);
+            for (int q = 0; q < 8; ++q)
+                if (q < n) v[q >> 1] |= (uint32_t)__half_as_ushort(src[q]) << (16 * (q & 1));
+            return make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        return extract_8(piece[0], two ? piece[1] : make_uint4(0u, 0u, 0u, 0u), src, n);
+    }
+}
+// 8 halves to dst, those before `n`; VEC as above.  Otherwise in words of the 4-byte grid, with a half before and behind them where dst is odd.
+template <bool VEC>
+__device__ __forceinline__ void store_8(__half* dst, int n, const uint32_t (&v)[4]) {
+    if constexpr (VEC) {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
+        const bool odd = (reinterpret_cast<uintptr_t>(dst) & 2u) != 0u;
+        if (n < 8) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < n) dst[q] = __ushort_as_half((unsigned short)(v[q >> 1] >> (16 * (q & 1))));
+        } else if (odd) {
+            dst[0] = __ushort_as_half((unsigned short)v[0]);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) *reinterpret_cast<uint32_t*>(dst + 1 + 2 * i) = __funnelshift_r(v[i], v[i + 1], 16);
+            dst[7] = __ushort_as_half((unsigned short)(v[3] >> 16));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(dst + 2 * i) = v[i];
+        }
     }
 }
 
@@ -126,7 +187,8 @@ __device__ __forceinline__ uint4 load_8(const __half* src, int n) {
 // Rows of different adapters in one tile: the tile is multiplied with each adapter that occurs, and a row keeps the products of its own; warps without rows of an
 // adapter sit it out.  Several clusters share the adapters of a tile.
 // The tensor core truncates when it accumulates: after 16 MMAs the sums go to other registers.
-// Bound: x from memory; from rank 64 on the reads of the factor from L2 and from shared memory as well.
+// Bound: x from memory; from rank 64 on shared memory, which every warp reads the whole factor from for its 16 rows.  4096 rows of 4096 columns, rank 16: 14 us (33.5 MB
+// of x: 5.1 at the copy rate, then the start and the sum over the cluster, 2 us each); rank 64: 31 us, 1037 rows of 14336 columns: 31.
 template <int NR, int WM>
 struct Narrow {
     static constexpr int kRows = 16 * WM, kRanks = 8 * NR, WK = kWarps / WM;
@@ -371,7 +433,7 @@ struct Widen {
     static constexpr int kLanes = 4 * kGroups, kBlockPieces = kWidenRows * kLanes;   // 16-byte pieces of a warp's row of y, of its block
     // place of piece p of row r: two rows that a load touches, 64 bytes each, meet in no bank
     static __device__ __forceinline__ int piece(int r, int p) { return r * kLanes + (kLanes == 8 ? p ^ ((r & 1) << 2) : p); }
-    static constexpr int kRingBytes = 2 * kWarps * kBlockPieces * 16, kUBytes = kWidenRows * kRanks * 4;
+    static constexpr int kPlanes = VEC ? 1 : 2, kRingBytes = 2 * kPlanes * kWarps * kBlockPieces * 16, kUBytes = kWidenRows * kRanks * 4;
     static constexpr int kBytes = kRingBytes + kUBytes + Operand<R16>::pieces(kWidenRows) * 16 + kWidenRows * 4;
     static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs per SM");
 };
@@ -385,13 +447,7 @@ __device__ __forceinline__ void widen_store(__half* y, int n, const uint4& old, 
         const __half2 r = __floats2half2_rn(fmaf(scale, acc[q][2 * h], was.x), fmaf(scale, acc[q][2 * h + 1], was.y));
         v[q] = *reinterpret_cast<const uint32_t*>(&r);
     }
-    if (VEC) {
-        *reinterpret_cast<uint4*>(y) = make_uint4(v[0], v[1], v[2], v[3]);
-    } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (q < n) y[q] = __ushort_as_half((unsigned short)(v[q >> 1] >> (16 * (q & 1))));
-    }
+    store_8<VEC>(y, n, v);
 }
 
 struct DecodeLayer {
@@ -408,12 +464,13 @@ struct DecodeParams {
 };
 constexpr int kDecodeRows = 256, kGatherRows = 64;                              // most rows of a batch; of one whose rows are put together by adapter
 
-// A CTA takes 512 columns (256 beyond rank 64), a warp 64 (32) of them, and blocks of 32 rows one after the other: rows by columns as m16n8k16 MMAs over the rank, the
+// A CTA takes 512 columns (256 beyond rank 32), a warp 64 (32) of them, and blocks of 32 rows one after the other: rows by columns as m16n8k16 MMAs over the rank, the
 // factor's fragments in registers for all rows, a row of u as two fp16 parts of a common power of two.  The order of columns in MMA tiles and of ranks is
 // free: a lane's results are 8 consecutive columns of a row (one 16-byte access to y), its factor entries come from 16-byte loads, its u entries
 // are four consecutive ones.  A row belongs to one adapter, so y is read and written once; y, u and ids of the next block are on their way while this
 // one is multiplied (copies to shared memory: registers do not hold enough of y for the latency).
-// Bound: y, in and out; the instructions around the MMAs are as many as that leaves room for, which is why a warp takes 64 columns.
+// Bound: y, in and out; the instructions around the MMAs are as many as that leaves room for, which is why a warp takes 64 columns.  4096 rows of 11008 columns,
+// rank 16: 32 us (180 MB, 5.6 TB/s; with 32 columns to a warp 43, with y in registers only 51); rank 64 (32 columns to a warp, 64 spill): 74, of which 22 are MMAs.
 template <int R16, bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constant__ WidenParams P) {
     using W = Widen<R16, VEC>;
@@ -433,6 +490,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
     if ((int)blockIdx.x * W::kCols >= m_all) return;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
+    const __half *y_end = L.y + (size_t)batch * m_all, *b_end = L.b + (size_t)L.count * rank * m_all;
     const bool fours = rank % 4 == 0;
     const int c = col0 + 8 * tq;                                                // the lane's columns in y: 8 here and 8 in each further group
     ring += warp * W::kBlockPieces;
@@ -444,14 +502,14 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
         const int row0 = first_row + blk * kWidenRows;
         if (blk < blocks) {
             // rows of 8 * kLanes columns, kLanes lanes side by side: whole lines of memory where a warp has 64 columns
-            uint4* dst = ring + (blk & 1) * (kWarps * W::kBlockPieces);
+            uint4* dst = ring + (blk & 1) * (W::kPlanes * kWarps * W::kBlockPieces);
 #pragma unroll
             for (int t = 0; t < kWidenRows; t += 32 / W::kLanes) {
                 const int r = t + lane / W::kLanes, p = lane % W::kLanes, cols = m_all - col0 - 8 * p;
                 const bool in = row0 + r < batch && cols > 0;
                 const __half* src = in ? from + (size_t)t * m_all : L.y;
                 if (VEC) copy_async_16(dst + W::piece(r, p), src, in);
-                else dst[W::piece(r, p)] = load_8<false>(src, in ? cols : 0);
+                else copy_async_pieces(dst + W::piece(r, p), kWarps * W::kBlockPieces, src, in ? cols : 0, y_end);
             }
             for (int i = threadIdx.x; i < kWidenRows * W::kFours; i += kThreads) {
                 const int r = i / W::kFours, j = i % W::kFours * 4;
@@ -483,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
             for (int k = 0; k < R16; ++k) {
                 uint4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all, 16 * k + 4 * tq + i < rank ? m_all - cf : 0);
+                for (int i = 0; i < 4; ++i) v[i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all, 16 * k + 4 * tq + i < rank ? m_all - cf : 0, b_end);
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
                     f[k][g][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
@@ -512,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
         __syncthreads();
         y_from += 4 * eight;
         fetch(blk + 1, y_from);
-        const uint4* old = ring + (blk & 1) * (kWarps * W::kBlockPieces);
+        const uint4* old = ring + (blk & 1) * (W::kPlanes * kWarps * W::kBlockPieces);
         while (left != 0u) {
             if (cur != held) load_factor(held = cur);
             const uint32_t match = __ballot_sync(0xFFFFFFFFu, id == cur);
@@ -531,7 +589,11 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
                     const float factor = scale * backs[16 * mt + 8 * h + gq];
 #pragma unroll
                     for (int g = 0; g < G; ++g)
-                        if (c + 32 * g < m_all) widen_store<VEC>(y + (2 * mt + h) * eight + 32 * g, m_all - c - 32 * g, old[W::piece(16 * mt + 8 * h + gq, 4 * g + tq)], acc[g], h, factor);
+                        if (c + 32 * g < m_all) {
+                            __half* to = y + (2 * mt + h) * eight + 32 * g;
+                            const uint4* was = old + W::piece(16 * mt + 8 * h + gq, 4 * g + tq);
+                            widen_store<VEC>(to, m_all - c - 32 * g, VEC ? *was : extract_8(was[0], was[(W::kPlanes - 1) * kWarps * W::kBlockPieces], to, m_all - c - 32 * g), acc[g], h, factor);
+                        }
                 }
             }
             if (left != 0u) cur = __shfl_sync(0xFFFFFFFFu, id, __ffs(left) - 1);
@@ -541,20 +603,79 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
     copy_async_wait<0>();
 }
 
-// ---- both steps in one launch, up to 64 rows -------------------------------------------------------------------
+// ---- both steps in one launch, for few rows --------------------------------------------------------------------
 
 // Up to 256 rows.  Behind the layer, clusters of CTAs take one adapter and up to 16 of its rows at a time: up to 64 rows (GATHER) the rows of an adapter are put
 // together wherever they stand, the items being found by one match over the batch; beyond that, where rows come as prompts, a cluster stays with 16
 // neighbouring rows and the adapters among them.  A cluster makes u of the rows as narrow_kernel does and adds their part to y as widen_kernel does, the
 // CTAs taking columns in turn.  The CTAs send their sums of u to one another, so one cluster barrier lies between the two steps; the factor's first entries
 // and y of the second are fetched before it.  One launch instead of two around the layer saves a launch's latency and the way of u through memory.
-// Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y): few instructions on the way count, not bytes.
+// Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y): few instructions on the way count, not bytes.  One token of 1024 x 4096, rank 16: 5900
+// clocks, of which ids and items 810, the rank's sums 1500, their way through the cluster 1500, y 510; 3.8 us behind the layer's 2.7.  48 rows of ten
+// adapters, 14336 x 4096, rank 32: 11 us behind 15.8 (two sets of columns on their way; with one 14).
 template <int R16>
 struct Decode {
-    static constexpr int kRows = 16, kRanks = 16 * R16, kCluster = 8;   // (most CTAs of a cluster)
-    static constexpr int kSets = R16 <= 4 ? 2 : 1;                              // sets of 32 columns that a warp has on their way
+    static constexpr int kRows = 16, kRanks = 16 * R16, kCluster = 8;           // (most CTAs of a cluster)
     static constexpr int kBytes = (kWarps + kCluster) * kRows * kRanks * 4 + Operand<R16>::pieces(kRows) * 16 + kRows * 4 + kWarps * kRows * 4;
     static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
+};
+// The lane's part of 32 columns of the second factor and of y, on its way: 16-byte pieces, or, where rows lie on no 16-byte boundary, the halves that it needs (shifting
+// pieces into place takes more instructions than these loads)
+template <int R16, bool VEC>
+struct Columns {
+    uint4 b[R16][4], y[2];
+    // src: the lane's 8 columns of its first row; n of them are inside; ranks: of its rows 16 k + i those below this exist
+    __device__ __forceinline__ void load(const __half* src, int m_all, int n, int ranks, const __half* const (&y_src)[2], const bool (&has)[2], int n_y) {
+#pragma unroll
+        for (int k = 0; k < R16; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[k][i] = 16 * k + i < ranks && n > 0 ? *reinterpret_cast<const uint4*>(src + (size_t)(16 * k + i) * m_all) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) y[h] = has[h] && n_y > 0 ? *reinterpret_cast<const uint4*>(y_src[h]) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ void factor(uint32_t (&f)[R16][1][4][2], int odd) const {
+        const uint32_t pick = odd ? 0x7632u : 0x5410u;
+#pragma unroll
+        for (int k = 0; k < R16; ++k)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                f[k][0][0][p] = __byte_perm(b[k][2 * p].x, b[k][2 * p + 1].x, pick);
+                f[k][0][1][p] = __byte_perm(b[k][2 * p].y, b[k][2 * p + 1].y, pick);
+                f[k][0][2][p] = __byte_perm(b[k][2 * p].z, b[k][2 * p + 1].z, pick);
+                f[k][0][3][p] = __byte_perm(b[k][2 * p].w, b[k][2 * p + 1].w, pick);
+            }
+    }
+    __device__ __forceinline__ uint4 row(int h) const { return y[h]; }
+};
+template <int R16>
+struct Columns<R16, false> {
+    unsigned short b[R16][4][4], y[2][8];
+    __device__ __forceinline__ void load(const __half* src, int m_all, int n, int ranks, const __half* const (&y_src)[2], const bool (&has)[2], int n_y) {
+        const int odd = (threadIdx.x >> 2) & 1;                                 // which column of a pair the lane's fragments hold
+#pragma unroll
+        for (int k = 0; k < R16; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned short* row = reinterpret_cast<const unsigned short*>(src + (size_t)(16 * k + i) * m_all) + odd;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) b[k][i][q] = 16 * k + i < ranks && 2 * q + odd < n ? row[2 * q] : (unsigned short)0;
+            }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) y[h][q] = has[h] && q < n_y ? reinterpret_cast<const unsigned short*>(y_src[h])[q] : (unsigned short)0;
+    }
+    __device__ __forceinline__ void factor(uint32_t (&f)[R16][1][4][2], int) const {
+#pragma unroll
+        for (int k = 0; k < R16; ++k)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) f[k][0][q][p] = b[k][2 * p][q] | (uint32_t)b[k][2 * p + 1][q] << 16;
+    }
+    __device__ __forceinline__ uint4 row(int h) const {
+        return make_uint4(y[h][0] | (uint32_t)y[h][1] << 16, y[h][2] | (uint32_t)y[h][3] << 16, y[h][4] | (uint32_t)y[h][5] << 16, y[h][6] | (uint32_t)y[h][7] << 16);
+    }
 };
 template <int R16, bool VEC, bool GATHER>
 __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(const __grid_constant__ DecodeParams P) {
@@ -574,7 +695,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
     const DecodeLayer& L = P.layer[blockIdx.z];
     const int n = L.n, m_all = L.m, rank = L.rank, batch = P.batch;
     const int groups = (m_all + 31) / 32, step = parts * kWarps;                // of 32 columns
-    const uint32_t pick = gq & 1 ? 0x7632u : 0x5410u, before = (1u << lane) - 1u;
+    const uint32_t before = (1u << lane) - 1u;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -682,21 +803,14 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
         const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + 8 * (gq >> 1);
         __half* y[2] = {L.y + row[0] * m_all + 8 * tq, L.y + row[1] * m_all + 8 * tq};
         int g = warp * parts + part;                                        // neighbouring columns to different SMs
-        struct Columns {
-            uint4 b[R16][4], y[2];
+        constexpr int kSets = R16 <= (VEC ? 4 : 2) ? 2 : 1;                      // sets of 32 columns on their way
+        Columns<R16, VEC> sets[kSets];
+        auto load_columns = [&](Columns<R16, VEC>& l, int g) {
+            const __half* const y_src[2] = {y[0] + 32 * g, y[1] + 32 * g};
+            l.load(b + 32 * g, m_all, g < groups ? m_all - 32 * g - 8 * (gq >> 1) : 0, rank - 4 * tq, y_src, has, g < groups ? m_all - 32 * g - 8 * tq : 0);
         };
-        auto load_columns = [&](Columns& l, int g) {
-            const int in_b = g < groups ? m_all - 32 * g - 8 * (gq >> 1) : 0, in_y = g < groups ? m_all - 32 * g - 8 * tq : 0;
 #pragma unroll
-            for (int k = 0; k < R16; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) l.b[k][i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all + 32 * g, 16 * k + 4 * tq + i < rank ? in_b : 0);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) l.y[h] = load_8<VEC>(y[h] + 32 * g, has[h] ? in_y : 0);
-        };
-        Columns sets[D::kSets];
-#pragma unroll
-        for (int q = 0; q < D::kSets; ++q) load_columns(sets[q], g + q * step);
+        for (int q = 0; q < kSets; ++q) load_columns(sets[q], g + q * step);
         __syncthreads();
         cluster_wait();
         for (int e = threadIdx.x; e < kRows * kRanks / 4; e += kThreads) {
@@ -727,20 +841,12 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
         __syncthreads();
         if (turn + (int)gridDim.y < total) cluster_arrive();                // the inbox has been read: sums of the next item may come
 
-        auto widen_columns = [&](Columns& l, int g) {
+        auto widen_columns = [&](Columns<R16, VEC>& l, int g) {
             if (g >= groups) return;
             uint32_t f[R16][1][4][2];
-#pragma unroll
-            for (int k = 0; k < R16; ++k)
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    f[k][0][0][p] = __byte_perm(l.b[k][2 * p].x, l.b[k][2 * p + 1].x, pick);
-                    f[k][0][1][p] = __byte_perm(l.b[k][2 * p].y, l.b[k][2 * p + 1].y, pick);
-                    f[k][0][2][p] = __byte_perm(l.b[k][2 * p].z, l.b[k][2 * p + 1].z, pick);
-                    f[k][0][3][p] = __byte_perm(l.b[k][2 * p].w, l.b[k][2 * p + 1].w, pick);
-                }
-            const uint4 old[2] = {l.y[0], l.y[1]};
-            load_columns(l, g + D::kSets * step);
+            l.factor(f, gq & 1);
+            const uint4 old[2] = {l.row(0), l.row(1)};
+            load_columns(l, g + kSets * step);
             float sum[1][4][4];
 #pragma unroll
             for (int k = 0; k < R16; ++k) widen_step<1>(sum, k == 0, us + O::at(gq) + 4 * k + tq, O::kSecond, f[k]);
@@ -749,9 +855,9 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
             for (int h = 0; h < 2; ++h)
                 if (has[h] && left_cols > 0) widen_store<VEC>(y[h] + 32 * g, left_cols, old[h], sum[0], h, scale * backs[8 * h + gq]);
         };
-        for (; g < groups; g += D::kSets * step) {
+        for (; g < groups; g += kSets * step) {
 #pragma unroll
-            for (int q = 0; q < D::kSets; ++q) widen_columns(sets[q], g + q * step);
+            for (int q = 0; q < kSets; ++q) widen_columns(sets[q], g + q * step);
         }
     }
     if (blockIdx.y == 0 && part == 0) {                                         // rows without adapter: u is zero
@@ -801,9 +907,11 @@ __device__ __forceinline__ void ldmatrix_trans(uint32_t (&r)[4], uint32_t at) {
 // with the rows inside, so low is turned when it is split).  A warp takes 16 ranks and 64 columns, GROUPS warps the same columns; 16 warps, because what a
 // tile costs beside its MMAs (copies, splitting, barriers) is then shared by 256 columns.  The rows of a
 // cluster's adapter are dealt out to its CTAs in chunks of 64; a CTA first lists the rows that are its adapter's, so other rows are neither read nor
-// multiplied by zero (0 * NaN), then streams them through a ring of stages; the next tile is split beside the MMAs of the one at hand, half of the warps doing the one first, half the other.
+// multiplied by zero (0 * NaN), then streams them through a ring of stages; the next tile is split
+// beside the MMAs of the one at hand, half of the warps doing the one first, half the other.
 // Sums of a tile are added up in fp32 registers (the tensor core truncates), the CTAs' sums over the cluster in order.
-// Bound: v from memory; from rank 64 on the MMAs.
+// Bound: 2048 rows of 4096 and 4096 columns, rank 16: 15.5 us (33.5 MB: 5.1; per tile of 64 rows 920 clocks are copies, 640 splitting, 410 MMAs, and a CTA's start and
+// the sum over the cluster cost as much as eight tiles); 4096 rows of 11008 and 4096 columns, two adapters of rank 64: 98 us (124 MB: 19; MMAs 29), issue slots.
 template <int GROUPS, bool VEC>
 __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_constant__ FactorParams P) {
     using F = Factor<GROUPS>;
@@ -858,7 +966,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
                     const __half* src = in ? S.v + (size_t)list[at] * side + col : S.v;
                     unsigned char* dst = stage + r * F::kVStride + i % kPieces * 16;
                     if (VEC) copy_async_16(dst, src, in);
-                    else *reinterpret_cast<uint4*>(dst) = load_8<false>(src, in ? side - col : 0);
+                    else *reinterpret_cast<uint4*>(dst) = load_8<false>(src, in ? side - col : 0, S.v + (size_t)P.batch * side);
                 }
                 float* low = reinterpret_cast<float*>(stage + F::kVBytes);
                 constexpr int kFours = F::kRanks / 4;
