@@ -135,29 +135,22 @@ __device__ __forceinline__ void copy_async_pieces(uint4* dst, int second, const 
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + h * second)), "l"(size ? from : piece), "r"(size) : "memory");
     }
 }
-// 8 halves at src, of which those before `n` are inside their row; `end` is the end of the buffer, which starts on 16 bytes.  VEC: src lies on 16 bytes and all or
-// none are inside.  Otherwise (rows of any length) aligned pieces are read, two loads instead of eight; halves one by one where a piece would reach
-// beyond the buffer.
-template <bool VEC>
+// The same straight from memory, for rows of any length; `end` is the end of the buffer, which starts on 16 bytes: halves one by one where a piece would reach beyond it.
 __device__ __forceinline__ uint4 load_8(const __half* src, int n, const __half* end) {
-    if constexpr (VEC) {
-        return n > 0 ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
-    } else {
-        if (n <= 0) return make_uint4(0u, 0u, 0u, 0u);
-        const uintptr_t at = reinterpret_cast<uintptr_t>(src);
-        const uint4* piece = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-        const bool two = (int)((at >> 1) & 7u) + min(n, 8) > 8;
-        if (reinterpret_cast<const __half*>(piece + (two ? 2 : 1)) > end) {
-            uint32_t v[4] = {};
+    if (n <= 0) return make_uint4(0u, 0u, 0u, 0u);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(src);
+    const uint4* piece = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+    const bool two = (int)((at >> 1) & 7u) + min(n, 8) > 8;
+    if (reinterpret_cast<const __half*>(piece + (two ? 2 : 1)) > end) {
+        uint32_t v[4] = {};
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (q < n) v[q >> 1] |= (uint32_t)__half_as_ushort(src[q]) << (16 * (q & 1));
-            return make_uint4(v[0], v[1], v[2], v[3]);
-        }
-        return extract_8(piece[0], two ? piece[1] : make_uint4(0u, 0u, 0u, 0u), src, n);
+        for (int q = 0; q < 8; ++q)
+            if (q < n) v[q >> 1] |= (uint32_t)__half_as_ushort(src[q]) << (16 * (q & 1));
+        return make_uint4(v[0], v[1], v[2], v[3]);
     }
+    return extract_8(piece[0], two ? piece[1] : make_uint4(0u, 0u, 0u, 0u), src, n);
 }
-// 8 halves to dst, those before `n`; VEC as above.  Otherwise in words of the 4-byte grid, with a half before and behind them where dst is odd.
+// 8 halves to dst, those before `n`.  VEC: dst lies on 16 bytes and all are inside.  Otherwise in words of the 4-byte grid, with a half before and behind them where dst is odd.
 template <bool VEC>
 __device__ __forceinline__ void store_8(__half* dst, int n, const uint32_t (&v)[4]) {
     if constexpr (VEC) {
@@ -490,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
     if ((int)blockIdx.x * W::kCols >= m_all) return;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    const __half *y_end = L.y + (size_t)batch * m_all, *b_end = L.b + (size_t)L.count * rank * m_all;
+    const __half* y_end = L.y + (size_t)batch * m_all;
     const bool fours = rank % 4 == 0;
     const int c = col0 + 8 * tq;                                                // the lane's columns in y: 8 here and 8 in each further group
     ring += warp * W::kBlockPieces;
@@ -539,15 +532,29 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
             const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + cf;
 #pragma unroll
             for (int k = 0; k < R16; ++k) {
-                uint4 v[4];
+                if constexpr (VEC) {
+                    uint4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = load_8<VEC>(b + (size_t)(16 * k + i) * m_all, 16 * k + 4 * tq + i < rank ? m_all - cf : 0, b_end);
+                    for (int i = 0; i < 4; ++i) v[i] = 16 * k + 4 * tq + i < rank && cf < m_all ? *reinterpret_cast<const uint4*>(b + (size_t)(16 * k + i) * m_all) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    f[k][g][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
-                    f[k][g][1][p] = __byte_perm(v[2 * p].y, v[2 * p + 1].y, pick);
-                    f[k][g][2][p] = __byte_perm(v[2 * p].z, v[2 * p + 1].z, pick);
-                    f[k][g][3][p] = __byte_perm(v[2 * p].w, v[2 * p + 1].w, pick);
+                    for (int p = 0; p < 2; ++p) {
+                        f[k][g][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
+                        f[k][g][1][p] = __byte_perm(v[2 * p].y, v[2 * p + 1].y, pick);
+                        f[k][g][2][p] = __byte_perm(v[2 * p].z, v[2 * p + 1].z, pick);
+                        f[k][g][3][p] = __byte_perm(v[2 * p].w, v[2 * p + 1].w, pick);
+                    }
+                } else {                                                        // the halves that the fragments hold
+                    uint32_t v[4][4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const unsigned short* row = reinterpret_cast<const unsigned short*>(b + (size_t)(16 * k + i) * m_all) + (gq & 1);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) v[i][q] = 16 * k + 4 * tq + i < rank && cf + 2 * q + (gq & 1) < m_all ? row[2 * q] : 0u;
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) f[k][g][q][p] = v[2 * p][q] | v[2 * p + 1][q] << 16;
                 }
             }
         }
@@ -966,7 +973,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
                     const __half* src = in ? S.v + (size_t)list[at] * side + col : S.v;
                     unsigned char* dst = stage + r * F::kVStride + i % kPieces * 16;
                     if (VEC) copy_async_16(dst, src, in);
-                    else *reinterpret_cast<uint4*>(dst) = load_8<false>(src, in ? side - col : 0, S.v + (size_t)P.batch * side);
+                    else *reinterpret_cast<uint4*>(dst) = load_8(src, in ? side - col : 0, S.v + (size_t)P.batch * side);
                 }
                 float* low = reinterpret_cast<float*>(stage + F::kVBytes);
                 constexpr int kFours = F::kRanks / 4;
@@ -1273,7 +1280,8 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
     if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
     // One launch behind the layer, or two around it?  The one reads the second factor again for every 16 rows, so rows times outputs decide (B200, us beyond the
     // layer alone, one launch against two: 200 rows of 4096 x 4096 rank 16 to 32 9.8 / 15.1, 256 rows 9.9 / 11.8, 200 rows of 14336 x 4096 23 / 12; rank 64, 130 rows of
-    // 4096 x 4096 15.0 / 17.7, 65 rows of 14336 x 4096 17.9 / 13.3).  Outputs that are not 16-byte pieces are slow in the one: up to 64 rows only.
+    // 4096 x 4096 15.0 / 17.7, 65 rows of 14336 x 4096 17.9 / 13.3; outputs that are not 16-byte pieces, 4099 x 4096, rank 16 at 130 and 200 rows 11.6 / 12.7 and
+    // 17.0 / 14.2, rank 32 at 200 12.7 / 17.9).
     bool vec = true;
     long long outputs = 0;
     int most_rank = 0;
@@ -1283,7 +1291,8 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         outputs += adapters[l]->n_out;
         most_rank = std::max(most_rank, adapters[l]->rank);
     }
-    const bool decode = batch <= kGatherRows || (vec && batch <= kDecodeRows && batch * outputs <= (most_rank <= 32 ? 1LL << 20 : 3LL << 18));
+    const long long most = most_rank > 32 ? 3LL << 18 : vec || most_rank > 16 ? 1LL << 20 : 5LL << 17;
+    const bool decode = batch <= kGatherRows || (batch <= kDecodeRows && batch * outputs <= most);
     cudaError_t e = cudaSuccess;
     if (!decode) {
         e = each_group([&] {
