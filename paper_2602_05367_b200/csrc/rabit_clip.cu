@@ -172,6 +172,10 @@ static int bind_call(const float* const* tensors, float* const* outs, const size
     cudaPointerAttributes attr;
     RABIT_CUDA_TRY(cudaPointerGetAttributes(&attr, dev_buf));
     if (attr.type != cudaMemoryTypeDevice && attr.type != cudaMemoryTypeManaged) return rabit_fail(RABIT_INVALID_ARG, "%s: dev_buf is not device memory", who);
+    // (a captured copy would read the table again at every replay, when it is gone)
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    RABIT_CUDA_TRY(cudaStreamIsCapturing((cudaStream_t)stream, &capturing));
+    if (capturing != cudaStreamCaptureStatusNone) return rabit_fail(RABIT_INVALID_ARG, "%s: the stream is being captured", who);
     std::vector<Chunk> table;
     table.reserve(n_chunks);
     for (int i = 0; i < n; ++i)

@@ -549,6 +549,22 @@ def test_clipping_replayed_and_refused():
         rabit.rabit_clip_gradients(G, 1.0)
 
 
+def test_gradients_are_not_bound_under_capture():
+    """A captured copy of the table would be repeated from host memory that is gone."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    t, s, graph = torch.ones(64, device="cuda"), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        t.mul_(2.0)
+        with pytest.raises(rabit.RabitError, match="captured"):
+            rabit.RabitGradients([t])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert bool((t == 2.0).all())
+
+
+
 def test_a_training_step_of_a_group_as_it_is_used():
     """Forward of two projections, backward through the transposed layers, all factor gradients, clipping; the loss is linear in the second factors,
     so moving them changes it by exactly what the gradient says, up to the roundings of y."""
