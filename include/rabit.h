@@ -172,8 +172,9 @@ typedef struct rabit_adapters {
  *             caller that does not gives a scratch buffer).  y and u may not overlap one another nor any input.
  * Rows may name adapters in any order; rows of one adapter that follow one another (a prompt) share its reads.
  * The layer's sum is rounded to fp16 in y and the adapter's part, kept in fp32, is added to that and rounded again: an error of at most
- * half a step of the layer's sum and half a step of y.  An infinite or NaN value in a row of x or in an adapter reaches the
- * rows that it belongs to and no others.
+ * half a step of the layer's sum and half a step of y.  u enters the second product to 22 bits, or to 2^-40 of the row's largest entry.
+ * An infinite or NaN value in a row of x or in an adapter reaches the rows that it belongs to and no others; the outputs that it takes part
+ * in are infinite or NaN, which of the two is open.  At most 2^31 - 256 rows.
  * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.
  */
 RABIT_API int rabit_linear_adapted(const rabit_layer* layer, const rabit_adapters* adapters, const void* x, const int* ids,
@@ -195,7 +196,9 @@ RABIT_API int rabit_linear_group_adapted(const rabit_layer* const* layers, const
  *   da  DEVICE fp32 [count][rank][n_in], db DEVICE fp32 [count][rank][n_out], 16-byte aligned, not overlapping each other nor any input.
  *       accumulate = 0: overwritten (zero for an adapter that no row names); otherwise the gradients are added to what is there.
  * Only the sizes, scale and nothing else of `adapters` is read.  Sums are fp32 in an order that the sizes and ids fix: the same call
- * gives the same bits.  What a row of another adapter, or of none, holds does not matter, be it infinite or NaN.
+ * gives the same bits.  u and p enter the products to 22 bits, or to 2^-40 of the largest entry of their rank in 64 rows.
+ * What a row of another adapter, or of none, holds does not matter, be it infinite or NaN; of a row of the adapter's it makes the gradients that it
+ * takes part in infinite or NaN, which of the two is open.
  * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.  The buffers' device must be the current device.
  */
 RABIT_API int rabit_adapter_gradients(const rabit_adapters* adapters, const void* x, const float* u, const void* dy, const float* p, const int* ids,
@@ -218,7 +221,7 @@ RABIT_API int rabit_transpose(const rabit_layer* layer, void* dev_buf, size_t de
  *   outs      HOST array of n DEVICE fp32 pointers that receive the clipped values, or NULL to clip in place; an output is its own
  *             tensor or overlaps none, nor another output
  *   dev_buf   DEVICE, 256-byte aligned, at least rabit_gradients_bytes(counts, n): table and partial sums, owned by the caller
- * rabit_gradients_bind copies the table on `stream` and returns when it has been staged.
+ * rabit_gradients_bind copies the table on `stream` and returns when it has been staged; not while `stream` is being captured.
  */
 typedef struct rabit_gradients rabit_gradients;
 RABIT_API size_t rabit_gradients_bytes(const size_t* counts, int n);

@@ -21,6 +21,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxGroup = 8;                           // layers in one launch
+constexpr int kMostRows = 0x7FFFFF00;                  // rows of a call: a tile's places behind the last one are 32-bit numbers too
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -1228,6 +1229,7 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
     if (!layers || !adapters || !xs || !ys || !us) return rabit_fail(RABIT_INVALID_ARG, "%s: null array", who);
     if (n_layers < 1) return rabit_fail(RABIT_INVALID_ARG, "%s: n_layers must be >= 1 (got %d)", who, n_layers);
     if (batch < 1) return rabit_fail(RABIT_INVALID_ARG, "%s: batch must be >= 1 (got %d)", who, batch);
+    if (batch > kMostRows) return rabit_fail(RABIT_UNSUPPORTED_SHAPE, "%s: batch must be <= %d (got %d)", who, kMostRows, batch);
     if (!ids || (((uintptr_t)ids) & 3u)) return rabit_fail(RABIT_INVALID_ARG, "%s: ids is NULL or misaligned", who);
     const Range r_ids{ids, (size_t)batch * 4};
     for (int l = 0; l < n_layers; ++l) {

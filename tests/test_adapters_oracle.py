@@ -132,3 +132,9 @@ def test_clip_refusals():
     assert lib.rabit_gradients_free(None) == 0
     assert lib.rabit_gradients_bytes(None, 1) == 0 and lib.rabit_gradients_bytes((ctypes.c_size_t * 1)(5), 0) == 0
     assert lib.rabit_gradients_bytes((ctypes.c_size_t * 2)(0, 5), 2) > 0
+
+
+def test_more_rows_than_32_bit_places_are_refused():
+    lib, s = binding.raw_lib(), _struct()
+    for batch in (2 ** 31 - 1, 2 ** 31 - 255):
+        assert lib.rabit_linear_adapted(None, ctypes.byref(s), P, P, P, P, batch, None) == -2 and "batch" in rabit.last_error()
