@@ -1,4 +1,4 @@
-"""B200-native residual-binary linear layer (RaBiT inference hot path).
+"""B200-native residual-binary linear layer (RaBiT inference hot path), with low-rank adapters beside it.
 
 The product is ``librabit.so`` (hand-written CUDA for sm_100a behind a C ABI, declared in
 ``include/rabit.h``).  This package is the thin binding: it marshals arguments and owns
