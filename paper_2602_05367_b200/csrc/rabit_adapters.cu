@@ -4,7 +4,7 @@
 //   da[i] = scale[i] * sum_{t: id_t = i} p[t] x[t]^T,   db[i] = scale[i] * sum_{t: id_t = i} u[t] dy[t]^T
 //
 // Every factor is `rank` rows along a side of the layer, so both products of the forward pass and of the input gradient are the same kernels: narrow_kernel (a
-// side to the rank) and widen_kernel (the rank to a side) around the layer, or decode_kernel, both in one behind it, for few rows; the gradients are
+// side to the rank) beside the layer and widen_kernel (the rank to a side) behind it, or decode_kernel, both in one, for few rows; the gradients are
 // factor_kernel.  All are MMAs of mma.sync: their products are a few per cent of the layer's, their inner or outer size is the rank (1 to 128),
 // and what bounds them is memory, latency or the instructions around the MMAs, not the tensor pipe (mma.sync reaches 537 TFLOP/s here).
 #include <cooperative_groups.h>
@@ -91,7 +91,8 @@ struct NarrowLayer {
 struct NarrowParams {
     NarrowLayer layer[kMaxGroup];
     const int* ids;
-    int batch, shares;                                                          // clusters that share the adapters of a tile of rows; the later ones are mostly idle, so they come last
+    int batch, beside;                                                          // beside: the kernel before this one is the layer's, still running
+    int shares;                                                                 // clusters that share the adapters of a tile of rows; the later ones are mostly idle, so they come last
 };
 
 // ---- asynchronous copies to shared memory --------------------------------------------------------------------
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, (Narrow<NR, WM>::kPerSm)) narrow_ker
     const NarrowLayer& L = P.layer[blockIdx.z];
     const int share = blockIdx.y, tile0 = (int)(blockIdx.x / parts) * T::kRows, n = L.n, rank = L.rank, row0 = tile0 + 16 * wm;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!P.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // rows of the tile lane by lane, 32 to a word
     constexpr int kWords = (T::kRows + 31) / 32;
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, (Narrow<NR, WM>::kPerSm)) narrow_ker
 #pragma unroll
     for (int w = 0; w < kWords; ++w) {
         const int r = 32 * w + lane;
-        id[w] = r < T::kRows && tile0 + r < P.batch ? P.ids[tile0 + r] : -1;
+        id[w] = r < T::kRows && tile0 + r < P.batch ? __ldcg(P.ids + tile0 + r) : -1;   // (from L2: beside the layer nothing has made L1 forget an earlier call's)
         if (id[w] >= L.count) id[w] = -1;
         named[w] = left[w] = __ballot_sync(0xFFFFFFFFu, id[w] >= 0);
         mine[w] = 0u;
@@ -352,6 +353,8 @@ __global__ void __launch_bounds__(kThreads, (Narrow<NR, WM>::kPerSm)) narrow_ker
         store_4(L.u + (size_t)(tile0 + row) * rank + j, cluster_sum(cluster, red, parts, e), rank - j, rank % 4 == 0);
     }
     cluster.sync();
+    // One CTA, whose share is always taken, waits for the layer: the grid ends behind the layer's, so what waits for this one has y.  The others make room.
+    if (P.beside && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // ---- y[t] += scale[id_t] * B[id_t]^T u[t] --------------------------------------------------------------------
@@ -365,7 +368,8 @@ struct WidenLayer {
 struct WidenParams {
     WidenLayer layer[kMaxGroup];
     const int* ids;
-    int batch, blocks;                                                          // row blocks of a CTA, one after the other
+    int batch, beside;                                                          // as in NarrowParams
+    int blocks;                                                                 // row blocks of a CTA, one after the other
 };
 // 16-byte pieces of a row (pair) of u as operand: half as many again are 4 more than a multiple of 8 from pair to pair, so that two pairs that a load touches, 64
 // bytes each, meet in no bank
@@ -454,7 +458,7 @@ struct DecodeLayer {
 struct DecodeParams {
     DecodeLayer layer[kMaxGroup];
     const int* ids;
-    int batch;
+    int batch, beside;                                                          // as in NarrowParams
 };
 constexpr int kDecodeRows = 256, kGatherRows = 64;                              // most rows of a batch; of one whose rows are put together by adapter
 
@@ -482,7 +486,9 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
     const int blocks = min(P.blocks, (batch - first_row + kWidenRows - 1) / kWidenRows);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if ((int)blockIdx.x * W::kCols >= m_all) return;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // beside: ids and the first factor before the wait (from L2, as in narrow_kernel; without 16-byte pieces the factor comes through L1, so behind it)
+    const bool early = VEC && P.beside;
+    if (!early) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const __half* y_end = L.y + (size_t)batch * m_all;
     const bool fours = rank % 4 == 0;
@@ -521,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
         copy_async_commit();
     };
     auto load_id = [&](int blk) {
-        const int r = first_row + blk * kWidenRows + lane, v = blk < blocks && r < batch ? P.ids[r] : -1;
+        const int r = first_row + blk * kWidenRows + lane, v = blk < blocks && r < batch ? __ldcg(P.ids + r) : -1;
         return v < L.count ? v : -1;
     };
     uint32_t f[R16][G][4][2];                                                   // [16 ranks][32 columns][column tile]: ranks 4 tq and 4 tq + 1, the two behind them
@@ -536,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
                 if constexpr (VEC) {
                     uint4 v[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = 16 * k + 4 * tq + i < rank && cf < m_all ? *reinterpret_cast<const uint4*>(b + (size_t)(16 * k + i) * m_all) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < 4; ++i) v[i] = 16 * k + 4 * tq + i < rank && cf < m_all ? __ldcg(reinterpret_cast<const uint4*>(b + (size_t)(16 * k + i) * m_all)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         f[k][g][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
@@ -561,8 +567,14 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
         }
     };
 
-    fetch(0, y_from);
+    if (!early) fetch(0, y_from);
     int next_id = load_id(0), held = -1;                                        // held: the adapter whose factor the registers hold
+    if (early) {
+        const uint32_t named = __ballot_sync(0xFFFFFFFFu, next_id >= 0);
+        if (named) load_factor(held = __shfl_sync(0xFFFFFFFFu, next_id, __ffs(named) - 1));
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        fetch(0, y_from);
+    }
     for (int blk = 0; blk < blocks; ++blk) {
         const int id = next_id;
         uint32_t left = __ballot_sync(0xFFFFFFFFu, id >= 0);
@@ -583,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
             if (cur != held) load_factor(held = cur);
             const uint32_t match = __ballot_sync(0xFFFFFFFFu, id == cur);
             left &= ~match;
-            const float scale = L.scale[cur];
+            const float scale = __ldcg(L.scale + cur);
 #pragma unroll
             for (int mt = 0; mt < kTiles; ++mt) {
                 const uint32_t hits = (match >> (16 * mt)) & 0xFFFFu;
@@ -617,10 +629,11 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
 // together wherever they stand, the items being found by one match over the batch; beyond that, where rows come as prompts, a cluster stays with 16
 // neighbouring rows and the adapters among them.  A cluster makes u of the rows as narrow_kernel does and adds their part to y as widen_kernel does, the
 // CTAs taking columns in turn.  The CTAs send their sums of u to one another, so one cluster barrier lies between the two steps; the factor's first entries
-// and y of the second are fetched before it.  One launch instead of two around the layer saves a launch's latency and the way of u through memory.
+// and y of the second are fetched before it.  One launch instead of two saves a launch's latency and the way of u through memory.
 // Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y): few instructions on the way count, not bytes.  One token of 1024 x 4096, rank 16: 5900
 // clocks, of which ids and items 810, the rank's sums 1500, their way through the cluster 1500, y 510; 3.8 us behind the layer's 2.7.  48 rows of ten
-// adapters, 14336 x 4096, rank 32: 11 us behind 15.8 (two sets of columns on their way; with one 14).
+// adapters, 14336 x 4096, rank 32: 10.4 us behind 15.9 (two sets of columns on their way; with one 14).  Behind the GEMM the step up to the sums of u runs beside it
+// (16 rows of 6144 outputs in three layers 16.9 -> 15.0 us, the 48 rows 27.6 -> 26.3; y and the sums' exchange behind one another instead, 15.8 and 26.7).
 template <int R16>
 struct Decode {
     static constexpr int kRows = 16, kRanks = 16 * R16, kCluster = 8;           // (most CTAs of a cluster)
@@ -705,11 +718,12 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
     const int groups = (m_all + 31) / 32, step = parts * kWarps;                // of 32 columns
     const uint32_t before = (1u << lane) - 1u;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    bool waited = P.beside == 0;                                                // (beside the layer everything is read from L2, as in narrow_kernel)
+    if (waited) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // GATHER: row `lane` and row 32 + lane of the batch; otherwise row `lane` of the cluster's 16
     const int row0 = GATHER ? 0 : (int)(blockIdx.x / parts) * kRows;
-    int id = lane < (GATHER ? 32 : kRows) && row0 + lane < batch ? P.ids[row0 + lane] : -1, id1 = GATHER && 32 + lane < batch ? P.ids[32 + lane] : -1;
+    int id = lane < (GATHER ? 32 : kRows) && row0 + lane < batch ? __ldcg(P.ids + row0 + lane) : -1, id1 = GATHER && 32 + lane < batch ? __ldcg(P.ids + 32 + lane) : -1;
     if (id >= L.count) id = -1;
     if (id1 >= L.count) id1 = -1;
     uint32_t same = __match_any_sync(kAll, id), same1 = 0u;                     // rows of the same adapter: in the first 32, in the second
@@ -750,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
         __syncwarp();
         const bool has[2] = {rows[gq] >= 0, rows[8 + gq] >= 0};
         const size_t row[2] = {(size_t)max(rows[gq], 0), (size_t)max(rows[8 + gq], 0)};
-        const float scale = L.scale[cur];
+        const float scale = __ldcg(L.scale + cur);
 
         float acc[NR][4] = {};
         {
@@ -765,9 +779,9 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
                 const bool in = u < u1;
                 const size_t col = (size_t)u * 32;
 #pragma unroll
-                for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? *reinterpret_cast<const uint4*>(x[m] + col) : make_uint4(0u, 0u, 0u, 0u);
+                for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? __ldcg(reinterpret_cast<const uint4*>(x[m] + col)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? *reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col) : make_uint4(0u, 0u, 0u, 0u);
+                for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? __ldcg(reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col)) : make_uint4(0u, 0u, 0u, 0u);
             };
             auto multiply = [&](const Loads& l) {
 #pragma unroll
@@ -807,6 +821,8 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
             if (pairs % 4 != 0 || pairs == 0) flush(pairs < 4);
         }
 
+        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");         // y
+        waited = true;
         // the second factor's entries and y of the warp's first 32 columns are on their way while u is put together
         const __half* b = L.b + ((size_t)cur * rank + 4 * tq) * m_all + 8 * (gq >> 1);
         __half* y[2] = {L.y + row[0] * m_all + 8 * tq, L.y + row[1] * m_all + 8 * tq};
@@ -868,6 +884,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
             for (int q = 0; q < kSets; ++q) widen_columns(sets[q], g + q * step);
         }
     }
+    if (!waited && blockIdx.y == 0) asm volatile("griddepcontrol.wait;" ::: "memory");   // (no item at all: the grid ends behind the layer's even so)
     if (blockIdx.y == 0 && part == 0) {                                         // rows without adapter: u is zero
         uint32_t bare[2] = {__ballot_sync(kAll, id < 0 && lane < (GATHER ? 32 : kRows) && row0 + lane < batch), __ballot_sync(kAll, GATHER && id1 < 0 && 32 + lane < batch)};
         int turn = 0;
@@ -1264,8 +1281,8 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
     RABIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev != layers[0]->device) return rabit_fail(RABIT_INVALID_ARG, "%s: the layers live on device %d but device %d is current", who, layers[0]->device, dev);
 
-    // u of all adapted layers, the layers themselves, then the adapters' part on top of their outputs: the kernels of the first step run while those of
-    // the second fetch their weights.  What the layers' calls refuse, they refuse before anything of this call has run.
+    // u of all adapted layers before or beside the layers themselves, then the adapters' part on top of their outputs.  What the layers' calls refuse, they refuse
+    // before anything of this call has run.
     int at[kMaxGroup], n = 0;
     auto each_group = [&](auto&& body) {
         cudaError_t e = cudaSuccess;
@@ -1280,7 +1297,7 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         return e;
     };
     if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
-    // One launch behind the layer, or two around it?  The one reads the second factor again for every 16 rows, so rows times outputs decide (B200, us beyond the
+    // One launch behind the layer, or two?  The one reads the second factor again for every 16 rows, so rows times outputs decide (B200, us beyond the
     // layer alone, one launch against two: 200 rows of 4096 x 4096 rank 16 to 32 9.8 / 15.1, 256 rows 9.9 / 11.8, 200 rows of 14336 x 4096 23 / 12; rank 64, 130 rows of
     // 4096 x 4096 15.0 / 17.7, 65 rows of 14336 x 4096 17.9 / 13.3; outputs that are not 16-byte pieces, 4099 x 4096, rank 16 at 130 and 200 rows 11.6 / 12.7 and
     // 17.0 / 14.2, rank 32 at 200 12.7 / 17.9).
@@ -1296,11 +1313,17 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
     const long long most = most_rank > 32 ? 3LL << 18 : vec || most_rank > 16 ? 1LL << 20 : 5LL << 17;
     const bool decode = batch <= kGatherRows || (batch <= kDecodeRows && batch * outputs <= most);
     cudaError_t e = cudaSuccess;
-    if (!decode) {
-        e = each_group([&] {
+    // u beside the layer's last kernel where that one lets the next start late (the GEMM): what is before it is complete then, x, ids and the readers of u among
+    // it, and u is made on the SMs that the GEMM leaves idle or leaves first (B200, layer and adapters, us, u before it / beside it: 300 rows of 1024 x 4096 rank
+    // 16 21.9 / 19.5, 1200 rows of 11008 x 4096 rank 128 242 / 236, 4096 rows of 11008 x 4096 rank 16 633 / 626).  Behind another kernel u would have to wait: it comes first.
+    bool beside = true;
+    for (int l = 0; l < n_layers; ++l) beside = beside && rabit_ends_late(*layers[l], batch);
+    auto narrow = [&] {
+        return each_group([&] {
             NarrowParams P{};
             P.ids = ids;
             P.batch = batch;
+            P.beside = beside;
             int max_rank = 0;
             for (int i = 0; i < n; ++i) {
                 const rabit_adapters* A = adapters[at[i]];
@@ -1309,15 +1332,23 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
             }
             return launch_narrow(P, n, max_rank, st);
         });
+    };
+    if (!decode && !beside) {
+        e = narrow();
         if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     }
     int rc = n_layers == 1 ? rabit_linear(layers[0], xs[0], ys[0], batch, stream) : rabit_linear_group(layers, xs, ys, n_layers, batch, stream);
     if (rc != RABIT_OK) return rc;
+    if (!decode && beside) {
+        e = narrow();
+        if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    }
     e = each_group([&] {
         DecodeParams D{};
         WidenParams P{};
         P.ids = D.ids = ids;
         P.batch = D.batch = batch;
+        P.beside = D.beside = beside;
         int max_rank = 0, max_m = 0, max_count = 0;
         for (int i = 0; i < n; ++i) {
             const rabit_adapters* A = adapters[at[i]];

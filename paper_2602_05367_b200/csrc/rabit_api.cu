@@ -279,6 +279,13 @@ static int linear_call(const rabit_layer* layer, const void* x, void* y, int bat
     return RABIT_OK;
 }
 
+// Whether the kernel that a call on this layer ends with, alone or in a group, lets the next one of the stream start only when all work before it is
+// complete: the GEMM, whose CTAs say so behind their dependency wait, and the plain kernel, beside which nothing starts.  The GEMVs say so when they start.
+bool rabit_ends_late(const rabit_layer& L, int batch) {
+    if (L.variant == 0) return batch > RABIT_MAX_GEMV_BATCH || (batch > kF16Rows && rabit_gemv_f16_supports(L, kF16Rows));
+    return L.variant == 1 || L.variant == 3 || L.variant == 4 || (L.variant == 6 && batch > kF16Rows);
+}
+
 extern "C" int rabit_linear(const rabit_layer* layer, const void* x, void* y, int batch, void* stream) {
     return rabit_guarded("rabit_linear", [&] { return linear_call(layer, x, y, batch, stream); });
 }

@@ -74,6 +74,7 @@ cudaError_t rabit_launch_transpose(const RabitGeom& G, const RabitHeader& hdr, c
 // up to 8 copies from device-visible host memory to the device by a kernel (rabit_fetch.cu); sizes are multiples of 16 bytes
 cudaError_t rabit_launch_fetch(const void* const* src, void* const* dst, const size_t* bytes, int n, cudaStream_t stream);
 
+bool rabit_ends_late(const rabit_layer& L, int batch);
 inline bool rabit_ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
     const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
     return a0 < b0 + bn && b0 < a0 + an;

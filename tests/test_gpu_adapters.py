@@ -244,6 +244,46 @@ def test_captured_replayed_and_on_another_stream():
     layer.free()
 
 
+@pytest.mark.parametrize("variant,batch,r,kind", [(0, 1, 16, "one"), (0, 7, 16, "mixed"), (0, 12, 16, "mixed"), (0, 48, 40, "mixed"), (0, 48, 16, "none"), (0, 200, 16, "none"), (0, 300, 16, "mixed"),
+                                                  (0, 1100, 64, "prompts"), (0, 1100, 64, "none"), (1, 70, 16, "mixed"), (2, 12, 16, "mixed"), (3, 12, 16, "mixed"),
+                                                  (4, 300, 128, "prompts"), (5, 300, 16, "prompts"), (6, 300, 16, "mixed")])
+def test_a_chain_of_calls_without_a_stop_between(variant, batch, r, kind):
+    """Each call's y is the next one's x, u is shared, and ids and factors change by copies on the stream: kernels that start while those before them run see all of it."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    side, n, steps = 512, 3, 6
+    L = make_layer(side, side, 2, key=(98,))
+    layer = rabit.rabit_pack(L.planes, (L.g.astype(np.float32) / 16).astype(np.float16), L.h)
+    if variant:
+        layer.set_variant(variant)
+    (xd,) = _cuda(make_x(batch, side, key=(98, batch)))
+    pools = [_cuda(*_pool(side, side, n, r, 11 + k)) for k in range(2)]
+    ids = [_cuda(_ids(batch, n, kind, k))[0] for k in range(2)]
+    s, outs = torch.cuda.Stream(), {}
+    torch.cuda.synchronize()
+    for stop in (True, False):
+        A, at = rabit.RabitAdapters(*[t.clone() for t in pools[0]]), ids[0].clone()
+        ys = [torch.zeros((batch, side), dtype=torch.float16, device="cuda") for _ in range(steps)]
+        u, us = torch.zeros((batch, r), device="cuda"), torch.zeros((steps, batch, r), device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for k in range(steps):
+                if k == 3:                                                              # calls 0-2 and 3-5 follow one another without anything between but the calls
+                    at.copy_(ids[1])
+                    for t, v in zip((A.a, A.b, A.scale), pools[1]):
+                        t.copy_(v)
+                rabit.rabit_linear_adapted(layer, A, ys[k - 1] if k else xd, at, ys[k], u if k % 3 != 2 else us[k])
+                if stop:
+                    s.synchronize()
+        torch.cuda.synchronize()
+        outs[stop] = [t.cpu().numpy() for t in ys] + [us.cpu().numpy(), u.cpu().numpy()]
+    assert all(np.isfinite(v).all() for v in outs[True][:steps]) and (outs[True][0] != 0).any()   # (rows without adapter shrink from call to call)
+    for k, (a, b) in enumerate(zip(outs[True], outs[False])):
+        assert np.array_equal(a, b), k
+    layer.free()
+
+
+
 def test_offsets_beyond_32_bits():
     """A pool of 4.4 GB whose last adapter is named, and its gradient of 8.8 GB."""
     import torch
