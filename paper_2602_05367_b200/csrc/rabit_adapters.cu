@@ -460,7 +460,7 @@ struct DecodeParams {
     const int* ids;
     int batch, beside;                                                          // as in NarrowParams
 };
-constexpr int kDecodeRows = 256, kGatherRows = 64;                              // most rows of a batch; of one whose rows are put together by adapter
+constexpr int kDecodeRows = 1024, kWindow = 64;                                 // most rows of a batch; of those whose rows of an adapter are put together
 
 // A CTA takes 512 columns (256 beyond rank 32), a warp 64 (32) of them, and blocks of 32 rows one after the other: rows by columns as m16n8k16 MMAs over the rank, the
 // factor's fragments in registers for all rows, a row of u as two fp16 parts of a common power of two.  The order of columns in MMA tiles and of ranks is
@@ -625,10 +625,9 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
 
 // ---- both steps in one launch, for few rows --------------------------------------------------------------------
 
-// Up to 256 rows.  Behind the layer, clusters of CTAs take one adapter and up to 16 of its rows at a time: up to 64 rows (GATHER) the rows of an adapter are put
-// together wherever they stand, the items being found by one match over the batch; beyond that, where rows come as prompts, a cluster stays with 16
-// neighbouring rows and the adapters among them.  A cluster makes u of the rows as narrow_kernel does and adds their part to y as widen_kernel does, the
-// CTAs taking columns in turn.  The CTAs send their sums of u to one another, so one cluster barrier lies between the two steps; the factor's first entries
+// Up to 1024 rows.  Behind the layer, clusters of CTAs take one adapter and up to 16 of its rows at a time: in windows of 64 rows the rows of an adapter are
+// put together wherever they stand, the items being found by one match over the window.  A cluster makes u of the rows as narrow_kernel does and adds their part to y
+// as widen_kernel does, the CTAs taking columns in turn.  The CTAs send their sums of u to one another, so one cluster barrier lies between the two steps; the factor's first entries
 // and y of the second are fetched before it.  One launch instead of two saves a launch's latency and the way of u through memory.
 // Bound: latencies (dependency wait, ids, x and factor, cluster barrier, y): few instructions on the way count, not bytes.  One token of 1024 x 4096, rank 16: 5900
 // clocks, of which ids and items 810, the rank's sums 1500, their way through the cluster 1500, y 510; 3.8 us behind the layer's 2.7.  48 rows of ten
@@ -698,7 +697,7 @@ struct Columns<R16, false> {
         return make_uint4(y[h][0] | (uint32_t)y[h][1] << 16, y[h][2] | (uint32_t)y[h][3] << 16, y[h][4] | (uint32_t)y[h][5] << 16, y[h][6] | (uint32_t)y[h][7] << 16);
     }
 };
-template <int R16, bool VEC, bool GATHER>
+template <int R16, bool VEC>
 __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(const __grid_constant__ DecodeParams P) {
     using D = Decode<R16>;
     using O = Operand<R16>;
@@ -714,22 +713,21 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
     int* rows = reinterpret_cast<int*>(backs + kRows) + warp * kRows;           // the rows at hand (-1: none), every warp for itself
     const DecodeLayer& L = P.layer[blockIdx.z];
-    const int n = L.n, m_all = L.m, rank = L.rank, batch = P.batch;
+    const int n = L.n, m_all = L.m, rank = L.rank, row0 = (int)(blockIdx.x / parts) * kWindow, batch = min(kWindow, P.batch - row0);   // rows of the window
     const int groups = (m_all + 31) / 32, step = parts * kWarps;                // of 32 columns
     const uint32_t before = (1u << lane) - 1u;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bool waited = P.beside == 0;                                                // (beside the layer everything is read from L2, as in narrow_kernel)
     if (waited) asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // GATHER: row `lane` and row 32 + lane of the batch; otherwise row `lane` of the cluster's 16
-    const int row0 = GATHER ? 0 : (int)(blockIdx.x / parts) * kRows;
-    int id = lane < (GATHER ? 32 : kRows) && row0 + lane < batch ? __ldcg(P.ids + row0 + lane) : -1, id1 = GATHER && 32 + lane < batch ? __ldcg(P.ids + 32 + lane) : -1;
+    // rows `lane` and 32 + `lane` of the window
+    int id = lane < batch ? __ldcg(P.ids + row0 + lane) : -1, id1 = 32 + lane < batch ? __ldcg(P.ids + row0 + 32 + lane) : -1;
     if (id >= L.count) id = -1;
     if (id1 >= L.count) id1 = -1;
     uint32_t same = __match_any_sync(kAll, id), same1 = 0u;                     // rows of the same adapter: in the first 32, in the second
     bool leads = id >= 0 && (same & before) == 0u, leads1 = false;              // the adapter's first row
     uint32_t same_of1 = 0u, same1_of1 = 0u;
-    if (GATHER && batch > 32) {
+    if (batch > 32) {
         same1_of1 = __match_any_sync(kAll, id1);
         for (uint32_t each = __ballot_sync(kAll, id1 >= 0 && (same1_of1 & before) == 0u); each != 0u; each &= each - 1u) {   // the adapters among the second 32 rows
             const int who = __ffs(each) - 1, v = __shfl_sync(kAll, id1, who);
@@ -760,7 +758,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
         __syncwarp();
         const int place = __popc(mask & before) - skip, place1 = __popc(mask) + __popc(mask1 & before) - skip;
         if ((mask >> lane & 1u) && place >= 0 && place < kRows) rows[place] = row0 + lane;
-        if ((mask1 >> lane & 1u) && place1 >= 0 && place1 < kRows) rows[place1] = 32 + lane;
+        if ((mask1 >> lane & 1u) && place1 >= 0 && place1 < kRows) rows[place1] = row0 + 32 + lane;
         __syncwarp();
         const bool has[2] = {rows[gq] >= 0, rows[8 + gq] >= 0};
         const size_t row[2] = {(size_t)max(rows[gq], 0), (size_t)max(rows[8 + gq], 0)};
@@ -886,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
     }
     if (!waited && blockIdx.y == 0) asm volatile("griddepcontrol.wait;" ::: "memory");   // (no item at all: the grid ends behind the layer's even so)
     if (blockIdx.y == 0 && part == 0) {                                         // rows without adapter: u is zero
-        uint32_t bare[2] = {__ballot_sync(kAll, id < 0 && lane < (GATHER ? 32 : kRows) && row0 + lane < batch), __ballot_sync(kAll, GATHER && id1 < 0 && 32 + lane < batch)};
+        uint32_t bare[2] = {__ballot_sync(kAll, id < 0 && lane < batch), __ballot_sync(kAll, id1 < 0 && 32 + lane < batch)};
         int turn = 0;
         for (int h = 0; h < 2; ++h)
             for (; bare[h] != 0u; bare[h] &= bare[h] - 1u)
@@ -1182,14 +1180,12 @@ cudaError_t launch_widen(WidenParams& P, int n_layers, int max_m, cudaStream_t s
 
 template <int R16, bool VEC>
 cudaError_t launch_decode(const DecodeParams& P, int n_layers, int max_count, cudaStream_t stream) {
-    // up to 64 rows an item for every adapter that they can name, and one for every 16 rows beyond that; more rows are prompts, with few adapters to 16 of
-    // them.  Clusters as large as leave the CTAs of one wave; those without an item end at once.
-    const bool gather = P.batch <= kGatherRows;
-    const int items = gather ? std::min(P.batch, max_count) + P.batch / 16 : (P.batch + 15) / 16 * 4;
+    // a window has an item for every adapter that its rows can name, and one for every 16 rows beyond that; where there are several windows, CTAs for the first 12 (the
+    // others come in turn).  Clusters as large as leave the CTAs of one wave; those without an item end at once.
+    const int windows = (P.batch + kWindow - 1) / kWindow, all = std::min(std::min(P.batch, kWindow), max_count) + std::min(P.batch, kWindow) / 16, items = windows == 1 ? all : std::min(all, 12);
     int c = Decode<R16>::kCluster;
-    while (c > 2 && (long long)items * n_layers * c > (R16 == 1 ? 296 : 222)) c /= 2;
-    const dim3 grid((unsigned)(gather ? c : items / 4 * c), (unsigned)(gather ? items : 4), (unsigned)n_layers);
-    return gather ? launch(decode_kernel<R16, VEC, true>, grid, c, Decode<R16>::kBytes, P, stream) : launch(decode_kernel<R16, VEC, false>, grid, c, Decode<R16>::kBytes, P, stream);
+    while (c > 2 && (long long)windows * items * n_layers * c > (R16 == 1 ? 296 : 222)) c /= 2;
+    return launch(decode_kernel<R16, VEC>, dim3((unsigned)(windows * c), (unsigned)items, (unsigned)n_layers), c, Decode<R16>::kBytes, P, stream);
 }
 
 template <int GROUPS>
@@ -1297,21 +1293,24 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         return e;
     };
     if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
-    // One launch behind the layer, or two?  The one reads the second factor again for every 16 rows, so rows times outputs decide (B200, us beyond the
-    // layer alone, one launch against two: 200 rows of 4096 x 4096 rank 16 to 32 9.8 / 15.1, 256 rows 9.9 / 11.8, 200 rows of 14336 x 4096 23 / 12; rank 64, 130 rows of
-    // 4096 x 4096 15.0 / 17.7, 65 rows of 14336 x 4096 17.9 / 13.3; outputs that are not 16-byte pieces, 4099 x 4096, rank 16 at 130 and 200 rows 11.6 / 12.7 and
-    // 17.0 / 14.2, rank 32 at 200 12.7 / 17.9).
+    // One launch behind the layer, or two?  The one reads the second factor again for every 16 rows, so rows times outputs decide; the two multiply every tile with
+    // each adapter in it, so where the pool has many to name the one is taken further (B200, us with the layer, one launch / two; few: up to three adapters in
+    // prompts, many: 30 among single tokens.  Rank 16, few: 256 rows of 4096 x 4096 24.8 / 25.6, 300 rows 29.7 / 27.8, 1024 rows of 1024 x 4096 27.0 / 29.5, 100 rows of 14336
+    // x 4096 31.6 / 27.4; many: 130 rows of 4096 x 4096 30 / 50, 512 rows 55 / 85, 100 rows of 14336 x 4096 46 / 59, 130 rows of 28672 x 4096 95 / 91.  Rank 64, few: 130
+    // rows of 4096 x 4096 23.9 / 26.2, 200 rows 29.9 / 28.3, 512 rows 47 / 39; many: 512 rows 111 / 141.  Outputs that are not 16-byte pieces, rank 16, few: 130 and 200 rows of
+    // 4099 x 4096 24.5 / 22.9 and 26.9 / 26.0).
     bool vec = true;
     long long outputs = 0;
-    int most_rank = 0;
+    int most_rank = 0, most_count = 0;
     for (int l = 0; l < n_layers; ++l) {
         if (!adapters[l]) continue;
         vec = vec && adapters[l]->n_out % 8 == 0;
         outputs += adapters[l]->n_out;
         most_rank = std::max(most_rank, adapters[l]->rank);
+        most_count = std::max(most_count, adapters[l]->count);
     }
-    const long long most = most_rank > 32 ? 3LL << 18 : vec || most_rank > 16 ? 1LL << 20 : 5LL << 17;
-    const bool decode = batch <= kGatherRows || (batch <= kDecodeRows && batch * outputs <= most);
+    const long long most = most_count > 8 ? 1LL << 21 : most_rank > 32 || (!vec && most_rank <= 16) ? 5LL << 17 : 1LL << 20;
+    const bool decode = batch <= kWindow || (batch <= kDecodeRows && batch * outputs <= most);
     cudaError_t e = cudaSuccess;
     // u beside the layer's last kernel where that one lets the next start late (the GEMM): what is before it is complete then, x, ids and the readers of u among
     // it, and u is made on the SMs that the GEMM leaves idle or leaves first (B200, layer and adapters, us, u before it / beside it: 300 rows of 1024 x 4096 rank

@@ -89,6 +89,22 @@ def test_adapted_linear(K, M, N, batch, r, n, kind):
     layer.free()
 
 
+@pytest.mark.parametrize("K,M,N,batch,r,n,kind", [
+    (2, 20008, 64, 70, 8, 3, "mixed"), (1, 9001, 96, 130, 16, 2, "prompts"), (2, 10504, 32, 200, 24, 3, "prompts"), (1, 9003, 64, 150, 31, 4, "mixed"), (1, 12000, 64, 100, 60, 4, "mixed"),
+    (1, 8209, 32, 129, 64, 2, "one"), (2, 8200, 32, 257, 100, 2, "mixed"), (1, 8191, 96, 300, 128, 2, "prompts"), (2, 5008, 288, 513, 12, 9, "mixed"), (1, 4104, 64, 700, 16, 3, "mixed"),
+    (1, 2003, 64, 1100, 30, 3, "mixed"), (1, 2000, 160, 1500, 70, 3, "prompts"), (2, 1200, 64, 1030, 110, 2, "prompts"), (1, 520, 64, 2050, 50, 3, "mixed"), (1, 264, 96, 2049, 128, 2, "prompts"),
+    (1, 261, 96, 2049, 16, 40, "mixed"), (1, 9000, 64, 600, 16, 3, "none")])
+def test_adapted_linear_in_two_launches(K, M, N, batch, r, n, kind):
+    """Rows times outputs beyond what one launch behind the layer takes, in all tile heights and ranks."""
+    test_adapted_linear(K, M, N, batch, r, n, kind)
+
+
+@pytest.mark.parametrize("batch", [130, 1025, 2050])
+def test_more_rows_of_a_group_and_what_is_not_finite(batch):
+    test_adapted_group_with_unlike_ranks_and_a_layer_without(batch)
+    test_what_is_not_finite_stays_in_its_rows(batch)
+
+
 def test_one_flat_row():
     import torch
     import paper_2602_05367_b200 as rabit
