@@ -300,6 +300,35 @@ def test_a_chain_of_calls_without_a_stop_between(variant, batch, r, kind):
 
 
 
+@pytest.mark.parametrize("batch,r,kind", [(5, 16, "mixed"), (40, 16, "mixed"), (40, 16, "none"), (1100, 64, "prompts"), (1100, 16, "none")])
+def test_a_captured_chain_of_calls(batch, r, kind):
+    """The same kernels beside one another in a replayed graph: bit for bit the calls one by one."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    side, n, steps = 512, 3, 4
+    L = make_layer(side, side, 2, key=(98,))
+    layer, A = rabit.rabit_pack(L.planes, (L.g.astype(np.float32) / 16).astype(np.float16), L.h), _adapters(*_pool(side, side, n, r, 13))
+    xd, idd = _cuda(make_x(batch, side, key=(99, batch)), _ids(batch, n, kind))
+    ys = [torch.zeros((batch, side), dtype=torch.float16, device="cuda") for _ in range(steps)]
+    u, s, graph = torch.zeros((batch, r), device="cuda"), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        for k in range(steps):
+            rabit.rabit_linear_adapted(layer, A, ys[k - 1] if k else xd, idd, ys[k], u)
+    for rep in range(3):
+        x = _cuda(make_x(batch, side, key=(99, batch, rep)))[0]
+        want = [x]
+        for k in range(steps):
+            want.append(rabit.rabit_linear_adapted(layer, A, want[-1], idd))
+            torch.cuda.synchronize()
+        xd.copy_(x)
+        for _ in range(2):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ys, want[1:]))
+    layer.free()
+
+
 def test_offsets_beyond_32_bits():
     """A pool of 4.4 GB whose last adapter is named, and its gradient of 8.8 GB."""
     import torch
