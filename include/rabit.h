@@ -194,7 +194,7 @@ RABIT_API int rabit_linear_group_adapted(const rabit_layer* const* layers, const
  *   x   DEVICE fp16 [batch][n_in], dy DEVICE fp16 [batch][n_out], 16-byte aligned
  *   u, p   DEVICE fp32 [batch][rank], 16-byte aligned
  *   da  DEVICE fp32 [count][rank][n_in], db DEVICE fp32 [count][rank][n_out], 16-byte aligned, not overlapping each other nor any input.
- *       accumulate = 0: overwritten (zero for an adapter that no row names); otherwise the gradients are added to what is there.
+ *       accumulate = 0: overwritten (zero for an adapter that no row names, whatever its scale is); otherwise the gradients are added to what is there.
  * Only the sizes, scale and nothing else of `adapters` is read.  Sums are fp32 in an order that the sizes and ids fix: the same call
  * gives the same bits.  u and p enter the products to 22 bits, or to 2^-40 of the largest entry of their rank in 64 rows.
  * What a row of another adapter, or of none, holds does not matter, be it infinite or NaN; of a row of the adapter's it makes the gradients that it

@@ -939,7 +939,7 @@ template <int GROUPS, bool VEC>
 __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_constant__ FactorParams P) {
     using F = Factor<GROUPS>;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int counts[kFactorWarps];
+    __shared__ int counts[kFactorWarps], found;
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, tq = lane & 3;
@@ -958,6 +958,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const bool prepare_first = (warp & 4) != 0;                                 // half of a scheduler's warps copy and split while the others multiply
     float sum[8][4] = {};
+    int n_rows = 0;                                                             // of the adapter, among the CTA's
     for (long long base = 0; base < P.batch; base += (long long)kFactorList * parts) {
         // the rows of this round that are the adapter's, in order
         int n_list = 0;
@@ -977,6 +978,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
             if (hit) list[before + __popc(hits & ((1u << lane) - 1u))] = (int)t;
             __syncthreads();
         }
+        n_rows += n_list;
         const int n_tiles = (n_list + F::kRows - 1) / F::kRows;
         auto fetch = [&](int tile) {
             unsigned char* stage = smem + tile % F::kStages * F::kStageBytes;
@@ -1090,13 +1092,18 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
             fours_of[e] = total;
         }
     }
+    if (threadIdx.x == 0) found = n_rows;
     cluster.sync();
-    const float scale = P.scale[adapter];
+    // An adapter that no row names has the gradient zero whatever its scale is (0 * NaN): its slot in the pool may never have been written.
+    int named = 0;
+#pragma unroll
+    for (int q = 0; q < kMaxCluster; ++q) named |= q < parts ? *cluster.map_shared_rank(&found, q) : 0;
+    const float scale = named != 0 ? P.scale[adapter] : 0.f;
     const int cols = min(F::kCols, side - first);
     const bool side_fours = side % 4 == 0;
     for (int e = part * kFactorThreads + threadIdx.x; e < rank * F::kCols / 4; e += parts * kFactorThreads) {
         const int j = e / (F::kCols / 4), c = e % (F::kCols / 4) * 4;
-        if (c >= cols) continue;
+        if (c >= cols || (P.accumulate && !named)) continue;
         float4 total = cluster_sum(cluster, sums, parts, e);
         total.x *= scale; total.y *= scale; total.z *= scale; total.w *= scale;
         float* at = S.out + ((size_t)adapter * rank + j) * side + first + c;
