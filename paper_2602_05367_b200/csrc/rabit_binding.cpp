@@ -78,6 +78,23 @@ bool stream_of(PyObject* arg, c10::DeviceIndex device, void** out) {
     return !(*out == nullptr && PyErr_Occurred());
 }
 
+c10::cuda::CUDAStream torch_stream(void* stream, c10::DeviceIndex device) {
+    if (stream == (void*)cudaStreamLegacy) stream = nullptr;                    // (another name of the default stream, which is no address)
+    return c10::cuda::getStreamFromExternal((cudaStream_t)stream, device);
+}
+
+// Memory that a call on `stream` makes comes from the allocator's pool of that stream: a block of another stream's pool may still be in use by work that is
+// pending there.  What the caller gets is recorded for torch's current stream as well, on which it is likely to be used.
+at::Tensor empty_on(at::IntArrayRef sizes, at::ScalarType type, c10::DeviceIndex device, void* stream, bool returned) {
+    const at::TensorOptions options = at::TensorOptions().dtype(type).device(at::kCUDA, device);
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(device);
+    if (stream == (void*)current.stream()) return at::empty(sizes, options);
+    c10::cuda::CUDAStreamGuard guard(torch_stream(stream, device));
+    at::Tensor t = at::empty(sizes, options);
+    if (returned) t.record_stream(current.unwrap());
+    return t;
+}
+
 inline bool is_cuda_half(PyObject* o) {
     if (!THPVariable_Check(o)) return false;
     const at::Tensor& t = THPVariable_Unpack(o);
@@ -97,17 +114,16 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const int64_t batch = flat ? 1 : x.size(0), cols = flat ? x.numel() : x.size(1);
     if (cols != N) return PyErr_Format(PyExc_ValueError, "x has %lld columns, layer expects %lld", (long long)cols, (long long)N);
     at::Tensor made;
-    void* yp;
+    void *yp, *stream;
+    if (!stream_of(args[3], x.device().index(), &stream)) return nullptr;
     if (args[2] == Py_None) {
-        made = at::empty({batch, M}, at::TensorOptions().dtype(at::kHalf).device(x.device()));
+        made = empty_on({batch, M}, at::kHalf, x.device().index(), stream, true);
         yp = made.data_ptr();
     } else {
         if (!is_cuda_half(args[2]) || THPVariable_Unpack(args[2]).numel() != batch * M)
             return PyErr_Format(PyExc_ValueError, "y must be a contiguous CUDA float16 tensor of batch*M elements");
         yp = THPVariable_Unpack(args[2]).data_ptr();
     }
-    void* stream;
-    if (!stream_of(args[3], x.device().index(), &stream)) return nullptr;
     const void* xp = x.data_ptr();
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -191,14 +207,6 @@ inline bool is_cuda(PyObject* o, at::ScalarType type, int64_t n, c10::DeviceInde
     return t.scalar_type() == type && t.is_cuda() && t.is_contiguous() && t.numel() == n && t.device().index() == device;
 }
 
-// Memory for u of a caller that does not want it: freed (to the allocator of torch's current stream) when the call returns, so another stream has to be recorded.
-at::Tensor scratch_u(int64_t batch, int64_t rank, const at::Device& device, void* stream) {
-    at::Tensor u = at::empty({batch, rank}, at::TensorOptions().dtype(at::kFloat).device(device));
-    if (stream != (void*)c10::cuda::getCurrentCUDAStream(device.index()).stream())
-        u.record_stream(c10::cuda::getStreamFromExternal((cudaStream_t)stream, device.index()).unwrap());
-    return u;
-}
-
 // linear_adapted(layer, adapters, x, ids, y | None, u | None, stream | None) -> y
 PyObject* linear_adapted(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 7) return PyErr_Format(PyExc_TypeError, "linear_adapted takes 7 arguments");
@@ -219,7 +227,7 @@ PyObject* linear_adapted(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     void *yp, *stream;
     if (!stream_of(args[6], device, &stream)) return nullptr;
     if (args[4] == Py_None) {
-        made = at::empty({batch, M}, at::TensorOptions().dtype(at::kHalf).device(x.device()));
+        made = empty_on({batch, M}, at::kHalf, device, stream, true);
         yp = made.data_ptr();
     } else {
         if (!is_cuda(args[4], at::kHalf, batch * M, device)) return PyErr_Format(PyExc_ValueError, "y must be a contiguous CUDA float16 tensor of batch*M elements on the device of x");
@@ -227,7 +235,7 @@ PyObject* linear_adapted(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     }
     float* up;
     if (args[5] == Py_None) {
-        made_u = scratch_u(batch, A->rank, x.device(), stream);
+        made_u = empty_on({batch, A->rank}, at::kFloat, device, stream, false);
         up = made_u.data_ptr<float>();
     } else {
         if (!is_cuda(args[5], at::kFloat, batch * A->rank, device)) return PyErr_Format(PyExc_ValueError, "u must be a contiguous CUDA float32 tensor of batch*rank elements on the device of x");
@@ -292,7 +300,7 @@ PyObject* linear_group_adapted(PyObject*, PyObject* const* args, Py_ssize_t narg
         if (!ap[l]) continue;
         const int64_t rank = ((const rabit_adapters*)ap[l])->rank;
         if (uo == Py_None) {
-            made.push_back(scratch_u(batch, rank, THPVariable_Unpack(xo).device(), stream));
+            made.push_back(empty_on({batch, rank}, at::kFloat, device, stream, false));
             up[l] = made.back().data_ptr();
         } else {
             if (!is_cuda(uo, at::kFloat, batch * rank, device)) return PyErr_Format(PyExc_ValueError, "every u must be a contiguous CUDA float32 tensor of batch*rank elements, all on one device");
@@ -337,7 +345,7 @@ PyObject* adapter_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
     THPObjectPtr made[2];
     float* out[2];
     for (int i = 0; i < 2; ++i) {
-        if (args[6 + i] == Py_None) made[i] = THPVariable_Wrap(at::empty({A->count, A->rank, i == 0 ? A->n_in : A->n_out}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, device)));
+        if (args[6 + i] == Py_None) made[i] = THPVariable_Wrap(empty_on({A->count, A->rank, i == 0 ? A->n_in : A->n_out}, at::kFloat, device, stream, true));
         else made[i] = Py_NewRef(args[6 + i]);
         out[i] = THPVariable_Unpack(made[i].get()).data_ptr<float>();
     }
@@ -369,7 +377,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     void* stream;
     if (!stream_of(args[3], device, &stream)) return nullptr;
     c10::cuda::CUDAGuard guard(device);
-    THPObjectPtr norm(args[2] == Py_None ? THPVariable_Wrap(at::empty({1}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, device))) : Py_NewRef(args[2]));
+    THPObjectPtr norm(args[2] == Py_None ? THPVariable_Wrap(empty_on({1}, at::kFloat, device, stream, true)) : Py_NewRef(args[2]));
     float* out = THPVariable_Unpack(norm.get()).data_ptr<float>();
     int rc;
     Py_BEGIN_ALLOW_THREADS

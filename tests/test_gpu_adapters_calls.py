@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import adapters_oracle as ao
+from synth import make_layer, make_x
 from tests.test_gpu_adapters import _adapters, _cuda, _pool, _within
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,61 @@ def test_a_slot_that_no_row_names_may_hold_any_scale(batch, r, bad):
     assert abs(float(norm) - want_norm) <= 2.0 ** -23 * want_norm
     for got, w in zip((da, db), clipped):
         assert (np.abs(got.cpu().numpy() - w) <= 2.0 ** -22 * np.abs(w) + 2.0 ** -149).all()
+
+
+def _busy(stream):
+    """Some 50 ms of work on it."""
+    import torch
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(100_000_000)
+
+
+@pytest.mark.parametrize("batch", [3, 40, 300])
+@pytest.mark.parametrize("call", ["linear", "u", "y", "group u", "gradients", "norm"])
+def test_memory_that_a_call_makes_for_another_stream_is_not_in_use(call, batch):
+    """Blocks that were just dropped, but that torch's stream has still to read: a call on another stream must not be given them."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    M, N, n, r = 2048, 1024, 2, 16
+    L = make_layer(M, N, 2, key=(111,))
+    a, b, scale = _pool(M, N, n, r, 60)
+    layer, A = rabit.rabit_pack(L.planes, L.g, L.h), _adapters(a, b, scale)
+    rng = np.random.default_rng(61)
+    x, ids = make_x(batch, N, key=(111, batch)), np.zeros(batch, np.int32)
+    dy, p = rng.standard_normal((batch, M)).astype(np.float16), rng.standard_normal((batch, r)).astype(np.float32)
+    xd, idd, dyd, pd = _cuda(x, ids, dy, p)
+    y, u = torch.empty((batch, M), dtype=torch.float16, device="cuda"), torch.empty((batch, r), device="cuda")
+    want_plain = rabit.rabit_linear(layer, xd)
+    want_y = rabit.rabit_linear_adapted(layer, A, xd, idd, None, u)
+    want_da, want_db = rabit.rabit_adapter_gradients(A, xd, u, dyd, pd, idd)
+    shape, dtype = {"linear": (want_plain.shape, torch.float16), "y": (want_plain.shape, torch.float16), "gradients": (want_da.shape, torch.float32),
+                    "norm": ((1,), torch.float32)}.get(call, ((batch, r), torch.float32))
+    G = rabit.RabitGradients([torch.full((100,), 3.0, device="cuda")])
+    torch.cuda.synchronize()
+    here, there = torch.cuda.current_stream(), torch.cuda.Stream()
+    blocks = [torch.full(shape, 7.0, dtype=dtype, device="cuda") for _ in range(24)]
+    kept = torch.zeros((24,) + tuple(shape), dtype=dtype, device="cuda")
+    torch.cuda.synchronize()
+    _busy(here)
+    for i, block in enumerate(blocks):
+        kept[i].copy_(block)
+    del blocks, block
+    s = there.cuda_stream
+    if call == "linear":
+        got, want = [rabit.rabit_linear(layer, xd, stream=s)], [want_plain]
+    elif call == "u":
+        got, want = [rabit.rabit_linear_adapted(layer, A, xd, idd, y, None, s)], [want_y]
+    elif call == "y":
+        got, want = [rabit.rabit_linear_adapted(layer, A, xd, idd, None, u, s)], [want_y]
+    elif call == "group u":
+        got, want = rabit.rabit_linear_group_adapted([layer], [A], [xd], idd, [y], None, s), [want_y]
+    elif call == "gradients":
+        got, want = rabit.rabit_adapter_gradients(A, xd, u, dyd, pd, idd, stream=s), [want_da, want_db]
+    else:
+        got, want = [rabit.rabit_clip_gradients(G, 1e3, stream=s)], [torch.full((1,), 30.0, device="cuda")]
+    there.synchronize()
+    assert not here.query()                                                             # (it is still busy: the call was beside it)
+    torch.cuda.synchronize()
+    assert bool((kept == 7.0).all())
+    assert all(torch.equal(v, w) for v, w in zip(got, want))
+    layer.free()
