@@ -45,6 +45,7 @@ ErrorFn p_error = nullptr;
 PyObject* g_error_type = nullptr;      // RabitError
 PyObject* g_addr_name = nullptr;       // "_addr": the descriptor's address on a RabitLayer, None once freed; on a RabitAdapters that of its rabit_adapters
 
+PyObject* g_buf_name = nullptr;        // "dev_buf": the device memory of a RabitGradients
 PyObject* g_device_name = nullptr;     // "_device": the index of the device that a RabitAdapters or RabitGradients lives on
 
 constexpr Py_ssize_t kInline = 16;     // layers of a group whose pointers need no allocation
@@ -379,6 +380,10 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     c10::cuda::CUDAGuard guard(device);
     THPObjectPtr norm(args[2] == Py_None ? THPVariable_Wrap(empty_on({1}, at::kFloat, device, stream, true)) : Py_NewRef(args[2]));
     float* out = THPVariable_Unpack(norm.get()).data_ptr<float>();
+    // the table and the partial sums belong to the RabitGradients, which may be freed before the stream has come this far
+    THPObjectPtr buf(PyObject_GetAttr(args[0], g_buf_name));
+    if (!buf) return nullptr;
+    if (THPVariable_Check(buf.get())) THPVariable_Unpack(buf.get()).record_stream(torch_stream(stream, device).unwrap());
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = p_clip(h, (float)max_norm, out, stream);
@@ -456,5 +461,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rabit_binding", nullptr, -1, meth
 PyMODINIT_FUNC PyInit__rabit_binding(void) {
     g_addr_name = PyUnicode_InternFromString("_addr");
     g_device_name = PyUnicode_InternFromString("_device");
-    return g_addr_name && g_device_name ? PyModule_Create(&module) : nullptr;
+    g_buf_name = PyUnicode_InternFromString("dev_buf");
+    return g_addr_name && g_device_name && g_buf_name ? PyModule_Create(&module) : nullptr;
 }

@@ -98,3 +98,26 @@ def test_memory_that_a_call_makes_for_another_stream_is_not_in_use(call, batch):
     assert bool((kept == 7.0).all())
     assert all(torch.equal(v, w) for v, w in zip(got, want))
     layer.free()
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_what_a_clipping_on_another_stream_needs_outlives_its_owners(in_place):
+    """The norm is not looked at, the RabitGradients is freed at once, and their memory is asked for again before the stream has come so far."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    t, hold = torch.full((10000,), 2.0, device="cuda"), torch.full((10000,), 2.0, device="cuda")
+    there = torch.cuda.Stream()
+    G = rabit.RabitGradients([t], None if in_place else [hold])
+    torch.zeros(16, device="cuda").to(torch.uint8).fill_(0)                             # (the first launch of a kernel waits for the device)
+    rabit.rabit_clip_gradients(rabit.RabitGradients([torch.ones(9, device="cuda")]), 1.0)
+    torch.cuda.synchronize()
+    _busy(there)
+    rabit.rabit_clip_gradients(G, 1.0, stream=there.cuda_stream)
+    size = G.dev_buf.numel()
+    G.free()
+    others = [torch.full((size,), 0, dtype=torch.uint8, device="cuda") for _ in range(8)] + [torch.full((1,), 5.0, device="cuda") for _ in range(8)]
+    torch.cuda.current_stream().synchronize()
+    assert not there.query()
+    torch.cuda.synchronize()
+    assert all(bool((v == v.flatten()[0]).all()) and float(v.flatten()[0]) in (0.0, 5.0) for v in others)
+    assert float(((t if in_place else hold) - 0.01).abs().max()) < 1e-8 and (in_place or bool((t == 2.0).all()))
