@@ -124,6 +124,11 @@ def _stream_of(device, stream: Optional[int]) -> int:
     return _native.current_stream(torch.cuda.current_device() if device.index is None else device.index)
 
 
+def _empty(nbytes: int, device, stream: int):
+    """Device memory of a call on `stream`: from the allocator's pool of that stream, where nothing pending elsewhere can still use it."""
+    return _native.empty(nbytes, torch.cuda.current_device() if device.index is None else device.index, stream)
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -238,8 +243,8 @@ def rabit_pack(planes, g, h, device="cuda:0", stream: Optional[int] = None) -> R
     if nbytes == 0:
         raise RabitError(-2, f"unsupported shape K={K} M={M} N={N}")
     dev = torch.device(device)
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     st = _stream_of(dev, stream)
+    buf = _empty(nbytes, dev, st)
     out = _c_void_p()
     with torch.cuda.device(dev):
         _check(_lib.rabit_pack(planes.ctypes.data, g16.ctypes.data, h16.ctypes.data, K, M, N,
@@ -261,8 +266,8 @@ def rabit_derive_pack(W, g, h, stream: Optional[int] = None) -> RabitLayer:
     nbytes = packed_bytes(K, M, N)
     if nbytes == 0:
         raise RabitError(-2, f"unsupported shape K={K} M={M} N={N}")
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
     st = _stream_of(W.device, stream)
+    buf = _empty(nbytes, W.device, st)
     out = _c_void_p()
     with torch.cuda.device(W.device):
         _check(_lib.rabit_derive_pack(_c_void_p(W.data_ptr()), g16.ctypes.data, h16.ctypes.data, K, M, N,
@@ -296,9 +301,9 @@ def rabit_linear_group_host(layers, xs_host, ys_host, stream: Optional[int] = No
     h = (_c_void_p * n)(*[L.handle for L in layers])
     need = int(_lib.rabit_group_stage_bytes(h, n, batch))
     first = layers[0]
-    if first._stage is None or first._stage.numel() < need:
-        first._stage = torch.empty(need, dtype=torch.uint8, device=first.dev_buf.device)
     st = _stream_of(first.dev_buf.device, stream)
+    if first._stage is None or first._stage.numel() < need:
+        first._stage = _empty(need, first.dev_buf.device, st)
     xp = (_c_void_p * n)(*[x.data_ptr() for x in xs_host])
     yp = (_c_void_p * n)(*[y.data_ptr() for y in ys_host])
     _check(_lib.rabit_linear_group_host(h, xp, yp, n, batch, _c_void_p(first._stage.data_ptr()), need, _c_void_p(st)))
@@ -349,9 +354,9 @@ def rabit_linear_host(layer: RabitLayer, x_host, y_host, stream: Optional[int] =
     if x_host.numel() != batch * layer.N or y_host.numel() != batch * layer.M:
         raise ValueError("x_host / y_host sizes do not match the layer")
     need = int(_lib.rabit_stage_bytes(layer.handle, batch))
-    if layer._stage is None or layer._stage.numel() < need:
-        layer._stage = torch.empty(need, dtype=torch.uint8, device=layer.dev_buf.device)
     st = _stream_of(layer.dev_buf.device, stream)
+    if layer._stage is None or layer._stage.numel() < need:
+        layer._stage = _empty(need, layer.dev_buf.device, st)
     _check(_lib.rabit_linear_host(layer.handle, _c_void_p(x_host.data_ptr()), _c_void_p(y_host.data_ptr()), batch,
                                   _c_void_p(layer._stage.data_ptr()), need, _c_void_p(st)))
     return y_host
@@ -422,8 +427,8 @@ def rabit_transpose(layer: RabitLayer, stream: Optional[int] = None) -> RabitLay
     nbytes = packed_bytes(K, M, N)
     if nbytes == 0:
         raise RabitError(-2, f"rabit_transpose: the layer's M = {N} becomes the contraction and must be a multiple of 32")
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     st = _stream_of(dev, stream)
+    buf = _empty(nbytes, dev, st)
     out = _c_void_p()
     with torch.cuda.device(dev):
         _check(_lib.rabit_transpose(handle, _c_void_p(buf.data_ptr()), nbytes, _c_void_p(st), ctypes.byref(out)))
@@ -457,10 +462,11 @@ class RabitGradients:
         nbytes = int(_lib.rabit_gradients_bytes(counts, n))
         self._addr = None                               # the descriptor, for the native module; None once freed
         self._device = dev.index
-        self.dev_buf = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        st = _stream_of(dev, stream)
+        self.dev_buf = _empty(nbytes, dev, st)
         out = _c_void_p()
         with torch.cuda.device(dev):
-            _check(_lib.rabit_gradients_bind(src, dst, counts, n, _c_void_p(self.dev_buf.data_ptr()), nbytes, _c_void_p(_stream_of(dev, stream)), ctypes.byref(out)))
+            _check(_lib.rabit_gradients_bind(src, dst, counts, n, _c_void_p(self.dev_buf.data_ptr()), nbytes, _c_void_p(st), ctypes.byref(out)))
         self._addr = out.value
 
     def free(self) -> None:

@@ -421,6 +421,18 @@ PyObject* current_stream(PyObject*, PyObject* arg) {
     END_HANDLE_TH_ERRORS
 }
 
+// empty(bytes, device index, stream) -> uint8 tensor for a call on that stream
+PyObject* empty_bytes(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 3) return PyErr_Format(PyExc_TypeError, "empty takes 3 arguments");
+    HANDLE_TH_ERRORS
+    const long long n = PyLong_AsLongLong(args[0]);
+    const long device = PyLong_AsLong(args[1]);
+    void* stream;
+    if (PyErr_Occurred() || !stream_of(args[2], (c10::DeviceIndex)device, &stream)) return nullptr;
+    return THPVariable_Wrap(empty_on({(int64_t)n}, at::kByte, (c10::DeviceIndex)device, stream, true));
+    END_HANDLE_TH_ERRORS
+}
+
 // init(error type, address of rabit_linear, _linear_group, _linear_group_host, _layer_M, _layer_N, _last_error, _linear_adapted, _linear_group_adapted,
 // _adapter_gradients, _clip_gradients)
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
@@ -451,6 +463,7 @@ PyMethodDef methods[] = {
     {"adapter_gradients", (PyCFunction)(void (*)(void))adapter_gradients, METH_FASTCALL, nullptr},
     {"clip", (PyCFunction)(void (*)(void))clip, METH_FASTCALL, nullptr},
     {"group_host", (PyCFunction)(void (*)(void))group_host, METH_FASTCALL, nullptr},
+    {"empty", (PyCFunction)(void (*)(void))empty_bytes, METH_FASTCALL, nullptr},
     {"current_stream", current_stream, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -121,3 +121,29 @@ def test_what_a_clipping_on_another_stream_needs_outlives_its_owners(in_place):
     torch.cuda.synchronize()
     assert all(bool((v == v.flatten()[0]).all()) and float(v.flatten()[0]) in (0.0, 5.0) for v in others)
     assert float(((t if in_place else hold) - 0.01).abs().max()) < 1e-8 and (in_place or bool((t == 2.0).all()))
+
+
+def test_a_layer_made_on_another_stream_is_not_in_memory_in_use():
+    import torch
+    import paper_2602_05367_b200 as rabit
+    L = make_layer(256, 512, 2, key=(112,))
+    image = rabit.pack_host(L.planes, L.g, L.h)
+    layer = rabit.rabit_pack(L.planes, L.g, L.h)
+    turned = rabit.rabit_transpose(layer)
+    want = turned.dev_buf.clone()
+    here, there = torch.cuda.current_stream(), torch.cuda.Stream()
+    blocks = [torch.full((v.numel(),), 7, dtype=torch.uint8, device="cuda") for v in 12 * [layer.dev_buf, turned.dev_buf]]
+    kept = [torch.zeros_like(v) for v in blocks]
+    torch.cuda.synchronize()
+    _busy(here)
+    for k, block in zip(kept, blocks):
+        k.copy_(block)
+    del blocks, block
+    made = rabit.rabit_pack(L.planes, L.g, L.h, stream=there.cuda_stream), rabit.rabit_transpose(layer, stream=there.cuda_stream)
+    there.synchronize()
+    assert not here.query()
+    torch.cuda.synchronize()
+    assert all(bool((k == 7).all()) for k in kept)
+    assert np.array_equal(made[0].dev_buf.cpu().numpy(), image) and torch.equal(made[1].dev_buf, want)
+    for v in (layer, turned) + made:
+        v.free()
