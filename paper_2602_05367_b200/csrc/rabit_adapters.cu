@@ -1300,6 +1300,8 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         return e;
     };
     if (int rc = check_layers(who, layers, xs, ys, n_layers, batch)) return rc;
+    for (int l = 0; l < n_layers; ++l)
+        if (int rc = rabit_check_call(*layers[l], batch)) return rc;
     // One launch behind the layer, or two?  The one reads the second factor again for every 16 rows, so rows times outputs decide; the two multiply every tile with
     // each adapter in it, so where the pool has many to name the one is taken further (B200, us with the layer, one launch / two; few: up to three adapters in
     // prompts, many: 30 among single tokens.  Rank 16, few: 256 rows of 4096 x 4096 24.8 / 25.6, 300 rows 29.7 / 27.8, 1024 rows of 1024 x 4096 27.0 / 29.5, 100 rows of 14336

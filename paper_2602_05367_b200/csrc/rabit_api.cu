@@ -195,6 +195,40 @@ static bool ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
 // 4096 x 4096 6.8 / 8.4 / 8.9 against 7.5, 14336 x 4096 13 / 18.3 / 20.6 against 14.6, 28672 x 8192 38 / 54 / 55 against 40).
 static const int kF16Rows = 8;
 
+// The kernel family that a call on one layer takes (numbers as in rabit_set_variant).
+static int choose_variant(const rabit_layer& L, int batch) {
+    const RabitGeom& G = L.geom;
+    if (L.variant != 0) return L.variant;
+    const rabit_layer* one = &L;
+    if (rabit_gemv_lut_supports(L, batch) && rabit_gemv_lut_preferred(&one, 1, batch)) return 5;
+    if (batch > RABIT_MAX_GEMV_BATCH) return rabit_gemm_tc_supports(L, batch) ? 3 : 1;
+    if (rabit_gemv_f16_supports(L, kF16Rows)) return 6;    // the f16 GEMV, beyond kF16Rows the GEMM (also two rows of small layers of three paths)
+    if (!rabit_gemv_mma_supports(L, batch)) return 1;
+    // Layers of more than 255 slices, or beyond the f16 GEMV's 32-bit offsets.  From 5 batch rows on the integer-MMA GEMV
+    // makes two to four passes over the weights; the tensor-core GEMM, which costs the same from 1 to 16 rows, is then
+    // often cheaper.  Both estimates are fits to measurements on B200 (us): a GEMV pass of four rows costs
+    // 10 + max(0, packed MB - 4) / 1.3.
+    if (batch > 4 && rabit_gemm_tc_supports(L, batch)) {
+        const double packed_mb = (double)G.K * G.Mp * G.N / 8.0e6;
+        const double passes = (double)((batch + rabit_gemv_mma_max_rows() - 1) / rabit_gemv_mma_max_rows());
+        const double gemv_us = passes * (10.0 + (packed_mb > 4.0 ? (packed_mb - 4.0) / 1.3 : 0.0));
+        const double gemm_us = rabit_gemm_tc_estimate_us(L, batch);
+        if (gemm_us < 0.9 * gemv_us) return 3;
+    }
+    return 2;
+}
+
+static int check_variant(const rabit_layer& L, int variant, int batch) {
+    if (variant == 2 && !rabit_gemv_mma_supports(L, batch)) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: integer-MMA GEMV cannot run batch %d", batch);
+    if ((variant == 3 || variant == 4) && !rabit_gemm_tc_supports(L, batch)) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: tcgen05 GEMM cannot run batch %d", batch);
+    if (variant == 5 && !rabit_gemv_lut_supports(L, 1)) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: table-driven GEMV cannot run this layer");
+    if (variant == 6 && (!rabit_gemv_f16_supports(L, std::min(batch, kF16Rows)) || (batch > kF16Rows && !rabit_gemm_tc_supports(L, batch))))
+        return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: f16 tensor-core GEMV cannot run this layer");
+    return RABIT_OK;
+}
+
+int rabit_check_call(const rabit_layer& L, int batch) { return check_variant(L, L.variant, batch); }
+
 static int linear_call(const rabit_layer* layer, const void* x, void* y, int batch, void* stream) {
     rabit_clear_error();
     if (!layer) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: layer is NULL");
@@ -213,62 +247,27 @@ static int linear_call(const rabit_layer* layer, const void* x, void* y, int bat
             return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: the layer lives on device %d but device %d is current", layer->device, dev);
     }
 
-    int variant = layer->variant;
-    if (variant == 0) {
-        if (rabit_gemv_lut_supports(*layer, batch) && rabit_gemv_lut_preferred(&layer, 1, batch)) {
-            variant = 5;
-        } else if (batch <= RABIT_MAX_GEMV_BATCH && rabit_gemv_f16_supports(*layer, kF16Rows)) {
-            variant = 6;                    // the f16 GEMV, beyond kF16Rows the GEMM (also two rows of small layers of three paths)
-        } else if (batch <= RABIT_MAX_GEMV_BATCH) {
-            variant = rabit_gemv_mma_supports(*layer, batch) ? 2 : 1;
-            // Layers of more than 255 slices, or beyond the f16 GEMV's 32-bit offsets.  From 5 batch rows on the integer-MMA GEMV
-            // makes two to four passes over the weights; the tensor-core GEMM, which costs the same from 1 to 16 rows, is then
-            // often cheaper.  Both estimates are fits to measurements on B200 (us): a GEMV pass of four rows costs
-            // 10 + max(0, packed MB - 4) / 1.3.
-            if (variant == 2 && batch > 4 && rabit_gemm_tc_supports(*layer, batch)) {
-                const double packed_mb = (double)G.K * G.Mp * G.N / 8.0e6;
-                const double passes = (double)((batch + rabit_gemv_mma_max_rows() - 1) / rabit_gemv_mma_max_rows());
-                const double gemv_us = passes * (10.0 + (packed_mb > 4.0 ? (packed_mb - 4.0) / 1.3 : 0.0));
-                const double gemm_us = rabit_gemm_tc_estimate_us(*layer, batch);
-                if (gemm_us < 0.9 * gemv_us) variant = 3;
-            }
-        } else {
-            variant = rabit_gemm_tc_supports(*layer, batch) ? 3 : 1;
-        }
-    }
-    cudaError_t e;
+    const int variant = choose_variant(*layer, batch);
+    if (int rc = check_variant(*layer, variant, batch)) return rc;
+    cudaError_t e = cudaSuccess;
     switch (variant) {
         case 2:
-            if (!rabit_gemv_mma_supports(*layer, batch))
-                return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: integer-MMA GEMV cannot run batch %d", batch);
-            e = cudaSuccess;
             for (int b0 = 0; b0 < batch && e == cudaSuccess; b0 += rabit_gemv_mma_max_rows())   // up to 4 batch rows share one pass over the weights
                 e = rabit_launch_gemv_mma(*layer, (const char*)x + (size_t)b0 * G.N * 2, (char*)y + (size_t)b0 * G.M * 2,
                                           batch - b0 >= rabit_gemv_mma_max_rows() ? rabit_gemv_mma_max_rows() : batch - b0, st);
             break;
         case 3:
-            if (!rabit_gemm_tc_supports(*layer, batch))
-                return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: tcgen05 GEMM cannot run batch %d", batch);
-            e = rabit_launch_gemm_tc(*layer, x, y, batch, st);
-            break;
         case 4:
-            if (!rabit_gemm_tc_supports(*layer, batch))
-                return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: tcgen05 GEMM cannot run batch %d", batch);
-            e = rabit_launch_gemm_tc(*layer, x, y, batch, st, true);
+            e = rabit_launch_gemm_tc(*layer, x, y, batch, st, variant == 4);
             break;
         case 5: {
-            if (!rabit_gemv_lut_supports(*layer, 1))
-                return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: table-driven GEMV cannot run this layer");
             const int rows = rabit_gemv_lut_supports(*layer, rabit_gemv_lut_max_rows()) ? rabit_gemv_lut_max_rows() : 1;
-            e = cudaSuccess;
             for (int b0 = 0; b0 < batch && e == cudaSuccess; b0 += rows)             // up to `rows` batch rows share one pass over the weights
                 e = rabit_launch_gemv_lut(*layer, (const char*)x + (size_t)b0 * G.N * 2, (char*)y + (size_t)b0 * G.M * 2,
                                           batch - b0 >= rows ? rows : batch - b0, st);
             break;
         }
         case 6:                             // beyond eight rows the GEMM (see kF16Rows)
-            if (!rabit_gemv_f16_supports(*layer, std::min(batch, kF16Rows)) || (batch > kF16Rows && !rabit_gemm_tc_supports(*layer, batch)))
-                return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: f16 tensor-core GEMV cannot run this layer");
             e = batch <= kF16Rows ? rabit_launch_gemv_f16(*layer, x, y, batch, st) : rabit_launch_gemm_tc(*layer, x, y, batch, st);
             break;
         default:
@@ -351,7 +350,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
         }
         if (f16) {                                               // unlike path counts, or one layer twice: launch by launch
             for (int l = 0; l < n_layers; ++l) {
-                int rc = rabit_linear(layers[l], xs[l], ys[l], batch, stream);
+                int rc = linear_call(layers[l], xs[l], ys[l], batch, stream);
                 if (rc != RABIT_OK) return rc;
             }
             return RABIT_OK;
@@ -361,7 +360,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
         for (int b = a + 1; b < n_layers; ++b)
             if (layers[a] == layers[b]) {                        // the same layer twice would share one reduction scratch: no fused launch
                 for (int l = 0; l < n_layers; ++l) {
-                    int rc = rabit_linear(layers[l], xs[l], ys[l], batch, stream);
+                    int rc = linear_call(layers[l], xs[l], ys[l], batch, stream);
                     if (rc != RABIT_OK) return rc;
                 }
                 return RABIT_OK;
@@ -370,7 +369,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
     for (int l = 0; l < n_layers && fused; ++l) fused = layers[l]->variant == 0 || layers[l]->variant == 2;
     if (!fused) {
         for (int l = 0; l < n_layers; ++l) {
-            int rc = rabit_linear(layers[l], xs[l], ys[l], batch, stream);
+            int rc = linear_call(layers[l], xs[l], ys[l], batch, stream);
             if (rc != RABIT_OK) return rc;
         }
         return RABIT_OK;

@@ -75,6 +75,7 @@ cudaError_t rabit_launch_transpose(const RabitGeom& G, const RabitHeader& hdr, c
 cudaError_t rabit_launch_fetch(const void* const* src, void* const* dst, const size_t* bytes, int n, cudaStream_t stream);
 
 bool rabit_ends_late(const rabit_layer& L, int batch);
+int rabit_check_call(const rabit_layer& L, int batch);      // what rabit_linear refuses because of a kernel family that was set (the automatic choice runs)
 inline bool rabit_ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
     const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
     return a0 < b0 + bn && b0 < a0 + an;

@@ -147,3 +147,30 @@ def test_a_layer_made_on_another_stream_is_not_in_memory_in_use():
     assert np.array_equal(made[0].dev_buf.cpu().numpy(), image) and torch.equal(made[1].dev_buf, want)
     for v in (layer, turned) + made:
         v.free()
+
+
+@pytest.mark.parametrize("variant,batch,M", [(2, 70, 520), (2, 1100, 1031), (6, 300, 520)])
+def test_what_the_layer_refuses_leaves_y_and_u_as_they_were(variant, batch, M):
+    """A kernel family that cannot run the batch: nothing of the call has run, in a group nothing of the layers before it either."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    N, n, r = 64, 3, 8
+    Ls = [make_layer(M, N, 2, key=(110, M, i)) for i in range(2)]
+    layers, pools = [rabit.rabit_pack(L.planes, L.g, L.h) for L in Ls], [_adapters(*_pool(M, N, n, r, 50 + i)) for i in range(2)]
+    xd, idd = _cuda(make_x(batch, N, key=(110, batch)), np.zeros(batch, np.int32))
+    ys = [torch.full((batch, M), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+    us = [torch.full((batch, r), 7.0, device="cuda") for _ in range(2)]
+    layers[1].set_variant(variant)
+    refused = variant == 2                                                              # (6 takes the GEMM here: the same call answered)
+    for call in (lambda: rabit.rabit_linear_adapted(layers[1], pools[1], xd, idd, ys[1], us[1]), lambda: rabit.rabit_linear_group_adapted(layers, pools, [xd, xd], idd, ys, us)):
+        if refused:
+            with pytest.raises(rabit.RabitError, match="cannot run"):
+                call()
+        else:
+            call()
+        torch.cuda.synchronize()
+        assert not refused or all(bool((t == 7.0).all()) for t in ys + us)
+    if not refused:
+        assert not any(bool((t == 7.0).all()) for t in ys + us)
+    for layer in layers:
+        layer.free()
