@@ -1284,8 +1284,8 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
     RABIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev != layers[0]->device) return rabit_fail(RABIT_INVALID_ARG, "%s: the layers live on device %d but device %d is current", who, layers[0]->device, dev);
 
-    // u of all adapted layers before or beside the layers themselves, then the adapters' part on top of their outputs.  What the layers' calls refuse, they refuse
-    // before anything of this call has run.
+    // The layers, u of all adapted ones beside or behind the last kernel of that, then the adapters' part on top of the outputs.  What the layers' calls refuse is
+    // refused before anything of this call has run.
     int at[kMaxGroup], n = 0;
     auto each_group = [&](auto&& body) {
         cudaError_t e = cudaSuccess;
@@ -1320,14 +1320,14 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
     }
     const long long most = most_count > 8 ? 1LL << 21 : most_rank > 32 || (!vec && most_rank <= 16) ? 5LL << 17 : 1LL << 20;
     const bool decode = batch <= kWindow || (batch <= kDecodeRows && batch * outputs <= most);
-    cudaError_t e = cudaSuccess;
-    // u beside the layer's last kernel where that one lets the next start late (the GEMM): what is before it is complete then, x, ids and the readers of u among
+    bool beside = false;
+    if (int rc = rabit_run_layers(layers, xs, ys, n_layers, batch, stream, &beside)) return rc;
+    // Beside the layer's last kernel where that one lets the next start late (the GEMM): what is before the layer is complete then, x, ids and the readers of u among
     // it, and u is made on the SMs that the GEMM leaves idle or leaves first (B200, layer and adapters, us, u before it / beside it: 300 rows of 1024 x 4096 rank
-    // 16 21.9 / 19.5, 1200 rows of 11008 x 4096 rank 128 242 / 236, 4096 rows of 11008 x 4096 rank 16 633 / 626).  Behind another kernel u would have to wait: it comes first.
-    bool beside = true;
-    for (int l = 0; l < n_layers; ++l) beside = beside && rabit_ends_late(*layers[l], batch);
-    auto narrow = [&] {
-        return each_group([&] {
+    // 16 21.9 / 19.5, 1200 rows of 11008 x 4096 rank 128 242 / 236, 4096 rows of 11008 x 4096 rank 16 633 / 626).  Behind another kernel u waits for it.
+    cudaError_t e = cudaSuccess;
+    if (!decode) {
+        e = each_group([&] {
             NarrowParams P{};
             P.ids = ids;
             P.batch = batch;
@@ -1340,15 +1340,6 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
             }
             return launch_narrow(P, n, max_rank, st);
         });
-    };
-    if (!decode && !beside) {
-        e = narrow();
-        if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
-    }
-    int rc = n_layers == 1 ? rabit_linear(layers[0], xs[0], ys[0], batch, stream) : rabit_linear_group(layers, xs, ys, n_layers, batch, stream);
-    if (rc != RABIT_OK) return rc;
-    if (!decode && beside) {
-        e = narrow();
         if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "%s: launch failed: %s", who, cudaGetErrorString(e));
     }
     e = each_group([&] {

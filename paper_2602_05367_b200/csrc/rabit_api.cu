@@ -229,7 +229,8 @@ static int check_variant(const rabit_layer& L, int variant, int batch) {
 
 int rabit_check_call(const rabit_layer& L, int batch) { return check_variant(L, L.variant, batch); }
 
-static int linear_call(const rabit_layer* layer, const void* x, void* y, int batch, void* stream) {
+// ends_late: whether the call's last kernel lets the next one of the stream start only when all work before the call is complete.
+static int linear_call(const rabit_layer* layer, const void* x, void* y, int batch, void* stream, bool* ends_late) {
     rabit_clear_error();
     if (!layer) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: layer is NULL");
     if (!x || !y) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear: null x or y");
@@ -249,6 +250,8 @@ static int linear_call(const rabit_layer* layer, const void* x, void* y, int bat
 
     const int variant = choose_variant(*layer, batch);
     if (int rc = check_variant(*layer, variant, batch)) return rc;
+    // The GEMM's CTAs let the next kernel start behind their dependency wait; beside the plain kernel nothing starts; the GEMVs let it start when they do.
+    *ends_late = variant == 1 || variant == 3 || variant == 4 || (variant == 6 && batch > kF16Rows);
     cudaError_t e = cudaSuccess;
     switch (variant) {
         case 2:
@@ -278,18 +281,12 @@ static int linear_call(const rabit_layer* layer, const void* x, void* y, int bat
     return RABIT_OK;
 }
 
-// Whether the kernel that a call on this layer ends with, alone or in a group, lets the next one of the stream start only when all work before it is
-// complete: the GEMM, whose CTAs say so behind their dependency wait, and the plain kernel, beside which nothing starts.  The GEMVs say so when they start.
-bool rabit_ends_late(const rabit_layer& L, int batch) {
-    if (L.variant == 0) return batch > RABIT_MAX_GEMV_BATCH || (batch > kF16Rows && rabit_gemv_f16_supports(L, kF16Rows));
-    return L.variant == 1 || L.variant == 3 || L.variant == 4 || (L.variant == 6 && batch > kF16Rows);
-}
-
 extern "C" int rabit_linear(const rabit_layer* layer, const void* x, void* y, int batch, void* stream) {
-    return rabit_guarded("rabit_linear", [&] { return linear_call(layer, x, y, batch, stream); });
+    bool late;
+    return rabit_guarded("rabit_linear", [&] { return linear_call(layer, x, y, batch, stream, &late); });
 }
 
-static int group_call(const rabit_layer* const* layers, const void* const* xs, void* const* ys, int n_layers, int batch, void* stream) {
+static int group_call(const rabit_layer* const* layers, const void* const* xs, void* const* ys, int n_layers, int batch, void* stream, bool* ends_late) {
     rabit_clear_error();
     if (!layers || !xs || !ys) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear_group: null array");
     if (n_layers < 1) return rabit_fail(RABIT_INVALID_ARG, "rabit_linear_group: n_layers must be >= 1 (got %d)", n_layers);
@@ -311,6 +308,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
         }
     }
     cudaStream_t st = (cudaStream_t)stream;
+    *ends_late = false;                                          // (as linear_call: of the fused launches only the GEMM's)
     {
         int dev = -1;
         RABIT_CUDA_TRY(cudaGetDevice(&dev));
@@ -338,6 +336,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
             gemm = rabit_gemm_tc_group_supports(layers + l, std::min(rabit_gemm_tc_max_group(), n_layers - l), batch);
         if (gemm) {
             cudaError_t e = cudaSuccess;
+            *ends_late = true;
             for (int l = 0; l < n_layers && e == cudaSuccess; l += rabit_gemm_tc_max_group())
                 e = rabit_launch_gemm_tc_group(layers + l, std::min(rabit_gemm_tc_max_group(), n_layers - l), xs + l, ys + l, batch, st);
             if (e != cudaSuccess) return rabit_fail(RABIT_CUDA_ERROR, "rabit_linear_group: launch failed: %s", cudaGetErrorString(e));
@@ -350,7 +349,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
         }
         if (f16) {                                               // unlike path counts, or one layer twice: launch by launch
             for (int l = 0; l < n_layers; ++l) {
-                int rc = linear_call(layers[l], xs[l], ys[l], batch, stream);
+                int rc = linear_call(layers[l], xs[l], ys[l], batch, stream, ends_late);
                 if (rc != RABIT_OK) return rc;
             }
             return RABIT_OK;
@@ -360,7 +359,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
         for (int b = a + 1; b < n_layers; ++b)
             if (layers[a] == layers[b]) {                        // the same layer twice would share one reduction scratch: no fused launch
                 for (int l = 0; l < n_layers; ++l) {
-                    int rc = linear_call(layers[l], xs[l], ys[l], batch, stream);
+                    int rc = linear_call(layers[l], xs[l], ys[l], batch, stream, ends_late);
                     if (rc != RABIT_OK) return rc;
                 }
                 return RABIT_OK;
@@ -369,7 +368,7 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
     for (int l = 0; l < n_layers && fused; ++l) fused = layers[l]->variant == 0 || layers[l]->variant == 2;
     if (!fused) {
         for (int l = 0; l < n_layers; ++l) {
-            int rc = linear_call(layers[l], xs[l], ys[l], batch, stream);
+            int rc = linear_call(layers[l], xs[l], ys[l], batch, stream, ends_late);
             if (rc != RABIT_OK) return rc;
         }
         return RABIT_OK;
@@ -391,7 +390,14 @@ static int group_call(const rabit_layer* const* layers, const void* const* xs, v
 
 extern "C" int rabit_linear_group(const rabit_layer* const* layers, const void* const* xs, void* const* ys,
                                   int n_layers, int batch, void* stream) {
-    return rabit_guarded("rabit_linear_group", [&] { return group_call(layers, xs, ys, n_layers, batch, stream); });
+    bool late;
+    return rabit_guarded("rabit_linear_group", [&] { return group_call(layers, xs, ys, n_layers, batch, stream, &late); });
+}
+
+int rabit_run_layers(const rabit_layer* const* layers, const void* const* xs, void* const* ys, int n_layers, int batch, void* stream, bool* ends_late) {
+    return rabit_guarded("rabit_linear", [&] {
+        return n_layers == 1 ? linear_call(layers[0], xs[0], ys[0], batch, stream, ends_late) : group_call(layers, xs, ys, n_layers, batch, stream, ends_late);
+    });
 }
 
 extern "C" size_t rabit_stage_bytes(const rabit_layer* layer, int batch) {

@@ -74,7 +74,9 @@ cudaError_t rabit_launch_transpose(const RabitGeom& G, const RabitHeader& hdr, c
 // up to 8 copies from device-visible host memory to the device by a kernel (rabit_fetch.cu); sizes are multiples of 16 bytes
 cudaError_t rabit_launch_fetch(const void* const* src, void* const* dst, const size_t* bytes, int n, cudaStream_t stream);
 
-bool rabit_ends_late(const rabit_layer& L, int batch);
+// rabit_linear of one layer, rabit_linear_group of several.  ends_late: whether the last kernel lets the next one of the stream start only when all work
+// before the call is complete (not the call's own).
+int rabit_run_layers(const rabit_layer* const* layers, const void* const* xs, void* const* ys, int n_layers, int batch, void* stream, bool* ends_late);
 int rabit_check_call(const rabit_layer& L, int batch);      // what rabit_linear refuses because of a kernel family that was set (the automatic choice runs)
 inline bool rabit_ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
     const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;

@@ -4,7 +4,7 @@ import pytest
 
 from oracle import adapters_oracle as ao
 from synth import make_layer, make_x
-from tests.test_gpu_adapters import _adapters, _cuda, _pool, _within
+from tests.test_gpu_adapters import _adapters, _cuda, _ids, _pool, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -174,3 +174,44 @@ def test_what_the_layer_refuses_leaves_y_and_u_as_they_were(variant, batch, M):
         assert not any(bool((t == 7.0).all()) for t in ys + us)
     for layer in layers:
         layer.free()
+
+
+@pytest.mark.parametrize("variant,batch,M,N,r,kind", [
+    (0, 2, 509, 512, 5, "one"), (0, 6, 509, 512, 33, "mixed"), (0, 12, 509, 512, 5, "mixed"), (0, 16, 509, 512, 33, "prompts"), (0, 48, 509, 512, 33, "mixed"), (0, 200, 509, 512, 5, "prompts"),
+    (0, 200, 4099, 4128, 5, "mixed"), (0, 200, 4099, 4128, 33, "prompts"), (0, 300, 4099, 4128, 21, "mixed"), (0, 1100, 509, 512, 5, "mixed"), (0, 1100, 509, 512, 33, "prompts"),
+    (0, 1100, 509, 512, 3, "none"), (1, 1100, 509, 512, 5, "mixed"), (5, 1100, 512, 512, 16, "prompts"), (5, 1100, 509, 512, 33, "mixed"), (4, 1100, 509, 512, 100, "mixed")])
+def test_a_chain_of_calls_with_odd_outputs_and_ranks(variant, batch, M, N, r, kind):
+    """As the chains of square layers, in both forms, behind every kind of layer kernel: y of one call lies in the memory that the next one reads as x, u is shared, ids and
+    factors change by copies on the stream.  Rows of y lie on no 16-byte boundary, u is read by single values."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    n, steps = 3, 6
+    L = make_layer(M, N, 2, key=(113, M))
+    layer = rabit.rabit_pack(L.planes, (L.g.astype(np.float32) / (16 * np.sqrt(N / 512))).astype(np.float16), L.h)
+    if variant:
+        layer.set_variant(variant)
+    (x0,) = _cuda(make_x(batch, N, key=(113, batch)))
+    pools = [_cuda(*_pool(M, N, n, r, 70 + k)) for k in range(2)]
+    ids = [_cuda(_ids(batch, n, kind, k))[0] for k in range(2)]
+    s, outs = torch.cuda.Stream(), {}
+    torch.cuda.synchronize()
+    for stop in (True, False):
+        A, at = rabit.RabitAdapters(*[t.clone() for t in pools[0]]), ids[0].clone()
+        bufs = [x0.clone()] + [torch.zeros((batch, N), dtype=torch.float16, device="cuda") for _ in range(steps)]
+        u, us = torch.zeros((batch, r), device="cuda"), [torch.zeros((batch, r), device="cuda") for _ in range(steps)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for k in range(steps):
+                if k == 3:                                                              # calls 0-2 and 3-5 follow one another without anything between but the calls
+                    at.copy_(ids[1])
+                    for t, v in zip((A.a, A.b, A.scale), pools[1]):
+                        t.copy_(v)
+                rabit.rabit_linear_adapted(layer, A, bufs[k], at, bufs[k + 1].view(-1)[:batch * M].view(batch, M), u if k % 3 != 2 else us[k])
+                if stop:
+                    s.synchronize()
+        torch.cuda.synchronize()
+        outs[stop] = [t.cpu().numpy() for t in bufs + us + [u]]
+    assert all(np.isfinite(v).all() for v in outs[True][:steps + 1]) and (outs[True][1] != 0).any()
+    for k, (v, w) in enumerate(zip(outs[True], outs[False])):
+        assert np.array_equal(v, w), k
+    layer.free()
