@@ -172,7 +172,7 @@ typedef struct rabit_adapters {
  *             caller that does not gives a scratch buffer).  y and u may not overlap one another nor any input.
  * Rows may name adapters in any order; rows of one adapter that follow one another (a prompt) share its reads.
  * The layer's sum is rounded to fp16 in y and the adapter's part, kept in fp32, is added to that and rounded again: an error of at most
- * half a step of the layer's sum and half a step of y.  u enters the second product to 22 bits, or to 2^-40 of the row's largest entry.
+ * half a step of the layer's sum and half a step of y.  u enters the second product to 22 bits, or to 2^-39 of the row's largest entry.
  * An infinite or NaN value in a row of x or in an adapter reaches the rows that it belongs to and no others; the outputs that it takes part
  * in are infinite or NaN, which of the two is open.  At most 2^31 - 256 rows.
  * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.
@@ -196,7 +196,7 @@ RABIT_API int rabit_linear_group_adapted(const rabit_layer* const* layers, const
  *   da  DEVICE fp32 [count][rank][n_in], db DEVICE fp32 [count][rank][n_out], 16-byte aligned, not overlapping each other nor any input.
  *       accumulate = 0: overwritten (zero for an adapter that no row names, whatever its scale is); otherwise the gradients are added to what is there.
  * Only the sizes, scale and nothing else of `adapters` is read.  Sums are fp32 in an order that the sizes and ids fix: the same call
- * gives the same bits.  u and p enter the products to 22 bits, or to 2^-40 of the largest entry of their rank in 64 rows.
+ * gives the same bits.  u and p enter the products to 22 bits, or to 2^-39 of the largest entry of their rank in up to 64 of the adapter's rows.
  * What a row of another adapter, or of none, holds does not matter, be it infinite or NaN; of a row of the adapter's it makes the gradients that it
  * takes part in infinite or NaN, which of the two is open.
  * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.  The buffers' device must be the current device.

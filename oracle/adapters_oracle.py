@@ -36,7 +36,7 @@ def adapted(planes, g, h, a, b, scale, x, ids):
         u[t] = a[i] @ x[t]
         err_u[t] = _sum_steps(N) * STEP32 * (np.abs(a[i]) @ np.abs(x[t])) + 1e-37
         y[t] += scale[i] * (u[t] @ b[i])
-        # u enters as two fp16 parts of a power of two of its row: with 22 bits, or to 2^-40 of its largest finite entry (the parts' smallest step is
+        # u enters as two fp16 parts of a power of two of its row: with 22 bits, or to 2^-39 of its largest finite entry (the parts' smallest step is
         # 2^-24 where the largest entry is at least 2^14: rounding is off by half of it, 2^-39 of that entry at most); the sum over the rank and the scaling are fp32
         size = np.abs(u[t][np.isfinite(u[t])]).max(initial=0.0)
         err[t] += abs(scale[i]) * ((err_u[t] + 2.0 ** -39 * size + np.abs(u[t]) * (2.0 ** -21 + (2 * r + 4) * STEP32)) @ np.abs(b[i]))

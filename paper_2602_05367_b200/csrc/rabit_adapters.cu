@@ -33,7 +33,7 @@ __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // fp32 operands of MMAs with fp16 ones.  Values that share a power of two are scaled so that the largest lies in [2^14, 2^15), then each is the sum of two fp16
-// values: 22 bits of it, or all bits down to 2^-40 of the largest where that is less.  (tf32 MMAs, two per operand part, have twice the number for the
+// values: 22 bits of it, or all bits down to 2^-39 of the largest where that is less.  (tf32 MMAs, two per operand part, have twice the number for the
 // same products, and their fp16 operand has to be converted: 4096 x 11008, rank 64, 4096 tokens took 150 us for the gradients and 118 for widen_kernel.)
 __device__ __forceinline__ void range_of(float largest, float& to, float& back) {   // to * largest in [2^14, 2^15); back = 1 / to
     const uint32_t e = max(__float_as_uint(largest) >> 23, 15u);

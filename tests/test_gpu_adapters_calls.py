@@ -215,3 +215,22 @@ def test_a_chain_of_calls_with_odd_outputs_and_ranks(variant, batch, M, N, r, ki
     for k, (v, w) in enumerate(zip(outs[True], outs[False])):
         assert np.array_equal(v, w), k
     layer.free()
+
+
+@pytest.mark.parametrize("r", [1, 17, 40, 128])
+def test_small_low_rank_products_beside_large_ones(r):
+    """The second fp16 part has steps of 2^-24 where the largest entry of the rank is scaled to 2^14: an entry is off by at most 2^-39 of the largest, and by that
+    much at a tie, which goes to the even neighbour 0."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    M, N, batch = 32, 64, 5
+    a, b, _ = _pool(M, N, 1, r, 80)
+    x, p = np.zeros((batch, N), np.float16), np.zeros((batch, r), np.float32)
+    p[0] = 1.0                                                                          # the largest, where x is zero
+    entries = np.array([2.0 ** -39, 1.5 * 2.0 ** -39, 2.0 ** -38, 2.0 ** -20 + 2.0 ** -39], np.float32)
+    p[1:] = entries[:, None]
+    x[np.arange(1, 5), np.arange(4)] = 1.0
+    da, _ = rabit.rabit_adapter_gradients(_adapters(a, b, np.ones(1, np.float32)), *_cuda(x, p, np.zeros((batch, M), np.float16), p, np.zeros(batch, np.int32)))
+    got = da[0, :, :4].cpu().numpy().astype(np.float64)
+    assert (np.abs(got - entries) <= 2.0 ** -39).all()
+    assert (got[:, 0] == 0).all() and (got[:, 1] == 2.0 ** -38).all() and (got[:, 2] == 2.0 ** -38).all() and not da[0, :, 4:].any()
