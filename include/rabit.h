@@ -171,8 +171,9 @@ typedef struct rabit_adapters {
  *   u         DEVICE fp32 [batch][rank], 16-byte aligned: receives the rows' low-rank products (the backward pass needs them; a
  *             caller that does not gives a scratch buffer).  y and u may not overlap one another nor any input.
  * Rows may name adapters in any order; rows of one adapter that follow one another (a prompt) share its reads.
- * The layer's sum is rounded to fp16 in y and the adapter's part, kept in fp32, is added to that and rounded again: an error of at most
- * half a step of the layer's sum and half a step of y.  u enters the second product to 22 bits, or to 2^-39 of the row's largest entry.
+ * The layer's sum is rounded to fp16 in y, as rabit_linear does it, and the adapter's part, kept in fp32, is added to that and rounded again: an error of at
+ * most half a step of the layer's sum and half a step of y.  Where the layer's sum alone is beyond fp16 (65504 and half a step), it is infinite in y and stays so,
+ * though the whole may not be.  u enters the second product to 22 bits, or to 2^-39 of the row's largest entry.
  * An infinite or NaN value in a row of x or in an adapter reaches the rows that it belongs to and no others; the outputs that it takes part
  * in are infinite or NaN, which of the two is open.  At most 2^31 - 256 rows.
  * Asynchronous on `stream`, allocates nothing, may be captured in a CUDA graph.

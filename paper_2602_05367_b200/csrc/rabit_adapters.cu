@@ -435,7 +435,9 @@ struct Widen {
     static constexpr int kBytes = kRingBytes + kUBytes + Operand<R16>::pieces(kWidenRows) * 16 + kWidenRows * 4;
     static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs per SM");
 };
-// Row gq (h = 0) or gq + 8 (h = 1) of those products on top of the 8 columns of y that were read as `old`
+// Row gq (h = 0) or gq + 8 (h = 1) of those products on top of the 8 columns of y that were read as `old`.  The layer's sum is there in fp16, rounded by the layer's own kernel:
+// every GEMV and GEMM writes its y so, and the call has no other memory for it (fp32 would be twice the bytes of y, out and in again).  Against one rounding of the whole that costs 0.00029 of the
+// largest output for 0.00021, and what is infinite there stays so.
 template <bool VEC>
 __device__ __forceinline__ void widen_store(__half* y, int n, const uint4& old, const float (&acc)[4][4], int h, float scale) {
     uint32_t v[4] = {old.x, old.y, old.z, old.w};

@@ -234,3 +234,24 @@ def test_small_low_rank_products_beside_large_ones(r):
     got = da[0, :, :4].cpu().numpy().astype(np.float64)
     assert (np.abs(got - entries) <= 2.0 ** -39).all()
     assert (got[:, 0] == 0).all() and (got[:, 1] == 2.0 ** -38).all() and (got[:, 2] == 2.0 ** -38).all() and not da[0, :, 4:].any()
+
+
+@pytest.mark.parametrize("batch,M,r", [(1, 64, 3), (5, 64, 16), (12, 67, 4), (100, 64, 40), (1100, 1024, 16)])
+def test_a_layer_sum_beyond_fp16_is_infinite_whatever_the_adapter_adds(batch, M, r):
+    """y is the layer's fp16 output plus the adapter's part: rows whose layer sum is 80000 stay infinite although 40000 are taken away.  781.25 is 781 in fp16 (a tie between
+    steps of 0.5), 64 of them 49984, exact: plus 12.8 * 781 that is 59980.8, in steps of 32 59968; plus 25.6 * 781 it is infinite."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    N = 64
+    L = make_layer(M, N, 1, key=(114, M))
+    L.planes[:], L.g[:], L.h[:] = 0, 1, 1
+    a, b = np.zeros((3, r, N), np.float16), np.zeros((3, r, M), np.float16)
+    a[:, r - 1, 0], b[:, r - 1] = 1, 1                                                  # u = x[0]
+    which = np.arange(batch) % 3
+    x = np.full((batch, N), 50000 / 64, np.float16)       
+    x[which == 0] = 80000 / 64
+    scale = np.array([-40000 / 1250, 10000 / 781.25, 20000 / 781.25], np.float32)
+    layer = rabit.rabit_pack(L.planes, L.g, L.h)
+    y = rabit.rabit_linear_adapted(layer, _adapters(a, b, scale), *_cuda(x, which.astype(np.int32))).cpu().numpy()
+    assert (y[which == 0] == np.inf).all() and (y[which == 1] == 59968).all() and (y[which == 2] == np.inf).all()
+    layer.free()
