@@ -222,7 +222,8 @@ RABIT_API int rabit_transpose(const rabit_layer* layer, void* dev_buf, size_t de
  *   outs      HOST array of n DEVICE fp32 pointers that receive the clipped values, or NULL to clip in place; an output is its own
  *             tensor or overlaps none, nor another output
  *   dev_buf   DEVICE, 256-byte aligned, at least rabit_gradients_bytes(counts, n): table and partial sums, owned by the caller
- * rabit_gradients_bind copies the table on `stream` and returns when it has been staged; not while `stream` is being captured.
+ * rabit_gradients_bind copies the table on `stream` and returns when it is in place (it synchronises the stream), so calls may come on any stream; not
+ * while `stream` is being captured.
  */
 typedef struct rabit_gradients rabit_gradients;
 RABIT_API size_t rabit_gradients_bytes(const size_t* counts, int n);

@@ -184,7 +184,9 @@ static int bind_call(const float* const* tensors, float* const* outs, const size
             float* dst = outs ? outs[i] + at : const_cast<float*>(src);
             table.push_back(Chunk{src, dst, (uint32_t)std::min(kChunk, counts[i] - at), (uint32_t)(((uintptr_t)src | (uintptr_t)dst) % 16 == 0)});
         }
+    // The table is in place when this returns, so a call may come on any stream: one that read it too early would take whatever is there for addresses.
     if (!table.empty()) RABIT_CUDA_TRY(cudaMemcpyAsync(dev_buf, table.data(), table.size() * sizeof(Chunk), cudaMemcpyHostToDevice, (cudaStream_t)stream));
+    RABIT_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     int sms = 0;
     RABIT_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, attr.device));
     std::unique_ptr<rabit_gradients> R(new rabit_gradients);

@@ -255,3 +255,19 @@ def test_a_layer_sum_beyond_fp16_is_infinite_whatever_the_adapter_adds(batch, M,
     y = rabit.rabit_linear_adapted(layer, _adapters(a, b, scale), *_cuda(x, which.astype(np.int32))).cpu().numpy()
     assert (y[which == 0] == np.inf).all() and (y[which == 1] == 59968).all() and (y[which == 2] == np.inf).all()
     layer.free()
+
+
+def test_bound_gradients_may_be_clipped_on_any_stream():
+    """Binding returns when its table is in place, however long the stream's earlier work takes."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    s = torch.cuda.Stream()
+    t = torch.full((5000,), 2.0, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(100_000_000)                                                  # some 50 ms
+    G = rabit.RabitGradients([t], stream=s.cuda_stream)
+    assert s.query()
+    norm = rabit.rabit_clip_gradients(G, 1.0)
+    torch.cuda.synchronize()
+    assert abs(float(norm) - 2 * np.sqrt(5000)) < 1e-3 and abs(float(t[0]) - 1 / np.sqrt(5000)) < 1e-6
