@@ -86,11 +86,12 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Chunk* __restri
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-__global__ void __launch_bounds__(kThreads) scale_kernel(const Chunk* __restrict__ chunks, int n_chunks, const double* __restrict__ partial, double max_norm, float* __restrict__ norm_out) {
+__global__ void __launch_bounds__(kThreads) scale_kernel(const Chunk* __restrict__ chunks, int n_chunks, const double* partial, double max_norm, float* norm_out) {
     __shared__ double warps[kThreads / 32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     double sum = 0.0;
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) sum += partial[i];
+    // (from L2, and not as data that stays the same while this kernel runs: it starts while the sums are being written)
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) sum += __ldcg(partial + i);
     const double norm = sqrt(block_sum(sum, warps));
     double f = max_norm / (norm + 1e-6);
     if (f > 1.0) f = 1.0;                             // (a NaN stays)
