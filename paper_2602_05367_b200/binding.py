@@ -194,7 +194,7 @@ class RabitLayer:
 
     def __init__(self, handle: int, dev_buf, K: int, M: int, N: int):
         self._handle = _c_void_p(handle)
-        self._addr = handle             # the same as an integer, for the native module; None once freed
+        self._layer_addr = handle       # the same as an integer, for the native module; None once freed
         self.dev_buf = dev_buf          # keeps the device memory alive
         self.K, self.M, self.N = K, M, N
         self._stage = None              # device staging buffer of rabit_linear_host
@@ -225,7 +225,7 @@ class RabitLayer:
     def free(self) -> None:
         if self._handle is not None:
             _lib.rabit_free(self._handle)
-            self._handle = self._addr = None
+            self._handle = self._layer_addr = None
             self.dev_buf = None
             self._stage = None
 
@@ -460,19 +460,19 @@ class RabitGradients:
         dst = None if outs is None else (_c_void_p * n)(*[t.data_ptr() for t in outs])
         self._keep = (tensors, outs)
         nbytes = int(_lib.rabit_gradients_bytes(counts, n))
-        self._addr = None                               # the descriptor, for the native module; None once freed
+        self._gradients_addr = None                               # the descriptor, for the native module; None once freed
         self._device = dev.index
         st = _stream_of(dev, stream)
         self.dev_buf = _empty(nbytes, dev, st)
         out = _c_void_p()
         with torch.cuda.device(dev):
             _check(_lib.rabit_gradients_bind(src, dst, counts, n, _c_void_p(self.dev_buf.data_ptr()), nbytes, _c_void_p(st), ctypes.byref(out)))
-        self._addr = out.value
+        self._gradients_addr = out.value
 
     def free(self) -> None:
-        if self._addr is not None:
-            _lib.rabit_gradients_free(_c_void_p(self._addr))
-            self._addr = self._keep = self.dev_buf = None
+        if self._gradients_addr is not None:
+            _lib.rabit_gradients_free(_c_void_p(self._gradients_addr))
+            self._gradients_addr = self._keep = self.dev_buf = None
 
     def __del__(self):  # pragma: no cover
         try:

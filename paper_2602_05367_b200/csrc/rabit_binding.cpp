@@ -44,7 +44,10 @@ ClipFn p_clip = nullptr;
 DimFn p_M = nullptr, p_N = nullptr;
 ErrorFn p_error = nullptr;
 PyObject* g_error_type = nullptr;      // RabitError
-PyObject* g_addr_name = nullptr;       // "_addr": the descriptor's address on a RabitLayer, None once freed; on a RabitAdapters that of its rabit_adapters
+// Names of the attributes that hold addresses for this module, one for each class, so that no object is taken for one of another class:
+PyObject* g_layer_name = nullptr;      // "_layer_addr": the descriptor's address on a RabitLayer, None once freed
+PyObject* g_addr_name = nullptr;       // "_addr": that of its rabit_adapters on a RabitAdapters
+PyObject* g_gradients_name = nullptr;  // "_gradients_addr": the descriptor's on a RabitGradients, None once freed
 
 PyObject* g_buf_name = nullptr;        // "dev_buf": the device memory of a RabitGradients
 PyObject* g_device_name = nullptr;     // "_device": the index of the device that a RabitAdapters or RabitGradients lives on
@@ -60,15 +63,21 @@ PyObject* raise_code(int code, const char* msg) {
     return nullptr;
 }
 
-void* layer_handle(PyObject* layer) {
-    PyObject* a = PyObject_GetAttr(layer, g_addr_name);
-    if (!a) return nullptr;
+// the address under `name`, which objects of the class `what` have; nullptr with an exception set if it has none
+void* address_of(PyObject* o, PyObject* name, const char* what) {
+    PyObject* a = PyObject_GetAttr(o, name);
+    if (!a) {
+        if (PyErr_ExceptionMatches(PyExc_AttributeError)) PyErr_Format(PyExc_TypeError, "a %s is needed, not a %s", what, Py_TYPE(o)->tp_name);
+        return nullptr;
+    }
     void* p = nullptr;
-    if (a == Py_None) raise_code(-1, "layer already freed");
+    if (a == Py_None) raise_code(RABIT_INVALID_ARG, "already freed");
     else p = PyLong_AsVoidPtr(a);
     Py_DECREF(a);
     return p;
 }
+void* layer_handle(PyObject* o) { return address_of(o, g_layer_name, "RabitLayer"); }
+const rabit_adapters* adapters_of(PyObject* o) { return (const rabit_adapters*)address_of(o, g_addr_name, "RabitAdapters"); }
 
 // stream argument: an integer, or None for torch's current stream on that device
 bool stream_of(PyObject* arg, c10::DeviceIndex device, void** out) {
@@ -193,7 +202,7 @@ long device_of(PyObject* o) {
     return d ? PyLong_AsLong(d.get()) : -1;
 }
 const rabit_adapters* adapters_on(PyObject* o, c10::DeviceIndex device) {
-    const rabit_adapters* A = (const rabit_adapters*)layer_handle(o);
+    const rabit_adapters* A = adapters_of(o);
     if (!A) return nullptr;
     const long d = device_of(o);
     if (d == -1 && PyErr_Occurred()) return nullptr;
@@ -325,7 +334,7 @@ PyObject* linear_group_adapted(PyObject*, PyObject* const* args, Py_ssize_t narg
 PyObject* adapter_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 10) return PyErr_Format(PyExc_TypeError, "adapter_gradients takes 10 arguments");
     HANDLE_TH_ERRORS
-    const rabit_adapters* A = (const rabit_adapters*)layer_handle(args[0]);
+    const rabit_adapters* A = adapters_of(args[0]);
     if (!A) return nullptr;
     const long d = device_of(args[0]);
     if (d == -1 && PyErr_Occurred()) return nullptr;
@@ -368,7 +377,7 @@ PyObject* adapter_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
 PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 4) return PyErr_Format(PyExc_TypeError, "clip takes 4 arguments");
     HANDLE_TH_ERRORS
-    const void* h = layer_handle(args[0]);
+    const void* h = address_of(args[0], g_gradients_name, "RabitGradients");
     if (!h) return nullptr;
     const long d = device_of(args[0]);
     if (d == -1 && PyErr_Occurred()) return nullptr;
@@ -474,8 +483,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rabit_binding", nullptr, -1, meth
 }  // namespace
 
 PyMODINIT_FUNC PyInit__rabit_binding(void) {
+    g_layer_name = PyUnicode_InternFromString("_layer_addr");
     g_addr_name = PyUnicode_InternFromString("_addr");
+    g_gradients_name = PyUnicode_InternFromString("_gradients_addr");
     g_device_name = PyUnicode_InternFromString("_device");
     g_buf_name = PyUnicode_InternFromString("dev_buf");
-    return g_addr_name && g_device_name && g_buf_name ? PyModule_Create(&module) : nullptr;
+    return g_layer_name && g_addr_name && g_gradients_name && g_device_name && g_buf_name ? PyModule_Create(&module) : nullptr;
 }
