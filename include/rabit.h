@@ -357,6 +357,13 @@ RABIT_API int rabit_selftest_gemm_plan(int n_layers, const int* M, const int* N,
 RABIT_API int rabit_selftest_gemm_ready(int stream, int pass, int passes, int* parity_out);
 
 /*
+ * Test aid (no counterpart in the paper).  In a library built with -DRABIT_CHECKED every address that the adapters' kernels make from ids, lists
+ * of rows and sizes is compared with its buffer, and an access outside is skipped and recorded.  Synchronises the current device; returns RABIT_OK, or
+ * RABIT_DEVICE_FAULT if there was one since the last call.  RABIT_UNSUPPORTED_SHAPE in the ordinary build.
+ */
+RABIT_API int rabit_selftest_index_faults(void);
+
+/*
  * Measurement aid (no counterpart in the paper): one kernel that reads `bytes` bytes of device memory once with
  * 128-bit streaming loads and keeps nothing.  Timed by the caller with CUDA events over a buffer much larger than L2
  * it gives the read-only HBM bandwidth this GPU delivers to plain loads, the natural ceiling of the decode GEMV.

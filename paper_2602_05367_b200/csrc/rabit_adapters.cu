@@ -21,6 +21,20 @@ namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxGroup = 8;                           // layers in one launch
+// Checked build (-DRABIT_CHECKED, python paper_2602_05367_b200/build.py --checked): every address that is made from ids, lists of rows or sizes is compared with
+// its buffer first; a violation sets the word that rabit_selftest_index_faults reads, and the access is skipped.  In the ordinary build the checks compile to nothing.
+#ifdef RABIT_CHECKED
+__device__ unsigned int g_index_fault;
+#define RABIT_IN_RANGE(cond) ((cond) ? true : (atomicExch(&g_index_fault, 1u), false))
+// whether `bytes` bytes at p lie in the `size` bytes at base
+__device__ __forceinline__ bool inside(const void* p, size_t bytes, const void* base, size_t size) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), from = reinterpret_cast<uintptr_t>(base);
+    return at >= from && at + bytes <= from + size;
+}
+#else
+#define RABIT_IN_RANGE(cond) true
+#endif
+
 constexpr int kMostRows = 0x7FFFFF00;                  // rows of a call: a tile's places behind the last one are 32-bit numbers too
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -127,19 +141,21 @@ __device__ __forceinline__ uint4 extract_8(const uint4& lo, const uint4& hi, con
 }
 // Both pieces to shared memory (`second` 16-byte units apart), asynchronously: what lies beyond `end`, the end of the buffer, or is not needed arrives as zeros and is
 // not read.
-__device__ __forceinline__ void copy_async_pieces(uint4* dst, int second, const __half* src, int n, const __half* end) {
+__device__ __forceinline__ void copy_async_pieces(uint4* dst, int second, const __half* src, int n, const __half* begin, const __half* end) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(src), piece = at & ~(uintptr_t)15, last = reinterpret_cast<uintptr_t>(end);
     const bool two = n > 0 && (int)((at >> 1) & 7u) + min(n, 8) > 8;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const uintptr_t from = piece + 16 * h;
-        const uint32_t size = (h == 0 ? n > 0 : two) ? (uint32_t)min((long long)16, (long long)(last - from)) : 0u;
+        uint32_t size = (h == 0 ? n > 0 : two) ? (uint32_t)min((long long)16, (long long)(last - from)) : 0u;
+        if (size != 0u && !RABIT_IN_RANGE(size <= 16u && inside(reinterpret_cast<const void*>(from), size, begin, last - reinterpret_cast<uintptr_t>(begin)))) size = 0u;
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + h * second)), "l"(size ? from : piece), "r"(size) : "memory");
     }
 }
 // The same straight from memory, for rows of any length; `end` is the end of the buffer, which starts on 16 bytes: halves one by one where a piece would reach beyond it.
-__device__ __forceinline__ uint4 load_8(const __half* src, int n, const __half* end) {
+__device__ __forceinline__ uint4 load_8(const __half* src, int n, const __half* begin, const __half* end) {
     if (n <= 0) return make_uint4(0u, 0u, 0u, 0u);
+    if (!RABIT_IN_RANGE(inside(src, 2 * min(n, 8), begin, reinterpret_cast<const char*>(end) - reinterpret_cast<const char*>(begin)) && (reinterpret_cast<uintptr_t>(begin) & 15u) == 0u)) return make_uint4(0u, 0u, 0u, 0u);
     const uintptr_t at = reinterpret_cast<uintptr_t>(src);
     const uint4* piece = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
     const bool two = (int)((at >> 1) & 7u) + min(n, 8) > 8;
@@ -265,7 +281,8 @@ __global__ void __launch_bounds__(kThreads, (Narrow<NR, WM>::kPerSm)) narrow_ker
                         const int k = T::kRanks >= 32 ? i / kPer : i * (32 / T::kRanks) + j0 / T::kRanks, j = (T::kRanks >= 32 ? i % kPer * 32 : 0) + j0 % T::kRanks;
                         const bool in = j < rank && (whole || (chunk0 + k < c1 && (chunk0 + k) * 64 + piece * 8 < n));
                         const __half* src = a0 + (size_t)it * (T::WK * 64) + (T::kRanks >= 32 ? (size_t)(i % kPer) * rows32 + i / kPer * 64 : (size_t)(i * (32 / T::kRanks) * 64));
-                        copy_async_16(stage + (k * T::kRanks + j) * 128 + ((piece ^ ((j & 1) << 2)) << 4), in ? src : L.a, in);
+                        unsigned char* dst = stage + (k * T::kRanks + j) * 128 + ((piece ^ ((j & 1) << 2)) << 4);
+                        if (RABIT_IN_RANGE(inside(dst, 16, stage, T::kABytes) && (!in || inside(src, 16, L.a, (size_t)L.count * rank * n * 2)))) copy_async_16(dst, in ? src : L.a, in);
                     }
                 }
                 if (own != 0u) {
@@ -275,7 +292,8 @@ __global__ void __launch_bounds__(kThreads, (Narrow<NR, WM>::kPerSm)) narrow_ker
                     for (int m = 0; m < 4; ++m) {
                         const int r = 4 * m + x_row;
                         const bool in = col_in && (own >> r & 1u);
-                        copy_async_16(stage + T::kABytes + (warp * 16 + r) * 128 + (((lane & 7) ^ ((r & 1) << 2)) << 4), in ? src + m * rows4 : L.x, in);
+                        unsigned char* dst = stage + T::kABytes + (warp * 16 + r) * 128 + (((lane & 7) ^ ((r & 1) << 2)) << 4);
+                        if (RABIT_IN_RANGE(inside(dst, 16, stage, T::kStageBytes) && (!in || inside(src + m * rows4, 16, L.x, (size_t)P.batch * n * 2)))) copy_async_16(dst, in ? src + m * rows4 : L.x, in);
                     }
                 }
             }
@@ -350,7 +368,8 @@ __global__ void __launch_bounds__(kThreads, (Narrow<NR, WM>::kPerSm)) narrow_ker
         for (int w = 0; w < kWords; ++w)
             if (row / 32 == w) word = mine[w] | (share == 0 ? ~named[w] : 0u);
         if (j >= rank || tile0 + row >= P.batch || !((word >> (row & 31)) & 1u)) continue;
-        store_4(L.u + (size_t)(tile0 + row) * rank + j, cluster_sum(cluster, red, parts, e), rank - j, rank % 4 == 0);
+        float* to = L.u + (size_t)(tile0 + row) * rank + j;
+        if (RABIT_IN_RANGE(inside(to, 4 * min(rank - j, 4), L.u, (size_t)P.batch * rank * 4))) store_4(to, cluster_sum(cluster, red, parts, e), rank - j, rank % 4 == 0);
     }
     cluster.sync();
     // One CTA, whose share is always taken, waits for the layer: the grid ends behind the layer's, so what waits for this one has y.  The others make room.
@@ -510,14 +529,16 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
                 const int r = t + lane / W::kLanes, p = lane % W::kLanes, cols = m_all - col0 - 8 * p;
                 const bool in = row0 + r < batch && cols > 0;
                 const __half* src = in ? from + (size_t)t * m_all : L.y;
+                if (!RABIT_IN_RANGE(inside(dst + W::piece(r, p), 16, ring, W::kRingBytes - warp * W::kBlockPieces * 16) && (!in || inside(src, 2 * min(cols, 8), L.y, (size_t)batch * m_all * 2)))) continue;
                 if (VEC) copy_async_16(dst + W::piece(r, p), src, in);
-                else copy_async_pieces(dst + W::piece(r, p), kWarps * W::kBlockPieces, src, in ? cols : 0, y_end);
+                else copy_async_pieces(dst + W::piece(r, p), kWarps * W::kBlockPieces, src, in ? cols : 0, L.y, y_end);
             }
             for (int i = threadIdx.x; i < kWidenRows * W::kFours; i += kThreads) {
                 const int r = i / W::kFours, j = i % W::kFours * 4;
                 const float* src = L.u + (size_t)(row0 + r) * rank + j;
                 const bool in = row0 + r < batch;
                 float* to = u_block + 4 * i;
+                if (in && j < rank && !RABIT_IN_RANGE(inside(src, 4 * min(rank - j, 4), L.u, (size_t)batch * rank * 4))) continue;
                 if (fours) {
                     copy_async_16(to, in && j < rank ? src : L.u, in && j < rank);
                 } else {
@@ -544,7 +565,8 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
                 if constexpr (VEC) {
                     uint4 v[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = 16 * k + 4 * tq + i < rank && cf < m_all ? __ldcg(reinterpret_cast<const uint4*>(b + (size_t)(16 * k + i) * m_all)) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < 4; ++i)
+                        v[i] = 16 * k + 4 * tq + i < rank && cf < m_all && RABIT_IN_RANGE(inside(b + (size_t)(16 * k + i) * m_all, 16, L.b, (size_t)L.count * rank * m_all * 2)) ? __ldcg(reinterpret_cast<const uint4*>(b + (size_t)(16 * k + i) * m_all)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         f[k][g][0][p] = __byte_perm(v[2 * p].x, v[2 * p + 1].x, pick);
@@ -558,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
                     for (int i = 0; i < 4; ++i) {
                         const unsigned short* row = reinterpret_cast<const unsigned short*>(b + (size_t)(16 * k + i) * m_all) + (gq & 1);
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) v[i][q] = 16 * k + 4 * tq + i < rank && cf + 2 * q + (gq & 1) < m_all ? row[2 * q] : 0u;
+                        for (int q = 0; q < 4; ++q) v[i][q] = 16 * k + 4 * tq + i < rank && cf + 2 * q + (gq & 1) < m_all && RABIT_IN_RANGE(inside(row + 2 * q, 2, L.b, (size_t)L.count * rank * m_all * 2)) ? row[2 * q] : 0u;
                     }
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
@@ -597,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
             if (cur != held) load_factor(held = cur);
             const uint32_t match = __ballot_sync(0xFFFFFFFFu, id == cur);
             left &= ~match;
-            const float scale = __ldcg(L.scale + cur);
+            const float scale = RABIT_IN_RANGE(cur >= 0 && cur < L.count) ? __ldcg(L.scale + cur) : 0.f;
 #pragma unroll
             for (int mt = 0; mt < kTiles; ++mt) {
                 const uint32_t hits = (match >> (16 * mt)) & 0xFFFFu;
@@ -614,6 +636,7 @@ __global__ void __launch_bounds__(kThreads, 2) widen_kernel(const __grid_constan
                         if (c + 32 * g < m_all) {
                             __half* to = y + (2 * mt + h) * eight + 32 * g;
                             const uint4* was = old + W::piece(16 * mt + 8 * h + gq, 4 * g + tq);
+                            if (!RABIT_IN_RANGE(inside(to, 2 * min(m_all - c - 32 * g, 8), L.y, (size_t)batch * m_all * 2))) continue;
                             widen_store<VEC>(to, m_all - c - 32 * g, VEC ? *was : extract_8(was[0], was[(W::kPlanes - 1) * kWarps * W::kBlockPieces], to, m_all - c - 32 * g), acc[g], h, factor);
                         }
                 }
@@ -646,14 +669,14 @@ struct Decode {
 template <int R16, bool VEC>
 struct Columns {
     uint4 b[R16][4], y[2];
-    // src: the lane's 8 columns of its first row; n of them are inside; ranks: of its rows 16 k + i those below this exist
-    __device__ __forceinline__ void load(const __half* src, int m_all, int n, int ranks, const __half* const (&y_src)[2], const bool (&has)[2], int n_y) {
+    // L and batch only for the checks; src: the lane's 8 columns of its first row; n of them are inside; ranks: of its rows 16 k + i those below this exist
+    __device__ __forceinline__ void load(const DecodeLayer& L, int batch, const __half* src, int m_all, int n, int ranks, const __half* const (&y_src)[2], const bool (&has)[2], int n_y) {
 #pragma unroll
         for (int k = 0; k < R16; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) b[k][i] = 16 * k + i < ranks && n > 0 ? *reinterpret_cast<const uint4*>(src + (size_t)(16 * k + i) * m_all) : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < 4; ++i) b[k][i] = 16 * k + i < ranks && n > 0 && RABIT_IN_RANGE(inside(src + (size_t)(16 * k + i) * m_all, 16, L.b, (size_t)L.count * L.rank * m_all * 2)) ? *reinterpret_cast<const uint4*>(src + (size_t)(16 * k + i) * m_all) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) y[h] = has[h] && n_y > 0 ? *reinterpret_cast<const uint4*>(y_src[h]) : make_uint4(0u, 0u, 0u, 0u);
+        for (int h = 0; h < 2; ++h) y[h] = has[h] && n_y > 0 && RABIT_IN_RANGE(inside(y_src[h], 16, L.y, (size_t)batch * m_all * 2)) ? *reinterpret_cast<const uint4*>(y_src[h]) : make_uint4(0u, 0u, 0u, 0u);
     }
     __device__ __forceinline__ void factor(uint32_t (&f)[R16][1][4][2], int odd) const {
         const uint32_t pick = odd ? 0x7632u : 0x5410u;
@@ -672,7 +695,7 @@ struct Columns {
 template <int R16>
 struct Columns<R16, false> {
     unsigned short b[R16][4][4], y[2][8];
-    __device__ __forceinline__ void load(const __half* src, int m_all, int n, int ranks, const __half* const (&y_src)[2], const bool (&has)[2], int n_y) {
+    __device__ __forceinline__ void load(const DecodeLayer& L, int batch, const __half* src, int m_all, int n, int ranks, const __half* const (&y_src)[2], const bool (&has)[2], int n_y) {
         const int odd = (threadIdx.x >> 2) & 1;                                 // which column of a pair the lane's fragments hold
 #pragma unroll
         for (int k = 0; k < R16; ++k)
@@ -680,12 +703,12 @@ struct Columns<R16, false> {
             for (int i = 0; i < 4; ++i) {
                 const unsigned short* row = reinterpret_cast<const unsigned short*>(src + (size_t)(16 * k + i) * m_all) + odd;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) b[k][i][q] = 16 * k + i < ranks && 2 * q + odd < n ? row[2 * q] : (unsigned short)0;
+                for (int q = 0; q < 4; ++q) b[k][i][q] = 16 * k + i < ranks && 2 * q + odd < n && RABIT_IN_RANGE(inside(row + 2 * q, 2, L.b, (size_t)L.count * L.rank * m_all * 2)) ? row[2 * q] : (unsigned short)0;
             }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) y[h][q] = has[h] && q < n_y ? reinterpret_cast<const unsigned short*>(y_src[h])[q] : (unsigned short)0;
+            for (int q = 0; q < 8; ++q) y[h][q] = has[h] && q < n_y && RABIT_IN_RANGE(inside(y_src[h] + q, 2, L.y, (size_t)batch * m_all * 2)) ? reinterpret_cast<const unsigned short*>(y_src[h])[q] : (unsigned short)0;
     }
     __device__ __forceinline__ void factor(uint32_t (&f)[R16][1][4][2], int) const {
 #pragma unroll
@@ -764,7 +787,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
         __syncwarp();
         const bool has[2] = {rows[gq] >= 0, rows[8 + gq] >= 0};
         const size_t row[2] = {(size_t)max(rows[gq], 0), (size_t)max(rows[8 + gq], 0)};
-        const float scale = __ldcg(L.scale + cur);
+        const float scale = RABIT_IN_RANGE(who >= 0 && cur >= 0 && cur < L.count) ? __ldcg(L.scale + cur) : 0.f;
 
         float acc[NR][4] = {};
         {
@@ -779,9 +802,9 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
                 const bool in = u < u1;
                 const size_t col = (size_t)u * 32;
 #pragma unroll
-                for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] ? __ldcg(reinterpret_cast<const uint4*>(x[m] + col)) : make_uint4(0u, 0u, 0u, 0u);
+                for (int m = 0; m < 2; ++m) l.x[m] = in && has[m] && RABIT_IN_RANGE(inside(x[m] + col, 16, L.x, (size_t)P.batch * n * 2)) ? __ldcg(reinterpret_cast<const uint4*>(x[m] + col)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank ? __ldcg(reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col)) : make_uint4(0u, 0u, 0u, 0u);
+                for (int j = 0; j < NR; ++j) l.a[j] = in && 8 * j + gq < rank && RABIT_IN_RANGE(inside(a + (size_t)(8 * j) * n + col, 16, L.a, (size_t)L.count * rank * n * 2)) ? __ldcg(reinterpret_cast<const uint4*>(a + (size_t)(8 * j) * n + col)) : make_uint4(0u, 0u, 0u, 0u);
             };
             auto multiply = [&](const Loads& l) {
 #pragma unroll
@@ -831,7 +854,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
         Columns<R16, VEC> sets[kSets];
         auto load_columns = [&](Columns<R16, VEC>& l, int g) {
             const __half* const y_src[2] = {y[0] + 32 * g, y[1] + 32 * g};
-            l.load(b + 32 * g, m_all, g < groups ? m_all - 32 * g - 8 * (gq >> 1) : 0, rank - 4 * tq, y_src, has, g < groups ? m_all - 32 * g - 8 * tq : 0);
+            l.load(L, P.batch, b + 32 * g, m_all, g < groups ? m_all - 32 * g - 8 * (gq >> 1) : 0, rank - 4 * tq, y_src, has, g < groups ? m_all - 32 * g - 8 * tq : 0);
         };
 #pragma unroll
         for (int q = 0; q < kSets; ++q) load_columns(sets[q], g + q * step);
@@ -860,7 +883,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
             s = make_float4(j < rank ? s.x : 0.f, j + 1 < rank ? s.y : 0.f, j + 2 < rank ? s.z : 0.f, j + 3 < rank ? s.w : 0.f);
             const float back = split_row<R16>(us, r, j / 4, s);
             if (j == 0) backs[r] = back;
-            if (part == 0 && j < rank && rows[r] >= 0) store_4(L.u + (size_t)rows[r] * rank + j, s, rank - j, rank % 4 == 0);
+            if (part == 0 && j < rank && rows[r] >= 0 && RABIT_IN_RANGE(rows[r] < P.batch)) store_4(L.u + (size_t)rows[r] * rank + j, s, rank - j, rank % 4 == 0);
         }
         __syncthreads();
         if (turn + (int)gridDim.y < total) cluster_arrive();                // the inbox has been read: sums of the next item may come
@@ -877,7 +900,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
             const int left_cols = m_all - 32 * g - 8 * tq;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                if (has[h] && left_cols > 0) widen_store<VEC>(y[h] + 32 * g, left_cols, old[h], sum[0], h, scale * backs[8 * h + gq]);
+                if (has[h] && left_cols > 0 && RABIT_IN_RANGE(inside(y[h] + 32 * g, 2 * min(left_cols, 8), L.y, (size_t)P.batch * m_all * 2))) widen_store<VEC>(y[h] + 32 * g, left_cols, old[h], sum[0], h, scale * backs[8 * h + gq]);
         };
         for (; g < groups; g += kSets * step) {
 #pragma unroll
@@ -891,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, R16 == 1 ? 2 : 1) decode_kernel(cons
         for (int h = 0; h < 2; ++h)
             for (; bare[h] != 0u; bare[h] &= bare[h] - 1u)
                 if (turn++ % kWarps == warp)
-                    for (int j = lane; j < rank; j += 32) L.u[(size_t)(row0 + 32 * h + __ffs(bare[h]) - 1) * rank + j] = 0.f;
+                    for (int j = lane; j < rank && RABIT_IN_RANGE(row0 + 32 * h + __ffs(bare[h]) - 1 < P.batch); j += 32) L.u[(size_t)(row0 + 32 * h + __ffs(bare[h]) - 1) * rank + j] = 0.f;
     }
 }
 
@@ -977,7 +1000,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
                 if (w < warp) before += counts[w];
                 n_list += counts[w];
             }
-            if (hit) list[before + __popc(hits & ((1u << lane) - 1u))] = (int)t;
+            if (hit && RABIT_IN_RANGE(before + __popc(hits & ((1u << lane) - 1u)) < kFactorList)) list[before + __popc(hits & ((1u << lane) - 1u))] = (int)t;
             __syncthreads();
         }
         n_rows += n_list;
@@ -992,8 +1015,9 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
                     const bool in = at < n_list && col < side;
                     const __half* src = in ? S.v + (size_t)list[at] * side + col : S.v;
                     unsigned char* dst = stage + r * F::kVStride + i % kPieces * 16;
+                    if (!RABIT_IN_RANGE(inside(dst, 16, stage, F::kVBytes) && (!in || inside(src, 2 * min(side - col, 8), S.v, (size_t)P.batch * side * 2)))) continue;
                     if (VEC) copy_async_16(dst, src, in);
-                    else *reinterpret_cast<uint4*>(dst) = load_8(src, in ? side - col : 0, S.v + (size_t)P.batch * side);
+                    else *reinterpret_cast<uint4*>(dst) = load_8(src, in ? side - col : 0, S.v, S.v + (size_t)P.batch * side);
                 }
                 float* low = reinterpret_cast<float*>(stage + F::kVBytes);
                 constexpr int kFours = F::kRanks / 4;
@@ -1002,6 +1026,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
                     const bool in = at < n_list;
                     const float* src = in ? S.low + (size_t)list[at] * rank + j : S.low;
                     float* dst = low + r * F::kLowStride + j;
+                    if (!RABIT_IN_RANGE(inside(dst, 16, stage + F::kVBytes, F::kRows * F::kLowStride * 4) && (!in || j >= rank || inside(src, 4 * min(rank - j, 4), S.low, (size_t)P.batch * rank * 4)))) continue;
                     if (fours) {
                         copy_async_16(dst, in && j < rank ? src : S.low, in && j < rank);
                     } else {
@@ -1109,6 +1134,7 @@ __global__ void __launch_bounds__(kFactorThreads, 1) factor_kernel(const __grid_
         float4 total = cluster_sum(cluster, sums, parts, e);
         total.x *= scale; total.y *= scale; total.z *= scale; total.w *= scale;
         float* at = S.out + ((size_t)adapter * rank + j) * side + first + c;
+        if (!RABIT_IN_RANGE(inside(at, 4 * min(cols - c, 4), S.out, (size_t)gridDim.y * rank * side * 4))) continue;
         if (P.accumulate) {
             if (side_fours) {
                 const float4 old = *reinterpret_cast<const float4*>(at);
@@ -1423,4 +1449,17 @@ extern "C" int rabit_linear_group_adapted(const rabit_layer* const* layers, cons
 extern "C" int rabit_adapter_gradients(const rabit_adapters* adapters, const void* x, const float* u, const void* dy, const float* p, const int* ids,
                                        float* da, float* db, int batch, int accumulate, void* stream) {
     return gradients_call(adapters, x, u, dy, p, ids, da, db, batch, accumulate, stream);
+}
+
+extern "C" int rabit_selftest_index_faults(void) {
+    rabit_clear_error();
+#ifdef RABIT_CHECKED
+    unsigned int word = 0, zero = 0;
+    RABIT_CUDA_TRY(cudaDeviceSynchronize());
+    RABIT_CUDA_TRY(cudaMemcpyFromSymbol(&word, g_index_fault, sizeof word));
+    RABIT_CUDA_TRY(cudaMemcpyToSymbol(g_index_fault, &zero, sizeof zero));
+    return word ? rabit_fail(RABIT_DEVICE_FAULT, "rabit_selftest_index_faults: an index check of the adapters' kernels failed") : RABIT_OK;
+#else
+    return rabit_fail(RABIT_UNSUPPORTED_SHAPE, "rabit_selftest_index_faults: this library was built without RABIT_CHECKED");
+#endif
 }
