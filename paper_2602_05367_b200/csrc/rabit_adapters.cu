@@ -1327,11 +1327,14 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
     for (int l = 0; l < n_layers; ++l)
         if (int rc = rabit_check_call(*layers[l], batch)) return rc;
     // One launch behind the layer, or two?  The one reads the second factor again for every 16 rows, so rows times outputs decide; the two multiply every tile with
-    // each adapter in it, so where the pool has many to name the one is taken further (B200, us with the layer, one launch / two; few: up to three adapters in
-    // prompts, many: 30 among single tokens.  Rank 16, few: 256 rows of 4096 x 4096 24.8 / 25.6, 300 rows 29.7 / 27.8, 1024 rows of 1024 x 4096 27.0 / 29.5, 100 rows of 14336
-    // x 4096 31.6 / 27.4; many: 130 rows of 4096 x 4096 30 / 50, 512 rows 55 / 85, 100 rows of 14336 x 4096 46 / 59, 130 rows of 28672 x 4096 95 / 91.  Rank 64, few: 130
-    // rows of 4096 x 4096 23.9 / 26.2, 200 rows 29.9 / 28.3, 512 rows 47 / 39; many: 512 rows 111 / 141.  Outputs that are not 16-byte pieces, rank 16, few: 130 and 200 rows of
-    // 4099 x 4096 24.5 / 22.9 and 26.9 / 26.0).
+    // each adapter in it, so where the pool has many to name the one is taken further.  (B200, us with the layer, graph replays with 14 layers in turn, one launch / two.
+    // Three adapters in prompts, rank 16: 200 rows of 4096 x 4096 22.8 / 23.5, 256 rows 25.3 / 26.5, 512 rows 36.4 / 36.7, 1000 rows of 1024 x 4096 28.0 / 28.8, 130 rows of 8192 x
+    // 4096 29.9 / 28.2; rank 32: 256 rows of 4096 x 4096 28.5 / 29.3, 512 rows 38.2 / 36.7; rank 64: 130 rows 25.0 / 29.3, 200 rows 31.2 / 29.6; rank 128: 130 rows 34.9 / 35.9, 200 rows
+    // 45.3 / 36.7.  Outputs that are not 16-byte pieces, 4099 x 4096: rank 16 80 rows 21.2 / 21.7, 90 rows 21.6 / 21.1, 130 rows 25.1 / 24.2; rank 32 256 rows 32.4 / 33.9;
+    // rank 64 256 rows 38.2 / 44.4, 400 rows 48.3 / 47.7; rank 128 256 rows 54.6 / 58.3.  30 adapters among single tokens: rank 16 130 rows of 4096 x 4096 30 / 50, 512 rows 55 / 85; rank 64 512 rows 111 / 141.)
+    // The ids are on the device, so the size of the pool stands for how many adapters the rows name.  Rows that name one of a pool of 32 lose by that: 512 rows of 4096 x
+    // 4096 40.0 / 34.0 at rank 16, 47.7 / 38.9 at rank 64.  Up to 64 rows it is one launch whatever the rest: with 30 adapters 64 rows of 14336 x 4096 30 / 54 at rank 16,
+    // 57 / 93 at rank 64, with eight 26.3 / 34.7 and 39.9 / 51.2; with three it loses where outputs are many, 26.5 / 22.8 and 35.9 / 27.4.
     bool vec = true;
     long long outputs = 0;
     int most_rank = 0, most_count = 0;
@@ -1342,7 +1345,7 @@ int adapted_call(const char* who, const rabit_layer* const* layers, const rabit_
         most_rank = std::max(most_rank, adapters[l]->rank);
         most_count = std::max(most_count, adapters[l]->count);
     }
-    const long long most = most_count > 8 ? 1LL << 21 : most_rank > 32 || (!vec && most_rank <= 16) ? 5LL << 17 : 1LL << 20;
+    const long long most = most_count > 8 ? 1LL << 21 : !vec && most_rank <= 16 ? 3LL << 17 : most_rank > 32 && vec ? 5LL << 17 : 1LL << 20;
     const bool decode = batch <= kWindow || (batch <= kDecodeRows && batch * outputs <= most);
     bool beside = false;
     if (int rc = rabit_run_layers(layers, xs, ys, n_layers, batch, stream, &beside)) return rc;

@@ -203,7 +203,7 @@ def test_what_the_layer_refuses_leaves_y_and_u_as_they_were(variant, batch, M):
 
 @pytest.mark.parametrize("variant,batch,M,N,r,kind", [
     (0, 2, 509, 512, 5, "one"), (0, 6, 509, 512, 33, "mixed"), (0, 12, 509, 512, 5, "mixed"), (0, 16, 509, 512, 33, "prompts"), (0, 48, 509, 512, 33, "mixed"), (0, 200, 509, 512, 5, "prompts"),
-    (0, 200, 4099, 4128, 5, "mixed"), (0, 200, 4099, 4128, 33, "prompts"), (0, 300, 4099, 4128, 21, "mixed"), (0, 1100, 509, 512, 5, "mixed"), (0, 1100, 509, 512, 33, "prompts"),
+    (0, 200, 4099, 4128, 5, "mixed"), (0, 200, 4099, 4128, 33, "prompts"), (0, 300, 4099, 4128, 33, "prompts"), (0, 300, 4099, 4128, 21, "mixed"), (0, 1100, 509, 512, 5, "mixed"), (0, 1100, 509, 512, 33, "prompts"),
     (0, 1100, 509, 512, 3, "none"), (1, 1100, 509, 512, 5, "mixed"), (5, 1100, 512, 512, 16, "prompts"), (5, 1100, 509, 512, 33, "mixed"), (4, 1100, 509, 512, 100, "mixed")])
 def test_a_chain_of_calls_with_odd_outputs_and_ranks(variant, batch, M, N, r, kind):
     """As the chains of square layers, in both forms, behind every kind of layer kernel: y of one call lies in the memory that the next one reads as x, u is shared, ids and
