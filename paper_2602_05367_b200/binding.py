@@ -412,7 +412,9 @@ class RabitAdapters:
 def rabit_linear_adapted(layer: RabitLayer, adapters: RabitAdapters, x, ids, y=None, u=None, stream: Optional[int] = None):
     """y[t] = layer(x[t]) + scale[i] * b[i]^T (a[i] x[t]) with i = ids[t] (CUDA int32 [batch]; outside the pool: no adapter).  u, if given,
     receives the low-rank products (CUDA float32 [batch][rank]; zero for rows without adapter).  Returns y [batch][M].
-    With rabit_transpose(layer) and adapters.transposed() and the gradient of y as x it gives the gradient of x."""
+    With rabit_transpose(layer) and adapters.transposed() and the gradient of y as x it gives the gradient of x: like every call here it leaves no autograd
+    history, whatever requires_grad says; the backward pass is this call and rabit_adapter_gradients, for an autograd.Function to make.
+    y and u that the call makes itself belong to the given stream's memory pool."""
     return _native.linear_adapted(layer, adapters, x, ids, y, u, stream)
 
 
@@ -440,13 +442,15 @@ def rabit_transpose(layer: RabitLayer, stream: Optional[int] = None) -> RabitLay
 def rabit_adapter_gradients(adapters: RabitAdapters, x, u, dy, p, ids, da=None, db=None, accumulate: bool = False, stream: Optional[int] = None):
     """Gradients of the factors: da[i] = scale[i] * sum of p[t]^T x[t] and db[i] = scale[i] * sum of u[t]^T dy[t] over the rows t with
     ids[t] = i.  x float16 [batch][N] and u float32 [batch][rank] of the forward call, dy float16 [batch][M] and p float32 [batch][rank]
-    of the backward call on the transposed layer.  da, db: CUDA float32 like a and b, overwritten or, with `accumulate`, added to."""
+    of the backward call on the transposed layer.  da, db: CUDA float32 like a and b, overwritten or, with `accumulate`, added to.  They are returned, not put
+    into any .grad."""
     return _native.adapter_gradients(adapters, x, u, dy, p, ids, da, db, accumulate, stream)
 
 
 class RabitGradients:
     """Gradient tensors (contiguous CUDA float32, any number of them, all on one device) that rabit_clip_gradients treats as one vector; clipped
-    in place, or into `outs`.  Holds the tensors and the buffer with their table and the partial sums."""
+    in place, or into `outs`.  Holds the tensors and the buffer with their table and the partial sums.  Making one waits for the stream (the table
+    is in place then): it is meant to be made once for tensors that stay where they are."""
 
     def __init__(self, tensors, outs=None, stream: Optional[int] = None):
         tensors, outs = list(tensors), None if outs is None else list(outs)

@@ -296,3 +296,21 @@ def test_bound_gradients_may_be_clipped_on_any_stream():
     norm = rabit.rabit_clip_gradients(G, 1.0)
     torch.cuda.synchronize()
     assert abs(float(norm) - 2 * np.sqrt(5000)) < 1e-3 and abs(float(t[0]) - 1 / np.sqrt(5000)) < 1e-6
+
+
+def test_the_calls_leave_no_autograd_history():
+    """As they say: what they return needs no gradient, and nothing is put into .grad."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    M, N, batch, r = 64, 96, 4, 8
+    L = make_layer(M, N, 1, key=(115,))
+    a, b, scale = _pool(M, N, 2, r, 90)
+    layer, A = rabit.rabit_pack(L.planes, L.g, L.h), _adapters(a, b, scale)
+    xd, idd, dyd = _cuda(make_x(batch, N, key=(115, 1)), np.zeros(batch, np.int32), make_x(batch, M, key=(115, 2)))
+    for t in (A.a, A.b, A.scale, xd, dyd):
+        t.requires_grad_()
+    u = torch.empty((batch, r), device="cuda")
+    y = rabit.rabit_linear_adapted(layer, A, xd, idd, None, u)
+    da, db = rabit.rabit_adapter_gradients(A, xd, u, dyd, u, idd)
+    assert not any(t.requires_grad for t in (y, u, da, db)) and all(t.grad is None for t in (A.a, A.b, A.scale, xd, dyd))
+    layer.free()
