@@ -314,3 +314,52 @@ def test_the_calls_leave_no_autograd_history():
     da, db = rabit.rabit_adapter_gradients(A, xd, u, dyd, u, idd)
     assert not any(t.requires_grad for t in (y, u, da, db)) and all(t.grad is None for t in (A.a, A.b, A.scale, xd, dyd))
     layer.free()
+
+
+@pytest.mark.parametrize("n_in,n_out", [(1, 7), (5, 3), (8, 2), (9, 15), (257, 1)])
+@pytest.mark.parametrize("batch,r", [(1, 1), (3, 5), (70, 16), (300, 33)])
+def test_factor_gradients_of_narrow_sides(n_in, n_out, batch, r):
+    """Sides below the eight values of a 16-byte piece: the last rows of x and dy end inside the last piece of their buffer."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    n = 3
+    rng = np.random.default_rng([31, n_in, n_out, batch, r])
+    a, b, scale = rng.standard_normal((n, r, n_in)).astype(np.float16), rng.standard_normal((n, r, n_out)).astype(np.float16), rng.uniform(0.5, 2.0, n).astype(np.float32)
+    x, dy = rng.standard_normal((batch, n_in)).astype(np.float16), rng.standard_normal((batch, n_out)).astype(np.float16)
+    u, p = rng.standard_normal((batch, r)).astype(np.float32), rng.standard_normal((batch, r)).astype(np.float32)
+    ids = rng.integers(-1, n, batch).astype(np.int32)
+    guard = [torch.full((n * r * side + 8,), 3.0, device="cuda") for side in (n_in, n_out)]
+    outs = [g[:n * r * side].view(n, r, side) for g, side in zip(guard, (n_in, n_out))]
+    rabit.rabit_adapter_gradients(_adapters(a, b, scale), *_cuda(x, u, dy, p, ids), *outs)
+    for got, g, v, low in zip(outs, guard, (x, dy), (p, u)):
+        _within(got.cpu().numpy(), *ao.gradients(scale, v, low, ids, n), "gradient")
+        assert (g[-8:] == 3.0).all()
+
+
+@pytest.mark.parametrize("batch,r,kind", [(2, 5, "one"), (12, 33, "mixed"), (200, 5, "prompts"), (1100, 33, "mixed")])
+def test_a_captured_chain_with_odd_outputs(batch, r, kind):
+    """The chain in a graph that is replayed twice without a stop: bit for bit the calls one by one."""
+    import torch
+    import paper_2602_05367_b200 as rabit
+    M, N, n, steps = 509, 512, 3, 4
+    L = make_layer(M, N, 2, key=(116,))
+    layer, A = rabit.rabit_pack(L.planes, (L.g.astype(np.float32) / 16).astype(np.float16), L.h), _adapters(*_pool(M, N, n, r, 91))
+    xd, idd = _cuda(make_x(batch, N, key=(116, batch)), _ids(batch, n, kind))
+    bufs = [xd] + [torch.zeros((batch, N), dtype=torch.float16, device="cuda") for _ in range(steps)]
+    u, s, graph = torch.zeros((batch, r), device="cuda"), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    out = [t.view(-1)[:batch * M].view(batch, M) for t in bufs]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        for k in range(steps):
+            rabit.rabit_linear_adapted(layer, A, bufs[k], idd, out[k + 1], u)
+    for rep in range(3):
+        xd.copy_(_cuda(make_x(batch, N, key=(116, batch, rep)))[0])
+        want = [xd.clone()] + [torch.zeros_like(xd) for _ in range(steps)]
+        for k in range(steps):
+            rabit.rabit_linear_adapted(layer, A, want[k], idd, want[k + 1].view(-1)[:batch * M].view(batch, M))
+            torch.cuda.synchronize()
+        for _ in range(2):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(v, w) for v, w in zip(bufs, want))
+    layer.free()

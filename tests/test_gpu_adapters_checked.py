@@ -31,7 +31,7 @@ def test_the_adapters_pass_under_the_checked_build():
     if not os.path.exists(lib) or any(os.path.getmtime(f) > os.path.getmtime(lib) for f in sources):
         build.build(checked=True)
     cmd = [sys.executable, "-c", CHILD, os.path.join(ROOT, "tests", "test_gpu_adapters.py"), os.path.join(ROOT, "tests", "test_gpu_adapters_calls.py"),
-           "-k", "adapted or finite or any_size or chain or captured or gradients or training or 32_bits or slot or small_low_rank"]
+           "-k", "adapted or finite or any_size or chain or captured or gradients or training or 32_bits or slot or small_low_rank or narrow_sides"]
     proc = subprocess.run(cmd, cwd=ROOT, env=dict(os.environ, RABIT_LIBRARY=lib), capture_output=True, text=True, timeout=1200)
     assert proc.returncode == 0, proc.stdout[-3000:] + proc.stderr[-2000:]
     assert " passed" in proc.stdout and "index faults: 0" in proc.stdout
